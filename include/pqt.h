@@ -377,6 +377,94 @@ int pqt_stage_times(pqt_index* index, float ms[4], int* calls);
  */
 int pqt_measure_peaks(int device, double* hbm_read_gb_per_s, double* mfma_f32_tflop_per_s);
 
+/*
+ * The query encoder's operators -- what stands between the tokens of a text and the vectors the index is built from
+ * and asked with: rows of an embedding table, layer norm, and products with 8-bit weights, each with its gradient.  They
+ * belong to no index.  Conventions common to all of them:
+ *   - matrices are row-major device arrays on GPU `device`; a row begins `stride` elements after the one before
+ *     (stride >= the row's length, any number; a slice of a wider buffer needs no copy), and every pointer is aligned to
+ *     its element's size;
+ *   - element types are PQT_F32, PQT_BF16 and PQT_F16; sums, statistics and scales are fp32, rounded to nearest even once
+ *     when the result is stored;
+ *   - calls only enqueue work on hip_stream (NULL = the default stream), allocate nothing and may be captured
+ *     into a graph; a call that needs scratch memory takes it from the caller, with the size the function beside it names
+ *     (any alignment of 16 bytes, contents arbitrary, in use until the call's work is done; calls that overlap in time need one each);
+ *   - outputs must not overlap inputs; the same inputs give the same bytes;
+ *   - errors: PQT_EINVAL (null or misaligned pointer, size or stride out of range, unknown type, workspace too small),
+ *     PQT_EUNSUPPORTED (limits named below), PQT_EHIP.  Calls with no rows do nothing, except that sums over no rows are
+ *     zero.
+ */
+#define PQT_F32  0
+#define PQT_BF16 1
+#define PQT_F16  2
+
+/*
+ * pqt_embed -- out[t] = scale * table[tokens[t]] for n tokens; table is V x D of type `type`, out n x D of `out_type`.
+ * tokens: device array of n integers of token_bytes = 4 (int32) or 8 (int64).  A token outside 0 .. V-1 gives a row of
+ * zeros (so that -1 can stand for padding).
+ *
+ * pqt_embed_gradient -- out[v] = scale * sum of grad[t] over the places t with tokens[t] == v, ascending in groups
+ * of fixed size, for all v in 0 .. V-1 (zeros where v has no place); tokens outside 0 .. V-1 add to nothing.
+ * With accumulate != 0 that is added to what out holds, and rows without a place are not touched.  grad is n x D of
+ * `grad_type`, out V x D of `out_type`.
+ * D up to 2^20; for the gradient n below 2^31 and V up to 2^29 (beyond: PQT_EUNSUPPORTED).
+ */
+int pqt_embed(const void* table, int type, int64_t V, int64_t D, int64_t table_stride, const void* tokens, int token_bytes,
+              int64_t n, float scale, void* out, int out_type, int64_t out_stride, int device, void* hip_stream);
+size_t pqt_embed_gradient_workspace(int64_t n, int64_t V, int64_t D);
+int pqt_embed_gradient(const void* grad, int grad_type, int64_t grad_stride, const void* tokens, int token_bytes, int64_t n,
+                       int64_t V, int64_t D, float scale, int accumulate, void* out, int out_type, int64_t out_stride,
+                       void* workspace, size_t workspace_bytes, int device, void* hip_stream);
+
+/*
+ * pqt_layer_norm -- for every row x of D values: mean mu, rstd = 1 / sqrt(mean of (x - mu)^2 + eps) (two passes over the
+ * row, in registers), y = (x - mu) * rstd * weight + bias.  x is rows x D of `type`, y rows x D of `out_type`.  weight
+ * and bias: D values of param_type, either may be NULL (ones, zeros).  mean, rstd: fp32 arrays of `rows` values for the
+ * backward pass, either may be NULL.  1 <= D <= 32768 (above: PQT_EUNSUPPORTED), eps >= 0.
+ *
+ * pqt_layer_norm_gradient -- with h = (x - mean) * rstd and g = grad * weight:
+ *     dx = rstd * (g - mean(g) - h * mean(g * h)),   dweight = sum over rows of grad * h,   dbias = sum over rows of grad.
+ * grad, x and dx are rows x D of `type`; mean and rstd as pqt_layer_norm wrote them; weight may be NULL (ones); dweight
+ * and dbias: D fp32 values each, either may be NULL.
+ */
+int pqt_layer_norm(const void* x, int type, int64_t rows, int64_t D, int64_t x_stride, const void* weight, const void* bias,
+                   int param_type, float eps, void* y, int out_type, int64_t y_stride, float* mean, float* rstd, int device,
+                   void* hip_stream);
+size_t pqt_layer_norm_gradient_workspace(int64_t rows, int64_t D);
+int pqt_layer_norm_gradient(const void* grad, int64_t grad_stride, const void* x, int64_t x_stride, int type, int64_t rows,
+                            int64_t D, const void* weight, int param_type, const float* mean, const float* rstd, void* dx,
+                            int64_t dx_stride, float* dweight, float* dbias, void* workspace, size_t workspace_bytes,
+                            int device, void* hip_stream);
+
+/*
+ * 8-bit blocks.  A matrix of `rows` rows of `cols` values is held as
+ *     codes   rows x Kp bytes, Kp = cols rounded up to a multiple of PQT_BLOCK: OCP e4m3 numbers, zeros past `cols`
+ *     scales  rows x Kp / PQT_BLOCK bytes: e + 127 for the block's scale 2^e
+ * and stands for codes * 2^e.  e is the smallest integer >= -126 with max |x| <= 448 * 2^e over the finite values of the
+ * block; a value is the nearest e4m3 number to x * 2^-e (ties to even); infinities and NaN become NaN (code 0x7f).
+ * Both arrays are aligned to 16 bytes (codes) and to 1.  Powers of two change no bit of a value, and
+ * the matrix instruction multiplies by them itself.
+ *
+ * pqt_block_quantize -- the blocks of x (rows x cols of `type`, blocks along its rows) to codes / scales, and those of its
+ * transpose (cols x rows, blocks down its columns) to codes_t / scales_t, in one reading of x; either pair may be
+ * NULL.  The transpose's are what the gradients of a product take: kept from the forward pass, they are its
+ * input's checkpoint in half the bytes.
+ *
+ * pqt_block_product -- out[i][j] = bias[j] + sum over k of A[i][k] * B[j][k], A an m x k matrix and B an n x k matrix in
+ * 8-bit blocks, sums fp32; bias: n fp32 values or NULL; out m x n of `out_type`.  fp32 results are those of fp32 additions; for 16-bit ones
+ * a product may lose what lies below 2^-13 of the largest of eight neighbouring products (2^-10 of the sum of |A B| at
+ * most; 1.4e-5 of the result's size on normal data, far below its rounding).  Values below 2^-126 may count as zero.  With x (m x k) and weights w
+ * (n x k) in blocks: y = x w^T; dx = g w is the product of g's blocks with those of w's transpose; dw = g^T x that of the blocks
+ * of g's transpose with those of x's.  m, n and k below 2^31, k at least 1.
+ */
+#define PQT_BLOCK 128
+int pqt_block_quantize(const void* x, int type, int64_t rows, int64_t cols, int64_t x_stride, uint8_t* codes, uint8_t* scales,
+                       uint8_t* codes_t, uint8_t* scales_t, int device, void* hip_stream);
+size_t pqt_block_product_workspace(int64_t m, int64_t n, int64_t k);
+int pqt_block_product(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, int64_t m,
+                      int64_t n, int64_t k, const float* bias, void* out, int out_type, int64_t out_stride, void* workspace,
+                      size_t workspace_bytes, int device, void* hip_stream);
+
 /* Message of the last failing call on this thread ("" if none).  Static storage. */
 const char* pqt_last_error(void);
 

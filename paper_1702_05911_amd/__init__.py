@@ -10,7 +10,7 @@ machine without the compiled library; using the query path without it raises Imp
 """
 import importlib
 
-_BINDING_NAMES = ("Index", "Builder", "PqtError", "last_error")
+_BINDING_NAMES = ("Index", "Builder", "Blocks", "PqtError", "last_error")
 
 
 def __getattr__(name):

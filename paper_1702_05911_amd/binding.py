@@ -4,6 +4,7 @@ Every step of the query path runs inside libpqt.so's HIP kernels.  PyTorch is us
 device memory (tensors own the query/result buffers) and for the stream handle; there is
 no CPU fallback -- if the library is missing, importing this module raises.
 """
+import collections
 import ctypes
 import os
 
@@ -20,7 +21,9 @@ EXPORTS = (
     "pqt_builder_finish", "pqt_builder_free", "pqt_index_free", "pqt_index_info", "pqt_set_budget", "pqt_query_batch",
     "pqt_query_batch_debug", "pqt_query_batch_noalloc", "pqt_noalloc_workspace_bytes", "pqt_set_bin_order",
     "pqt_index_set_vectors", "pqt_query_batch_exact", "pqt_brute_force", "pqt_measure_peaks", "pqt_set_profiling",
-    "pqt_stage_times", "pqt_last_error",
+    "pqt_stage_times", "pqt_embed", "pqt_embed_gradient_workspace", "pqt_embed_gradient", "pqt_layer_norm",
+    "pqt_layer_norm_gradient_workspace", "pqt_layer_norm_gradient", "pqt_block_quantize", "pqt_block_product_workspace",
+    "pqt_block_product", "pqt_last_error",
 )
 
 
@@ -116,6 +119,25 @@ def load_library(path=LIB_PATH):
     lib.pqt_set_profiling.restype = ci
     lib.pqt_stage_times.argtypes = [vp, ctypes.POINTER(ctypes.c_float * 4), ctypes.POINTER(ci)]
     lib.pqt_stage_times.restype = ci
+    sz, cf = ctypes.c_size_t, ctypes.c_float
+    lib.pqt_embed.argtypes = [vp, ci, i64, i64, i64, vp, ci, i64, cf, vp, ci, i64, ci, vp]
+    lib.pqt_embed.restype = ci
+    lib.pqt_embed_gradient_workspace.argtypes = [i64, i64, i64]
+    lib.pqt_embed_gradient_workspace.restype = sz
+    lib.pqt_embed_gradient.argtypes = [vp, ci, i64, vp, ci, i64, i64, i64, cf, ci, vp, ci, i64, vp, sz, ci, vp]
+    lib.pqt_embed_gradient.restype = ci
+    lib.pqt_layer_norm.argtypes = [vp, ci, i64, i64, i64, vp, vp, ci, cf, vp, ci, i64, vp, vp, ci, vp]
+    lib.pqt_layer_norm.restype = ci
+    lib.pqt_layer_norm_gradient_workspace.argtypes = [i64, i64]
+    lib.pqt_layer_norm_gradient_workspace.restype = sz
+    lib.pqt_layer_norm_gradient.argtypes = [vp, i64, vp, i64, ci, i64, i64, vp, ci, vp, vp, vp, i64, vp, vp, vp, sz, ci, vp]
+    lib.pqt_layer_norm_gradient.restype = ci
+    lib.pqt_block_quantize.argtypes = [vp, ci, i64, i64, i64, vp, vp, vp, vp, ci, vp]
+    lib.pqt_block_quantize.restype = ci
+    lib.pqt_block_product_workspace.argtypes = [i64, i64, i64]
+    lib.pqt_block_product_workspace.restype = sz
+    lib.pqt_block_product.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, ci, i64, vp, sz, ci, vp]
+    lib.pqt_block_product.restype = ci
     lib.pqt_last_error.argtypes = []
     lib.pqt_last_error.restype = ctypes.c_char_p
     return lib
@@ -385,6 +407,218 @@ def pqt_measure_peaks(device=0):
     bw, fl = ctypes.c_double(), ctypes.c_double()
     _check(_lib.pqt_measure_peaks(int(device), ctypes.byref(bw), ctypes.byref(fl)))
     return bw.value, fl.value
+
+
+# ---- the query encoder's operators ---------------------------------------------------------------
+PQT_F32, PQT_BF16, PQT_F16 = 0, 1, 2
+PQT_BLOCK = 128
+_TYPES = {torch.float32: PQT_F32, torch.bfloat16: PQT_BF16, torch.float16: PQT_F16}
+_TOKEN_BYTES = {torch.int32: 4, torch.int64: 8}
+
+# A matrix in 8-bit blocks: codes (rows, cols rounded up to 128) float8_e4m3fn, scales (rows, blocks) uint8, cols.
+Blocks = collections.namedtuple("Blocks", "codes scales cols")
+
+
+def _matrix(name, t, shape=None, dtype=None):
+    """A matrix the library can read or write in place: (pointer, type, elements from row to row)."""
+    kind = _TYPES.get(t.dtype)
+    if kind is None or not t.is_cuda or t.dim() != 2 or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must be a 2-D {'float32, bfloat16 or float16' if dtype is None else dtype} CUDA tensor")
+    rows, cols = t.shape
+    if shape is not None and (rows, cols) != shape:
+        raise ValueError(f"{name} has shape {(rows, cols)}, expected {shape}")
+    step, unit = t.stride()
+    if cols > 1 and unit != 1 or rows > 1 and step < cols:
+        raise ValueError(f"{name}: the values of a row must lie side by side, and rows must not overlap (strides {(step, unit)})")
+    return t.data_ptr(), kind, max(step, cols)
+
+
+def _vector(name, t, length, dtypes, device):
+    """A contiguous vector, or None: its pointer."""
+    if t is None:
+        return None
+    if t.dtype not in dtypes or t.device != device or tuple(t.shape) != (length,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {length} values on {device}, of type {' or '.join(map(str, dtypes))}")
+    return t.data_ptr()
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, expected {device}")
+
+
+class _On:
+    """The stream of a call: what the call allocates belongs to it."""
+
+    def __init__(self, stream, device):
+        self.stream = torch.cuda.current_stream(device) if stream is None else stream
+        self.handle = self.stream.cuda_stream
+        self._given = None if stream is None else torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self._given is not None:
+            self._given.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self._given is not None:
+            self._given.__exit__(*exc)
+
+
+def _workspace(nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _tokens(tokens, device):
+    size = _TOKEN_BYTES.get(tokens.dtype)
+    if size is None or tokens.device != device or tokens.dim() != 1 or not tokens.is_contiguous():
+        raise ValueError(f"tokens must be a contiguous 1-D int32 or int64 tensor on {device}")
+    return tokens.data_ptr(), size, tokens.shape[0]
+
+
+def pqt_embed(table, tokens, scale=1.0, out=None, out_dtype=None, stream=None):
+    """pqt_embed.  table: (V, D); tokens: (n,) int32 or int64.  Returns (n, D): scale * table[tokens], rows of zeros for
+    tokens outside the table."""
+    ptr, kind, step = _matrix("table", table)
+    V, D = table.shape
+    tok, size, n = _tokens(tokens, table.device)
+    with _On(stream, table.device) as on:
+        if out is None:
+            out = torch.empty((n, D), dtype=out_dtype or table.dtype, device=table.device)
+        _same_device(table.device, out=out)
+        optr, okind, ostep = _matrix("out", out, (n, D), out_dtype)
+        _check(_lib.pqt_embed(ptr, kind, V, D, step, tok, size, n, scale, optr, okind, ostep, table.device.index, on.handle))
+    return out
+
+
+def pqt_embed_gradient(grad, tokens, V, scale=1.0, out=None, out_dtype=torch.float32, accumulate=False, stream=None):
+    """pqt_embed_gradient.  grad: (n, D).  Returns (V, D): scale times the sum of every token's rows; accumulate adds it to `out`."""
+    ptr, kind, step = _matrix("grad", grad)
+    n, D = grad.shape
+    tok, size, nt = _tokens(tokens, grad.device)
+    if nt != n:
+        raise ValueError(f"{nt} tokens for {n} rows")
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    with _On(stream, grad.device) as on:
+        if out is None:
+            out = torch.empty((V, D), dtype=out_dtype, device=grad.device)
+        _same_device(grad.device, out=out)
+        optr, okind, ostep = _matrix("out", out, (V, D))
+        nbytes = _lib.pqt_embed_gradient_workspace(n, V, D)
+        ws = _workspace(nbytes, grad.device)
+        _check(_lib.pqt_embed_gradient(ptr, kind, step, tok, size, n, V, D, scale, 1 if accumulate else 0, optr, okind, ostep,
+                                       ws.data_ptr() if nbytes else None, nbytes, grad.device.index, on.handle))
+    return out
+
+
+def pqt_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, out_dtype=None, stream=None):
+    """pqt_layer_norm.  x: (rows, D); weight, bias: (D,) of one type, or None.  Returns (y, mean, rstd)."""
+    ptr, kind, step = _matrix("x", x)
+    rows, D = x.shape
+    params = weight if weight is not None else bias
+    ptype = _TYPES if params is None else (params.dtype,)
+    w, b = _vector("weight", weight, D, ptype, x.device), _vector("bias", bias, D, ptype, x.device)
+    with _On(stream, x.device) as on:
+        if out is None:
+            out = torch.empty((rows, D), dtype=out_dtype or x.dtype, device=x.device)
+        _same_device(x.device, out=out)
+        optr, okind, ostep = _matrix("out", out, (rows, D), out_dtype)
+        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+        _check(_lib.pqt_layer_norm(ptr, kind, rows, D, step, w, b, PQT_F32 if params is None else _type_of(params), eps, optr, okind, ostep,
+                                   mean.data_ptr(), rstd.data_ptr(), x.device.index, on.handle))
+    return out, mean, rstd
+
+
+def pqt_layer_norm_gradient(grad, x, weight, mean, rstd, out=None, stream=None):
+    """pqt_layer_norm_gradient.  grad, x: (rows, D) of one type; mean, rstd: what pqt_layer_norm returned.  Returns (dx, dweight,
+    dbias), the last two float32."""
+    ptr, kind, step = _matrix("x", x)
+    rows, D = x.shape
+    _same_device(x.device, grad=grad)
+    gptr, _, gstep = _matrix("grad", grad, (rows, D), x.dtype)
+    w = _vector("weight", weight, D, _TYPES, x.device)
+    mptr, rptr = (_vector(name, t, rows, (torch.float32,), x.device) for name, t in (("mean", mean), ("rstd", rstd)))
+    with _On(stream, x.device) as on:
+        if out is None:
+            out = torch.empty((rows, D), dtype=x.dtype, device=x.device)
+        _same_device(x.device, out=out)
+        optr, _, ostep = _matrix("out", out, (rows, D), x.dtype)
+        dweight, dbias = torch.empty((2, D), dtype=torch.float32, device=x.device)
+        nbytes = _lib.pqt_layer_norm_gradient_workspace(rows, D)
+        ws = _workspace(nbytes, x.device)
+        _check(_lib.pqt_layer_norm_gradient(gptr, gstep, ptr, step, kind, rows, D, w, PQT_F32 if weight is None else _type_of(weight), mptr,
+                                            rptr, optr, ostep, dweight.data_ptr(), dbias.data_ptr(), ws.data_ptr() if nbytes else None,
+                                            nbytes, x.device.index, on.handle))
+    return out, dweight, dbias
+
+
+def _type_of(t):
+    return _TYPES[t.dtype]
+
+
+def _empty_blocks(rows, cols, device):
+    kb = -(-cols // PQT_BLOCK)
+    return Blocks(torch.empty((rows, kb * PQT_BLOCK), dtype=torch.float8_e4m3fn, device=device),
+                  torch.empty((rows, kb), dtype=torch.uint8, device=device), cols)
+
+
+def _blocks(name, b):
+    rows, kp = b.codes.shape
+    kb = -(-b.cols // PQT_BLOCK)
+    if b.codes.dtype != torch.float8_e4m3fn or b.scales.dtype != torch.uint8 or not b.codes.is_cuda or b.scales.device != b.codes.device or \
+            kp != kb * PQT_BLOCK or tuple(b.scales.shape) != (rows, kb) or not b.codes.is_contiguous() or not b.scales.is_contiguous():
+        raise ValueError(f"{name} must be Blocks: contiguous float8_e4m3fn codes (rows, {kb * PQT_BLOCK}) and uint8 scales (rows, {kb}) "
+                         f"for {b.cols} columns")
+    return rows
+
+
+def pqt_block_quantize(x, rows=True, columns=False, stream=None):
+    """pqt_block_quantize.  x: (r, c).  Returns the Blocks of x (rows), of its transpose (columns), or both as a pair."""
+    ptr, kind, step = _matrix("x", x)
+    r, c = x.shape
+    if not rows and not columns:
+        raise ValueError("rows, columns, or both")
+    with _On(stream, x.device) as on:
+        a = _empty_blocks(r, c, x.device) if rows else None
+        t = _empty_blocks(c, r, x.device) if columns else None
+        _check(_lib.pqt_block_quantize(ptr, kind, r, c, step, a.codes.data_ptr() if rows else None, a.scales.data_ptr() if rows else None,
+                                       t.codes.data_ptr() if columns else None, t.scales.data_ptr() if columns else None, x.device.index,
+                                       on.handle))
+    return (a, t) if rows and columns else a if rows else t
+
+
+def pqt_block_product(a, b, bias=None, out=None, out_dtype=torch.bfloat16, stream=None):
+    """pqt_block_product.  a, b: Blocks of m x k and n x k values; bias: (n,) float32 or None.  Returns (m, n): a b^T + bias."""
+    m, n = _blocks("a", a), _blocks("b", b)
+    device = a.codes.device
+    if a.cols != b.cols:
+        raise ValueError(f"a has {a.cols} columns, b {b.cols}")
+    _same_device(device, b=b.codes, out=out)
+    bptr = _vector("bias", bias, n, (torch.float32,), device)
+    with _On(stream, device) as on:
+        if out is None:
+            out = torch.empty((m, n), dtype=out_dtype, device=device)
+        optr, okind, ostep = _matrix("out", out, (m, n))
+        nbytes = _lib.pqt_block_product_workspace(m, n, a.cols)
+        ws = _workspace(nbytes, device)
+        _check(_lib.pqt_block_product(a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), m, n, a.cols, bptr,
+                                      optr, okind, ostep, ws.data_ptr() if nbytes else None, nbytes, device.index, on.handle))
+    return out
+
+
+# The sizes of scratch memory are asked for by the calls above; a caller of the C ABI asks for them itself.
+def pqt_embed_gradient_workspace(n, V, D):
+    return int(_lib.pqt_embed_gradient_workspace(n, V, D))
+
+
+def pqt_layer_norm_gradient_workspace(rows, D):
+    return int(_lib.pqt_layer_norm_gradient_workspace(rows, D))
+
+
+def pqt_block_product_workspace(m, n, k):
+    return int(_lib.pqt_block_product_workspace(m, n, k))
 
 
 def last_error():

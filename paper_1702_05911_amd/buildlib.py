@@ -11,7 +11,8 @@ SOURCES = ("pqt_api.hip", "pqt_host.cpp", "traverse.hip", "rank_bins.hip", "rera
            "rerank_table4.hip", "rerank_table8.hip",
            "rerank_pair_bytes.hip", "rerank_pair_long.hip", "rerank_pair2.hip", "rerank_pair4.hip", "rerank_pair6.hip",
            "rerank_pair8.hip", "rerank_pair16.hip",
-           "exact_rerank.hip", "builder.hip", "place.hip", "train.hip", "brute_force.hip", "peaks.hip")
+           "exact_rerank.hip", "builder.hip", "place.hip", "train.hip", "brute_force.hip", "peaks.hip",
+           "layer_norm.hip", "embed.hip", "block_quantize.hip", "block_product.hip")
 OUTPUT = os.path.join(HERE, "libpqt.so")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # packed fp32 instructions are kept off for all device code

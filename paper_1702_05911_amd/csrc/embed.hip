@@ -1,0 +1,478 @@
+// Rows of an embedding table for tokens, scaled, and the table's gradient.
+//
+// Lookup: out[t] = scale * table[tokens[t]].  Bound by memory: a row is read and written once.  A group of lanes (as many as the
+// row has pieces of 16 bytes, up to a wavefront) has a row or a section of one, two pieces a lane.
+//
+// Gradient: out[v] = scale * sum of grad[t] over the places of v.  Additions by atomics would give other bits on every call and
+// queue up at the tokens that are in every sentence, so the places are sorted by token first: digits of up to ten bits from
+// the lowest on, every pass stable, so that a token's places ascend.  Then the sorted places are walked in chunks of equal length,
+// one a group of lanes, whatever tokens they belong to: rows are read eight at a time, and where the token changes
+// the sum so far goes out.  A token that lies in one chunk is finished there; of the others the chunks' parts go to the workspace, and
+// join_kernel adds them in order.  Rows of tokens that do not occur are cleared beside the chunks.
+// Bound by memory: n rows read, V written; the sort moves 16 bytes a place and pass.
+#include <algorithm>
+
+#include "encoder.hpp"
+
+using pqt_host::DeviceGuard;
+using pqt_host::fail;
+
+namespace pqt {
+namespace {
+
+constexpr int kEmbedThreads = 256;
+constexpr int64_t kMaxEmbedD = 1 << 20;    // (sections of a row are the grid's second dimension: 2^16 - 1 at most)
+constexpr int64_t kMaxPlaces = 0x7fffffff; // places are 32-bit numbers
+constexpr int64_t kMaxRows = 1 << 29;      // of a gradient (64 a workgroup of 256, of 2^32 threads in all)
+constexpr int kEmbedPieces = 2;            // pieces of a row a lane has
+
+struct EmbedArgs {
+    const void* table;
+    const void* tokens;
+    void* out;
+    int64_t V, D, table_stride, n, out_stride;
+    float scale;
+    int log_lanes;                         // lanes of a row's section, log2
+    int wide_tokens;
+};
+
+__device__ __forceinline__ int64_t token_at(const void* tokens, int wide, int64_t i) {
+    return wide ? static_cast<const int64_t*>(tokens)[i] : (int64_t) static_cast<const int32_t*>(tokens)[i];
+}
+
+template <typename TX, typename TY>
+__global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs g) {
+    constexpr int E = sizeof(TX) == 2 && sizeof(TY) == 2 ? 8 : 4;           // elements of a piece
+    const int lanes = 1 << g.log_lanes, l = threadIdx.x & (lanes - 1);
+    const int64_t per_block = kEmbedThreads >> g.log_lanes;
+    const int64_t col = ((int64_t)blockIdx.y * kEmbedPieces * lanes + l) * E;
+    for (int64_t t = (int64_t)blockIdx.x * per_block + (threadIdx.x >> g.log_lanes); t < g.n; t += (int64_t)gridDim.x * per_block) {
+        const int64_t v = token_at(g.tokens, g.wide_tokens, t);
+        const bool have = v >= 0 && v < g.V;
+        const TX* src = static_cast<const TX*>(g.table) + (have ? v : 0) * g.table_stride;
+        TY* dst = static_cast<TY*>(g.out) + t * g.out_stride;
+        typename Floats<E>::type r[kEmbedPieces];
+#pragma unroll
+        for (int p = 0; p < kEmbedPieces; ++p) {
+            const int64_t c = col + (int64_t)p * lanes * E;
+            r[p] = 0.0f;
+            if (have && c < g.D) r[p] = load_piece<TX, E>(src + c, (int)min(g.D - c, (int64_t)E)) * g.scale;
+        }
+#pragma unroll
+        for (int p = 0; p < kEmbedPieces; ++p) {
+            const int64_t c = col + (int64_t)p * lanes * E;
+            if (c < g.D) store_piece<TY, E>(dst + c, r[p], (int)min(g.D - c, (int64_t)E));
+        }
+    }
+}
+
+// ---- gradient: places by token ---------------------------------------------------------------------------------------
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
+constexpr int kSortBits = 10, kSortBins = 1 << kSortBits;
+constexpr uint32_t kSortTiles = 128;       // tiles of the sort, at most: a tile adds up the counts of all of them itself
+constexpr uint32_t kSortAlone = 8192;      // places that one workgroup sorts in one launch
+
+struct SortArgs {
+    const void* tokens;
+    int wide_tokens;
+    uint32_t n, V, tile;                   // tile: places of a workgroup, a multiple of kSortThreads
+    uint32_t* key[2];                      // sorted tokens (V for those outside 0 .. V-1) and their places, to and fro
+    uint32_t* place[2];
+    uint32_t* counts;                      // tiles x kSortBins
+    int passes, bits;                      // bits of a digit
+};
+
+__device__ __forceinline__ uint32_t key_of(const SortArgs& g, int pass, uint32_t i) {
+    if (pass) return g.key[(pass - 1) & 1][i];
+    const int64_t v = token_at(g.tokens, g.wide_tokens, i);
+    return v >= 0 && v < (int64_t)g.V ? (uint32_t)v : g.V;
+}
+
+// how often every digit occurs in the tile
+__device__ void count_digits(const SortArgs& g, int pass, uint32_t first, uint32_t* hist) {
+    const int shift = pass * g.bits;
+    const uint32_t mask = (1u << g.bits) - 1u;
+    for (uint32_t b = threadIdx.x; b < kSortBins; b += kSortThreads) hist[b] = 0u;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < g.tile; i += kSortThreads)
+        if (first + i < g.n) atomicAdd(&hist[(key_of(g, pass, first + i) >> shift) & mask], 1u);
+    __syncthreads();
+}
+
+// Places of one tile, stable: every wavefront has a consecutive part of the tile and counters of its own, which start where its
+// digits' places start.  before / all: the digit's places in the tiles before this one, and in all of them (threadIdx.x is the digit).
+__device__ void place_digits(const SortArgs& g, int pass, uint32_t first, uint32_t before, uint32_t all, uint32_t (*next)[kSortBins], uint32_t* part) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const int shift = pass * g.bits;
+    const uint32_t mask = (1u << g.bits) - 1u, len = g.tile / kSortWaves;
+    uint32_t* out_key = g.key[pass & 1];
+    uint32_t* out_place = g.place[pass & 1];
+    for (uint32_t b = tid; b < kSortWaves * kSortBins; b += kSortThreads) (&next[0][0])[b] = 0u;
+    __syncthreads();
+    const uint32_t lo = first + wave * len;
+    for (uint32_t i = lane; i < len; i += kWave)
+        if (lo + i < g.n) atomicAdd(&next[wave][(key_of(g, pass, lo + i) >> shift) & mask], 1u);
+    uint32_t total;
+    uint32_t at = block_exclusive_sum(all, part, total) + before;         // (a barrier inside)
+    __syncthreads();
+    for (int w = 0; w < kSortWaves; ++w) {
+        const uint32_t c = next[w][tid];
+        next[w][tid] = at;
+        at += c;
+    }
+    __syncthreads();
+    for (uint32_t i = lane; i < len; i += kWave) {
+        const bool have = lo + i < g.n;
+        const uint32_t key = have ? key_of(g, pass, lo + i) : 0u;
+        const uint32_t place = have ? (pass ? g.place[(pass - 1) & 1][lo + i] : lo + i) : 0u;
+        const uint32_t digit = (key >> shift) & mask;
+        unsigned long long same = __ballot(have);
+        for (int b = 0; b < g.bits; ++b) {
+            const unsigned long long one = __ballot((digit >> b) & 1u);
+            same &= (digit >> b) & 1u ? one : ~one;
+        }
+        const uint32_t rank = (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
+        const uint32_t from = have ? next[wave][digit] : 0u;
+        wave_lds_order();
+        if (have) {
+            if (rank == 0) next[wave][digit] = from + (uint32_t)__popcll(same);
+            out_key[from + rank] = key;
+            out_place[from + rank] = place;
+        }
+        wave_lds_order();
+    }
+}
+
+__global__ __launch_bounds__(kSortThreads) void token_counts_kernel(SortArgs g, int pass) {
+    __shared__ uint32_t hist[kSortBins];
+    count_digits(g, pass, blockIdx.x * g.tile, hist);
+    for (uint32_t b = threadIdx.x; b < kSortBins; b += kSortThreads) g.counts[(size_t)blockIdx.x * kSortBins + b] = hist[b];
+}
+
+__global__ __launch_bounds__(kSortThreads) void token_places_kernel(SortArgs g, int pass) {
+    __shared__ uint32_t next[kSortWaves][kSortBins];
+    __shared__ uint32_t part[kSortWaves];
+    uint32_t before = 0, all = 0;
+    for (uint32_t t = 0; t < gridDim.x; ++t) {
+        const uint32_t c = g.counts[(size_t)t * kSortBins + threadIdx.x];
+        before += t < blockIdx.x ? c : 0u;
+        all += c;
+    }
+    place_digits(g, pass, blockIdx.x * g.tile, before, all, next, part);
+}
+
+// few places: all passes by one workgroup
+__global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(SortArgs g) {
+    __shared__ uint32_t next[kSortWaves][kSortBins];
+    __shared__ uint32_t part[kSortWaves];
+    __shared__ uint32_t hist[kSortBins];
+    for (int pass = 0; pass < g.passes; ++pass) {
+        count_digits(g, pass, 0, hist);
+        place_digits(g, pass, 0, 0, hist[threadIdx.x], next, part);
+        __threadfence_block();
+        __syncthreads();                                      // the next pass reads what other wavefronts wrote
+    }
+}
+
+// ---- gradient: sums ----------------------------------------------------------------------------------------------------
+constexpr int kSumThreads = 256;
+constexpr int kSumRows = 8;                // rows on their way at a time
+constexpr int kClearRows = 64;             // table rows a workgroup looks up and clears
+
+struct SumArgs {
+    const uint32_t* key;                   // n, ascending
+    const uint32_t* place;
+    const void* grad;
+    void* out;
+    float* parts;                          // chunks x 2 x D: of the token that began before the chunk, of the one that goes on after it
+    uint32_t n, V, chunk;                  // chunk: places of a group
+    uint32_t chunk_blocks;                 // workgroups with chunks; those behind them clear rows
+    int64_t D, grad_stride, out_stride;
+    float scale;
+    int log_lanes, accumulate;
+};
+
+__device__ __forceinline__ uint32_t first_not_below(const uint32_t* key, uint32_t lo, uint32_t hi, uint32_t v) {
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (key[mid] < v) lo = mid + 1; else hi = mid;
+    }
+    return lo;
+}
+
+template <typename TY, int E>
+__device__ __forceinline__ void finish_row(const SumArgs& g, uint32_t v, int64_t col, int have, typename Floats<E>::type sum) {
+    TY* dst = static_cast<TY*>(g.out) + (int64_t)v * g.out_stride + col;
+    sum = sum * g.scale;
+    if (g.accumulate) sum = sum + load_piece<TY, E>(dst, have);
+    store_piece<TY, E>(dst, sum, have);
+}
+
+template <typename TX, typename TY>
+__global__ __launch_bounds__(kSumThreads) void sum_rows_kernel(SumArgs g) {
+    constexpr int E = 16 / sizeof(TX);
+    typedef typename Floats<E>::type F;
+    const int tid = threadIdx.x;
+    if (blockIdx.x >= g.chunk_blocks) {                       // rows of tokens that have no place
+        __shared__ uint32_t absent[kClearRows];
+        const uint32_t v0 = (blockIdx.x - g.chunk_blocks) * kClearRows;
+        if (tid < kClearRows) {
+            const uint32_t v = v0 + tid;
+            const uint32_t at = first_not_below(g.key, 0, g.n, v);
+            absent[tid] = v < g.V && (at >= g.n || g.key[at] != v);
+        }
+        __syncthreads();
+        const int64_t col = ((int64_t)blockIdx.y << g.log_lanes) * E;     // the section of columns of this workgroup
+        const int64_t cols = min((int64_t)E << g.log_lanes, g.D - col);
+        const int pieces = (int)((cols + 3) / 4), total = pieces * kClearRows;
+        const float per = 1.0f / (float)pieces;
+        for (int e = tid; e < total; e += kSumThreads) {
+            const int r = (int)(((float)e + 0.5f) * per), c = (e - r * pieces) * 4;
+            if (absent[r]) store_piece<TY, 4>(static_cast<TY*>(g.out) + (int64_t)(v0 + r) * g.out_stride + col + c, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, (int)min((int64_t)4, cols - c));
+        }
+        return;
+    }
+    const int lanes = 1 << g.log_lanes, l = tid & (lanes - 1);
+    const uint32_t c = blockIdx.x * (kSumThreads >> g.log_lanes) + (tid >> g.log_lanes);
+    const uint64_t start = (uint64_t)c * g.chunk;
+    const int64_t col = (((int64_t)blockIdx.y << g.log_lanes) + l) * E;
+    if (start >= g.n || col >= g.D) return;
+    const uint32_t j0 = (uint32_t)start, j1 = (uint32_t)min((uint64_t)g.n, start + g.chunk);
+    const int have = (int)min((int64_t)E, g.D - col);
+    const TX* grad = static_cast<const TX*>(g.grad) + col;
+    uint32_t cur = g.key[j0];
+    bool from_before = j0 > 0 && g.key[j0 - 1] == cur;
+    F sum;
+    sum = 0.0f;
+    for (uint32_t j = j0; j < j1; j += kSumRows) {
+        F r[kSumRows];
+        uint32_t key[kSumRows];
+#pragma unroll
+        for (int u = 0; u < kSumRows; ++u) {
+            const uint32_t at = min(j + u, j1 - 1);
+            key[u] = g.key[at];
+            r[u] = 0.0f;
+            if (j + u < j1 && key[u] < g.V) r[u] = load_piece<TX, E>(grad + (int64_t)g.place[at] * g.grad_stride, have);
+        }
+#pragma unroll
+        for (int u = 0; u < kSumRows; ++u) {
+            if (j + u < j1) {
+                if (key[u] != cur) {
+                    if (from_before) store_piece<float, E>(g.parts + (size_t)c * 2 * g.D + col, sum, have);
+                    else finish_row<TY, E>(g, cur, col, have, sum);      // (cur < V: a larger key follows it, and V is the largest)
+                    from_before = false;
+                    cur = key[u];
+                    sum = 0.0f;
+                }
+                sum = sum + r[u];
+            }
+        }
+    }
+    if (cur >= g.V) return;
+    const bool goes_on = j1 < g.n && g.key[j1] == cur;
+    if (from_before) store_piece<float, E>(g.parts + (size_t)c * 2 * g.D + col, sum, have);
+    else if (goes_on) store_piece<float, E>(g.parts + ((size_t)c * 2 + 1) * g.D + col, sum, have);
+    else finish_row<TY, E>(g, cur, col, have, sum);
+}
+
+// The token that goes on after chunk c, if it began there: its parts, four wavefronts a quarter each.
+template <typename TY>
+__global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs g) {
+    constexpr int E = 4, kWaves = kSumThreads / kWave;
+    __shared__ f32x4 sums[kWaves][kWave];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const uint32_t c = blockIdx.x;
+    const uint64_t end = ((uint64_t)c + 1) * g.chunk;
+    if (end >= g.n) return;
+    const uint32_t j1 = (uint32_t)end, j0 = j1 - g.chunk;
+    const uint32_t v = g.key[j1 - 1];
+    if (v >= g.V || g.key[j1] != v) return;
+    if (g.key[j0] == v && j0 > 0 && g.key[j0 - 1] == v) return;       // an earlier chunk's
+    const uint32_t last = (first_not_below(g.key, j1, g.n, v + 1) - 1) / g.chunk;
+    // part 0 is chunk c's own, part i the i-th chunk's after it
+    const uint32_t parts = last - c + 1, per = (parts + kWaves - 1) / kWaves;
+    const int64_t col = ((int64_t)blockIdx.y * kWave + lane) * E;
+    const int have = (int)min((int64_t)E, g.D - col);
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (col < g.D) {
+        const uint32_t hi = min(parts, (wave + 1) * per);
+        for (uint32_t i = wave * per; i < hi; i += kSumRows) {
+            f32x4 r[kSumRows];
+#pragma unroll
+            for (int u = 0; u < kSumRows; ++u) {
+                r[u] = 0.0f;
+                if (i + u < hi) r[u] = load_piece<float, E>(g.parts + ((size_t)(c + i + u) * 2 + (i + u == 0 ? 1 : 0)) * g.D + col, have);
+            }
+#pragma unroll
+            for (int u = 0; u < kSumRows; ++u) sum = sum + r[u];
+        }
+    }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave || col >= g.D) return;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) sum = sum + sums[w][lane];
+    finish_row<TY, E>(g, v, col, have, sum);
+}
+
+// Places of a chunk: about 2,048 groups' worth, at least 16 so that few tokens are in parts, at most 256
+uint32_t chunk_places(int64_t n) {
+    uint32_t c = 16;
+    while (c < 256 && (int64_t)c * 2048 < n) c *= 2;
+    return c;
+}
+
+struct GradientSpace {                     // byte offsets of the workspace
+    size_t key[2], place[2], counts, parts, total;
+    uint32_t tile, tiles, chunk, chunks;
+};
+GradientSpace gradient_space(int64_t n, int64_t D) {
+    GradientSpace s{};
+    s.tile = (uint32_t)((n + kSortTiles - 1) / kSortTiles + kSortThreads - 1) / kSortThreads * kSortThreads;
+    if (n <= kSortAlone) s.tile = (uint32_t)(n + kSortThreads - 1) / kSortThreads * kSortThreads;
+    s.tiles = (uint32_t)((n + s.tile - 1) / s.tile);
+    s.chunk = chunk_places(n);
+    s.chunks = (uint32_t)((n + s.chunk - 1) / s.chunk);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t p = at; at += (bytes + 255) / 256 * 256; return p; };
+    for (int i = 0; i < 2; ++i) s.key[i] = take(sizeof(uint32_t) * (size_t)n);
+    for (int i = 0; i < 2; ++i) s.place[i] = take(sizeof(uint32_t) * (size_t)n);
+    s.counts = take(sizeof(uint32_t) * (size_t)s.tiles * kSortBins);
+    s.parts = take(sizeof(float) * 2 * (size_t)s.chunks * (size_t)D);
+    s.total = at;
+    return s;
+}
+
+int log_lanes_for(int64_t pieces) {
+    int l = 0;
+    while (l < 6 && ((int64_t)1 << l) < pieces) ++l;
+    return l;
+}
+
+}  // namespace
+}  // namespace pqt
+
+extern "C" {
+
+int pqt_embed(const void* table, int type, int64_t V, int64_t D, int64_t table_stride, const void* tokens, int token_bytes,
+              int64_t n, float scale, void* out, int out_type, int64_t out_stride, int device, void* hip_stream) {
+    using namespace pqt;
+    if (!known_type(type) || !known_type(out_type)) return fail(PQT_EINVAL, "pqt_embed: unknown type %d or %d", type, out_type);
+    if (token_bytes != 4 && token_bytes != 8) return fail(PQT_EINVAL, "pqt_embed: tokens of %d bytes (4 or 8)", token_bytes);
+    if (V < 1 || D < 1 || n < 0 || table_stride < D || out_stride < D)
+        return fail(PQT_EINVAL, "pqt_embed: V=%lld D=%lld n=%lld strides %lld, %lld out of range", (long long)V, (long long)D, (long long)n,
+                    (long long)table_stride, (long long)out_stride);
+    if (n == 0) return PQT_OK;
+    if (!table || !tokens || !out) return fail(PQT_EINVAL, "pqt_embed: null pointer");
+    if (!aligned_to(table, type_bytes(type)) || !aligned_to(out, type_bytes(out_type)) || !aligned_to(tokens, (size_t)token_bytes))
+        return fail(PQT_EINVAL, "pqt_embed: a pointer is not aligned to its element");
+    if (D > kMaxEmbedD) return fail(PQT_EUNSUPPORTED, "pqt_embed: D=%lld beyond 2^20", (long long)D);
+    if (const int rc = check_device(device, "pqt_embed")) return rc;
+    DeviceGuard guard(device);
+    if (!guard.ok) return fail(PQT_EHIP, "cannot select GPU %d", device);
+    const int E = type_bytes(type) == 2 && type_bytes(out_type) == 2 ? 8 : 4;
+    EmbedArgs g{table, tokens, out, V, D, table_stride, n, out_stride, scale, log_lanes_for((D + E - 1) / E), token_bytes == 8};
+    const int64_t per_block = kEmbedThreads >> g.log_lanes, section = ((int64_t)kEmbedPieces << g.log_lanes) * E;
+    const dim3 grid((unsigned)std::min<int64_t>((n + per_block - 1) / per_block, 1 << 20), (unsigned)((D + section - 1) / section));
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    with_type(type, [&](auto x) {
+        with_type(out_type, [&](auto y) {
+            hipLaunchKernelGGL((embed_kernel<decltype(x), decltype(y)>), grid, dim3(kEmbedThreads), 0, st, g);
+        });
+    });
+    HIP_TRY(hipGetLastError());
+    return PQT_OK;
+}
+
+size_t pqt_embed_gradient_workspace(int64_t n, int64_t V, int64_t D) {
+    if (n < 1 || V < 1 || D < 1 || n > pqt::kMaxPlaces || V > pqt::kMaxRows || D > pqt::kMaxEmbedD) return 0;
+    return pqt::gradient_space(n, D).total;
+}
+
+int pqt_embed_gradient(const void* grad, int grad_type, int64_t grad_stride, const void* tokens, int token_bytes, int64_t n,
+                       int64_t V, int64_t D, float scale, int accumulate, void* out, int out_type, int64_t out_stride,
+                       void* workspace, size_t workspace_bytes, int device, void* hip_stream) {
+    using namespace pqt;
+    if (!known_type(grad_type) || !known_type(out_type)) return fail(PQT_EINVAL, "pqt_embed_gradient: unknown type %d or %d", grad_type, out_type);
+    if (token_bytes != 4 && token_bytes != 8) return fail(PQT_EINVAL, "pqt_embed_gradient: tokens of %d bytes (4 or 8)", token_bytes);
+    if (V < 1 || D < 1 || n < 0 || grad_stride < D || out_stride < D)
+        return fail(PQT_EINVAL, "pqt_embed_gradient: V=%lld D=%lld n=%lld strides %lld, %lld out of range", (long long)V, (long long)D,
+                    (long long)n, (long long)grad_stride, (long long)out_stride);
+    if (n > kMaxPlaces || V > kMaxRows || D > kMaxEmbedD)
+        return fail(PQT_EUNSUPPORTED, "pqt_embed_gradient: n=%lld V=%lld D=%lld beyond the limits", (long long)n, (long long)V, (long long)D);
+    if (!out || (n > 0 && (!grad || !tokens))) return fail(PQT_EINVAL, "pqt_embed_gradient: null pointer");
+    if (!aligned_to(grad, type_bytes(grad_type)) || !aligned_to(out, type_bytes(out_type)) || !aligned_to(tokens, (size_t)token_bytes))
+        return fail(PQT_EINVAL, "pqt_embed_gradient: a pointer is not aligned to its element");
+    const GradientSpace s = n ? gradient_space(n, D) : GradientSpace{};
+    if (s.total && (!workspace || workspace_bytes < s.total || !aligned_to(workspace, 16)))
+        return fail(PQT_EINVAL, "pqt_embed_gradient: workspace of %zu bytes, aligned to 16, needed (%zu given)", s.total, workspace_bytes);
+    if (n == 0 && accumulate) return PQT_OK;
+    if (const int rc = check_device(device, "pqt_embed_gradient")) return rc;
+    DeviceGuard guard(device);
+    if (!guard.ok) return fail(PQT_EHIP, "cannot select GPU %d", device);
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    SumArgs g{};
+    if (n) {
+        SortArgs o{};
+        o.tokens = tokens;
+        o.wide_tokens = token_bytes == 8;
+        o.n = (uint32_t)n;
+        o.V = (uint32_t)V;
+        o.tile = s.tile;
+        for (int i = 0; i < 2; ++i) {
+            o.key[i] = reinterpret_cast<uint32_t*>(ws + s.key[i]);
+            o.place[i] = reinterpret_cast<uint32_t*>(ws + s.place[i]);
+        }
+        o.counts = reinterpret_cast<uint32_t*>(ws + s.counts);
+        int bits = 1;
+        while (bits < 32 && ((uint64_t)V >> bits) != 0) ++bits;             // V itself is a key
+        o.passes = (bits + kSortBits - 1) / kSortBits;
+        o.bits = (bits + o.passes - 1) / o.passes;
+        if (s.tiles == 1) {
+            hipLaunchKernelGGL(sort_tokens_kernel, dim3(1), dim3(kSortThreads), 0, st, o);
+            HIP_TRY(hipGetLastError());
+        } else {
+            for (int pass = 0; pass < o.passes; ++pass) {
+                hipLaunchKernelGGL(token_counts_kernel, dim3(s.tiles), dim3(kSortThreads), 0, st, o, pass);
+                HIP_TRY(hipGetLastError());
+                hipLaunchKernelGGL(token_places_kernel, dim3(s.tiles), dim3(kSortThreads), 0, st, o, pass);
+                HIP_TRY(hipGetLastError());
+            }
+        }
+        g.key = o.key[(o.passes - 1) & 1];
+        g.place = o.place[(o.passes - 1) & 1];
+    }
+    g.grad = grad;
+    g.out = out;
+    g.parts = reinterpret_cast<float*>(ws + s.parts);
+    g.n = (uint32_t)n;
+    g.V = (uint32_t)V;
+    g.chunk = n ? s.chunk : 1;
+    g.D = D;
+    g.grad_stride = grad_stride;
+    g.out_stride = out_stride;
+    g.scale = scale;
+    g.accumulate = accumulate != 0;
+    const int E = 16 / (int)type_bytes(grad_type);
+    g.log_lanes = log_lanes_for((D + E - 1) / E);
+    const uint32_t groups = kSumThreads >> g.log_lanes;
+    const int64_t section = (int64_t)E << g.log_lanes;
+    g.chunk_blocks = (s.chunks + groups - 1) / groups;
+    const uint32_t clear = accumulate ? 0 : (uint32_t)((V + kClearRows - 1) / kClearRows);
+    const dim3 grid(g.chunk_blocks + clear, (unsigned)((D + section - 1) / section));
+    with_type(grad_type, [&](auto x) {
+        with_type(out_type, [&](auto y) {
+            hipLaunchKernelGGL((sum_rows_kernel<decltype(x), decltype(y)>), grid, dim3(kSumThreads), 0, st, g);
+        });
+    });
+    HIP_TRY(hipGetLastError());
+    if (s.chunks > 1) {
+        const dim3 join(s.chunks - 1, (unsigned)((D + 4 * kWave - 1) / (4 * kWave)));
+        with_type(out_type, [&](auto y) { hipLaunchKernelGGL((join_kernel<decltype(y)>), join, dim3(kSumThreads), 0, st, g); });
+        HIP_TRY(hipGetLastError());
+    }
+    return PQT_OK;
+}
+
+}  // extern "C"

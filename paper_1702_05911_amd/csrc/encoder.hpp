@@ -1,0 +1,110 @@
+// What the query encoder's kernels share (embed.hip, layer_norm.hip, block_quantize.hip, block_product.hip): the element
+// types, rows read and written in pieces, sums over a group of lanes, and the checks of the C entries.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "pqt_device.hpp"
+#include "pqt_index.hpp"
+
+namespace pqt {
+
+struct Bf16 { uint16_t bits; };
+typedef _Float16 Half;
+
+// Pieces of a row.  Rows begin wherever an element may (odd lengths, slices of wider buffers): the pieces are declared
+// with the alignment of one element, and the memory system takes 16-byte accesses at such addresses as they are.
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+    typedef float v4 __attribute__((ext_vector_type(4), aligned(4)));
+    typedef float v8 __attribute__((ext_vector_type(8), aligned(4)));
+};
+template <> struct Vec<Bf16> {
+    typedef __bf16 v4 __attribute__((ext_vector_type(4), aligned(2)));
+    typedef __bf16 v8 __attribute__((ext_vector_type(8), aligned(2)));
+};
+template <> struct Vec<Half> {
+    typedef _Float16 v4 __attribute__((ext_vector_type(4), aligned(2)));
+    typedef _Float16 v8 __attribute__((ext_vector_type(8), aligned(2)));
+};
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+template <int N> struct Floats;
+template <> struct Floats<4> { typedef f32x4 type; };
+template <> struct Floats<8> { typedef f32x8 type; };
+template <typename T, int N> struct Piece_;
+template <typename T> struct Piece_<T, 4> { typedef typename Vec<T>::v4 type; };
+template <typename T> struct Piece_<T, 8> { typedef typename Vec<T>::v8 type; };
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(Half v) { return (float)v; }
+__device__ __forceinline__ float to_float(Bf16 v) { return __uint_as_float((uint32_t)v.bits << 16); }
+template <typename T> __device__ __forceinline__ T from_float(float v);           // to nearest even
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ Half from_float<Half>(float v) { return (Half)v; }
+template <> __device__ __forceinline__ Bf16 from_float<Bf16>(float v) { return Bf16{__builtin_bit_cast(uint16_t, (__bf16)v)}; }
+
+// N elements at p as floats; `have` of them exist (the rest are read as zeros, not at all from memory)
+template <typename T, int N>
+__device__ __forceinline__ typename Floats<N>::type load_piece(const T* p, int have) {
+    typedef typename Floats<N>::type F;
+    if (have >= N) return __builtin_convertvector(*reinterpret_cast<const typename Piece_<T, N>::type*>(p), F);
+    F out;
+#pragma unroll
+    for (int j = 0; j < N; ++j) out[j] = j < have ? to_float(p[j]) : 0.0f;
+    return out;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_piece(T* p, typename Floats<N>::type v, int have) {
+    typedef typename Piece_<T, N>::type V;
+    if (have >= N) {
+        *reinterpret_cast<V*>(p) = __builtin_convertvector(v, V);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (j < have) p[j] = from_float<T>(v[j]);
+}
+
+// Sum over the G lanes of a group (G a power of two up to 64, groups aligned), in every lane; the order of the additions is
+// fixed.
+template <int CTRL>
+__device__ __forceinline__ float dpp_move(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+    if constexpr (G >= 2) v += dpp_move<0xB1>(v);                        // lane ^ 1
+    if constexpr (G >= 4) v += dpp_move<0x4E>(v);                        // lane ^ 2
+    if constexpr (G >= 8) v += dpp_move<0x141>(v);                       // the other four of eight lanes
+    if constexpr (G >= 16) v += dpp_move<0x140>(v);                      // the other eight of sixteen
+    if constexpr (G >= 32) v += __uint_as_float((uint32_t)__builtin_amdgcn_ds_swizzle((int)__float_as_uint(v), (16 << 10) | 0x1f));
+    if constexpr (G >= 64) v += __shfl_xor(v, 32, kWave);
+    return v;
+}
+
+// ---- checks of the C entries -----------------------------------------------------------------------------------------
+inline bool known_type(int type) { return type == PQT_F32 || type == PQT_BF16 || type == PQT_F16; }
+inline size_t type_bytes(int type) { return type == PQT_F32 ? 4 : 2; }
+// (nullptr, and pointers off their element's alignment, are refused: a kernel would read or write at half an element)
+inline bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+inline int check_device(int device, const char* who) {
+    int ndev = 0;
+    if (hipGetDeviceCount(&ndev) != hipSuccess || device < 0 || device >= ndev) {
+        (void)hipGetLastError();
+        return pqt_host::fail(PQT_EHIP, "%s: GPU %d is not available (%d visible)", who, device, ndev);
+    }
+    return PQT_OK;
+}
+
+// calls f(T{}) with the element type that `type` names
+template <typename F>
+inline void with_type(int type, F&& f) {
+    if (type == PQT_F32) f(float{});
+    else if (type == PQT_BF16) f(Bf16{});
+    else f(Half{});
+}
+
+}  // namespace pqt

@@ -1,0 +1,682 @@
+"""The query encoder's operators against their definitions in 64 bits: embedding lookup and gradient, layer norm and its gradient,
+8-bit blocks and their products.
+
+Tolerances follow from the arithmetic, u = 2^-24 the unit of fp32: a sum of c terms in any order is off by at most c u times the sum
+of their magnitudes, a product or a stored result by its type's unit.  What is exact (codes, scales, integer-valued products) is
+compared bit for bit."""
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1702_05911_amd import buildlib
+
+if not os.path.exists(buildlib.OUTPUT):
+    buildlib.build_library()
+import paper_1702_05911_amd.binding as pqt  # noqa: E402
+
+gpu = pytest.mark.gpu
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+UNIT = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}      # rounding to 24, 8 and 11 significant bits, relative, ...
+LEAST = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -25}  # ... and below the type's normal numbers
+
+
+def dev():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU: no silent fallback")
+    return torch.device("cuda", 0)
+
+
+def normal(shape, dtype, seed, pad=0, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    wide = torch.zeros(shape[0], shape[1] + pad, dtype=dtype)
+    wide[:, :shape[1]] = (torch.randn(shape, generator=g) * scale).to(dtype)
+    return wide.to(dev())[:, :shape[1]]
+
+
+def within(got, want, tol, what):
+    """|got - want| <= tol + the rounding of the stored type, element by element; want, tol: float64 on the CPU."""
+    t = got.dtype
+    got = got.double().cpu()
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    tol = tol + want.abs() * UNIT[t] * (1 + 2.0 ** -6) + LEAST[t]
+    bad = ~((got - want).abs() <= tol)
+    if bad.any():
+        i = tuple(int(v) for v in bad.nonzero()[0])
+        raise AssertionError(f"{what}: {int(bad.sum())} of {bad.numel()} values off, first at {i}: {got[i]} for {want[i]}, tolerance {tol[i]}")
+
+
+def guarded(rows, cols, dtype, pad=3):
+    """An output inside a wider buffer, and a check that nothing outside it was written."""
+    wide = torch.full((rows + 2, cols + 2 * pad), 7.0, dtype=dtype, device=dev())
+    view = wide[1:1 + rows, pad:pad + cols]
+
+    def check():
+        keep = wide.clone()
+        keep[1:1 + rows, pad:pad + cols] = 7.0
+        assert bool((keep == 7.0).all()), "written outside the output"
+    return view, check
+
+
+# ---- embedding -------------------------------------------------------------------------------------------------------
+def some_tokens(n, V, seed, ids=torch.int64, outside=True):
+    g = torch.Generator().manual_seed(seed)
+    t = torch.exp(torch.rand(n, generator=g, dtype=torch.float64) * np.log(V + 1.0)).long().clamp(1, V) - 1      # a few tokens hold much
+    if outside and n > 3:
+        t[::7] = -1
+        t[1::31] = V
+        t[2::29] = 2 ** 31 - 1
+    return t.to(ids).to(dev())
+
+
+EMBED = [  # n, V, D, table's type, output's, ids, pad
+    (1, 1, 1, "f32", "f32", 64, 0), (1, 10, 7, "bf16", "bf16", 32, 0), (7, 100, 1024, "bf16", "bf16", 64, 0), (33, 50, 1025, "bf16", "f32", 64, 3),
+    (300, 1000, 128, "f16", "f16", 32, 8), (1000, 77, 31, "f32", "bf16", 64, 1), (64, 2000, 4099, "f16", "f32", 32, 5), (5000, 3, 8, "f32", "f16", 64, 0),
+    (129, 513, 512, "bf16", "f16", 64, 0), (20011, 900, 65, "bf16", "bf16", 32, 0)]
+
+
+@gpu
+@pytest.mark.parametrize("n,V,D,kind,out,ids,pad", EMBED)
+def test_embed(n, V, D, kind, out, ids, pad):
+    table = normal((V, D), TYPES[kind], n + D, pad)
+    tok = some_tokens(n, V, n, torch.int32 if ids == 32 else torch.int64)
+    view, check = guarded(n, D, TYPES[out])
+    for scale in (1.0, 11.3137085):
+        got = pqt.pqt_embed(table, tok, scale, out=view)
+        t = tok.long().cpu()
+        keep = (t >= 0) & (t < V)
+        want = table.double().cpu()[t.clamp(0, V - 1)] * float(np.float32(scale))
+        want[~keep] = 0.0
+        within(got, want, want.abs() * U, "embed")
+        check()
+    assert torch.equal(pqt.pqt_embed(table, tok, 2.0, out_dtype=TYPES[out]), pqt.pqt_embed(table, tok, 2.0, out=view))
+
+
+@gpu
+def test_embed_special_values_and_no_tokens():
+    table = torch.tensor([[float("inf"), -0.0, float("nan"), 65504.0], [1e-40, 3.4e38, -3.4e38, 0.0]], device=dev())
+    tok = torch.tensor([1, 0, -5], device=dev())
+    got = pqt.pqt_embed(table, tok, 2.0)
+    want = torch.tensor([[2 * float(np.float32(1e-40)), float("inf"), -float("inf"), 0.0], [float("inf"), -0.0, float("nan"), 131008.0], [0.0, 0.0, 0.0, 0.0]])
+    assert torch.equal(got.cpu().nan_to_num(nan=123.0), want.nan_to_num(nan=123.0))
+    assert pqt.pqt_embed(table, tok[:0]).shape == (0, 4)
+
+
+@gpu
+def test_embed_offsets_beyond_32_bits():
+    V, D = 2_200_000, 1000                                        # 2.2e9 elements
+    table = torch.zeros((V, D), dtype=torch.bfloat16, device=dev())
+    rows = torch.tensor([0, 1, 2_147_483, 2_147_484, 2_199_999])
+    for i, r in enumerate(rows):
+        table[r] = torch.arange(D, device=dev()).to(torch.bfloat16) + i
+    got = pqt.pqt_embed(table, rows.to(dev()))
+    for i in range(len(rows)):
+        assert torch.equal(got[i], torch.arange(D, device=dev()).to(torch.bfloat16) + i)
+    del table
+
+
+GRADIENT = [  # n, V, D, gradient's type, output's, ids, pad
+    (1, 1, 1, "f32", "f32", 64, 0), (1, 200, 9, "bf16", "f32", 32, 0), (7, 5, 130, "f16", "f16", 64, 2), (333, 8192, 512, "f32", "f32", 64, 0),
+    (1000, 3, 64, "bf16", "bf16", 32, 0), (1025, 1023, 33, "f32", "f32", 64, 5), (8192, 1024, 40, "bf16", "f32", 64, 0), (8193, 70_000, 72, "f32", "bf16", 32, 0),
+    (40_000, 50, 257, "bf16", "f32", 64, 3), (150_001, 2_000_000, 12, "f16", "f32", 64, 0), (300_000, 1, 8, "bf16", "f32", 32, 0)]
+
+
+def gradient_reference(grad, tok, V, scale):
+    """(sum, sum of magnitudes, number of terms) of every token."""
+    t, g = tok.long().cpu(), grad.double().cpu()
+    keep = (t >= 0) & (t < V)
+    total = torch.zeros(V, g.shape[1], dtype=torch.float64).index_add_(0, t[keep], g[keep])
+    size = torch.zeros(V, g.shape[1], dtype=torch.float64).index_add_(0, t[keep], g[keep].abs())
+    count = torch.zeros(V, dtype=torch.float64).index_add_(0, t[keep], torch.ones(int(keep.sum()), dtype=torch.float64))
+    s = float(np.float32(scale))
+    return total * s, size * abs(s), count[:, None]
+
+
+@gpu
+@pytest.mark.parametrize("n,V,D,kind,out,ids,pad", GRADIENT)
+def test_embed_gradient(n, V, D, kind, out, ids, pad):
+    grad = normal((n, D), TYPES[kind], n + D, pad)
+    tok = some_tokens(n, V, n, torch.int32 if ids == 32 else torch.int64)
+    want, size, count = gradient_reference(grad, tok, V, 0.37)
+    view, check = guarded(V, D, TYPES[out])
+    got = pqt.pqt_embed_gradient(grad, tok, V, 0.37, out=view)
+    within(got, want, (count + 2) * U * size, "embed gradient")
+    assert bool((got[(count[:, 0] == 0).to(dev())] == 0).all())
+    check()
+    again = pqt.pqt_embed_gradient(grad, tok, V, 0.37, out_dtype=TYPES[out])
+    assert torch.equal(again, got)                                   # the same bytes
+    # accumulating: rows without a place keep their bits
+    old = normal((V, D), TYPES[out], 99)
+    held = old.clone()
+    got = pqt.pqt_embed_gradient(grad, tok, V, 0.37, out=held, accumulate=True)
+    within(got, want + old.double().cpu(), (count + 2) * U * size + U * (want.abs() + old.double().cpu().abs()), "accumulated")
+    none = (count[:, 0] == 0).to(dev())
+    assert torch.equal(got[none], old[none])
+
+
+@gpu
+@pytest.mark.parametrize("tokens", ["outside", "one", "ascending", "descending", "alternating", "last"])
+def test_embed_gradient_orders(tokens):
+    n, V, D = 20_000, 5000, 48
+    i = torch.arange(n, device=dev())
+    tok = {"outside": torch.full_like(i, -1), "one": torch.full_like(i, 17), "ascending": i // 4, "descending": (n - 1 - i) // 4,
+           "alternating": (i % 2) * (V - 1), "last": torch.full_like(i, V - 1)}[tokens]
+    grad = normal((n, D), torch.bfloat16, 4)
+    want, size, count = gradient_reference(grad, tok, V, 1.0)
+    within(pqt.pqt_embed_gradient(grad, tok, V), want, (count + 2) * U * size, tokens)
+
+
+@gpu
+def test_embed_gradient_of_nothing():
+    grad = torch.zeros((0, 16), device=dev())
+    tok = torch.zeros(0, dtype=torch.int64, device=dev())
+    out = torch.full((300, 16), 5.0, device=dev())
+    assert torch.equal(pqt.pqt_embed_gradient(grad, tok, 300, out=out, accumulate=True), torch.full_like(out, 5.0))
+    assert not bool(pqt.pqt_embed_gradient(grad, tok, 300, out=out).any())
+
+
+@gpu
+def test_embed_gradient_offsets_beyond_32_bits():
+    n, D, step = 3000, 64, 1_000_000                              # 3e9 elements from the first row to the last
+    wide = torch.empty((n, step), dtype=torch.bfloat16, device=dev())
+    grad = wide[:, 1000:1000 + D]
+    grad.copy_(normal((n, D), torch.bfloat16, 3))
+    tok = some_tokens(n, 700, 3)
+    want, size, count = gradient_reference(grad, tok, 700, 1.0)
+    within(pqt.pqt_embed_gradient(grad, tok, 700), want, (count + 2) * U * size, "far rows")
+    del wide
+
+
+@gpu
+def test_embed_gradient_by_differences():
+    """<embed(T + d E), c> - <embed(T - d E), c> = 2 d <gradient of c, E>: the lookup is linear in the table."""
+    V, D, n = 40, 24, 90
+    tok = some_tokens(n, V, 8)
+    c, E = normal((n, D), torch.float32, 1), normal((V, D), torch.float32, 2)
+    T = normal((V, D), torch.float32, 3)
+    d = 2.0 ** -3
+    up, down = (pqt.pqt_embed(T + s * d * E, tok, 3.0).double() for s in (1, -1))
+    rise = float(((up - down) * c.double()).sum()) / (2 * d)
+    grad = pqt.pqt_embed_gradient(c, tok, V, 3.0).double()
+    # every value of up, down and T +- d E is rounded once or twice: 3 u of about 3 (|T| + d |E|), n D of them against c
+    tol = 3 * U * 3.0 * float((pqt.pqt_embed(T.abs() + d * E.abs(), tok).double() * c.double().abs()).sum()) / d + (n + 2) * U * 3.0 * \
+        float((pqt.pqt_embed(E.abs(), tok).double() * c.double().abs()).sum())
+    assert abs(rise - float((grad * E.double()).sum())) <= tol
+
+
+# ---- layer norm ------------------------------------------------------------------------------------------------------
+NORM = [  # rows, D, x's type, output's, parameters', pad
+    (1, 1, "f32", "f32", "f32", 0), (3, 2, "bf16", "bf16", "bf16", 0), (5, 64, "f32", "f32", "f32", 1), (1000, 128, "f32", "bf16", "f32", 0),
+    (257, 129, "bf16", "f32", "bf16", 7), (33, 500, "f16", "f16", "f16", 4), (70, 513, "bf16", "bf16", "f32", 0), (4099, 960, "bf16", "bf16", "bf16", 64),
+    (19, 1025, "f32", "f16", "f16", 3), (9, 2048, "f16", "f32", "bf16", 0), (6, 2049, "bf16", "bf16", "bf16", 5), (12, 4096, "bf16", "bf16", "bf16", 0),
+    (5, 4097, "f32", "f32", "f32", 0), (3, 8193, "bf16", "bf16", "bf16", 1), (4, 16384, "f16", "f16", "f32", 0), (3, 16385, "bf16", "f32", "bf16", 0), (2, 32768, "f32", "f32", "f32", 8)]
+DEPTH = 40                                                        # additions that a term of a row's sum passes through, at most
+
+
+def norm_inputs(rows, D, kind, param, pad, seed=0):
+    x = normal((rows, D), TYPES[kind], seed + rows + D, pad, 1.5)
+    x += normal((1, D), TYPES[kind], seed + 5) * 2                # columns with an offset
+    w = normal((1, D), TYPES[param], seed + 6)[0].contiguous()
+    b = normal((1, D), TYPES[param], seed + 7)[0].contiguous()
+    return x, w, b
+
+
+def norm_reference(x, w, b, eps):
+    x = x.double().cpu()
+    D = x.shape[1]
+    w = torch.ones(D, dtype=torch.float64) if w is None else w.double().cpu()
+    b = torch.zeros(D, dtype=torch.float64) if b is None else b.double().cpu()
+    mean = x.mean(1, keepdim=True)
+    var = ((x - mean) ** 2).mean(1, keepdim=True)
+    rstd = 1 / torch.sqrt(var + eps)
+    h = (x - mean) * rstd
+    off = DEPTH * U * x.abs().mean(1, keepdim=True)               # of the mean
+    spread = (2 * DEPTH * U) + off ** 2 / (var + eps)             # of rstd, relative
+    tol = w.abs() * (rstd * off + spread * h.abs()) + 6 * U * ((w * h).abs() + b.abs())
+    return h * w + b, mean[:, 0], rstd[:, 0], tol, off[:, 0], (spread * rstd)[:, 0]
+
+
+@gpu
+@pytest.mark.parametrize("rows,D,kind,out,param,pad", NORM)
+def test_layer_norm(rows, D, kind, out, param, pad):
+    x, w, b = norm_inputs(rows, D, kind, param, pad)
+    for weight, bias in ((w, b), (None, None), (w, None)):
+        view, check = guarded(rows, D, TYPES[out])
+        y, mean, rstd = pqt.pqt_layer_norm(x, weight, bias, 1e-5, out=view)
+        want, wm, wr, tol, tm, tr = norm_reference(x, weight, bias, float(np.float32(1e-5)))
+        within(y, want, tol, "y")
+        within(mean, wm, tm, "mean")
+        within(rstd, wr, tr, "rstd")
+        check()
+
+
+@gpu
+def test_layer_norm_far_from_zero_and_constant_rows():
+    """A mean thousands of times the spread, and rows of one value: the squares are of distances from the mean."""
+    D = 1000
+    x = normal((4, D), torch.float32, 1) + 4096.0
+    x[1] = 3.0
+    x[2] = 0.0
+    y, mean, rstd = pqt.pqt_layer_norm(x, None, None, 1e-5)
+    want, wm, wr, tol, tm, tr = norm_reference(x, None, None, float(np.float32(1e-5)))
+    within(mean, wm, tm, "mean")
+    within(y, want, tol, "y")
+    assert bool((y[1:3] == 0).all())
+
+
+@gpu
+def test_layer_norm_keeps_bad_rows_to_themselves():
+    x, w, b = norm_inputs(70, 960, "bf16", "bf16", 0)
+    good = pqt.pqt_layer_norm(x, w, b)[0].clone()
+    x[3, 17], x[40, 0], x[69, 959] = float("nan"), float("inf"), -float("inf")
+    y = pqt.pqt_layer_norm(x, w, b)[0]
+    bad = torch.zeros(70, dtype=torch.bool, device=dev())
+    bad[[3, 40, 69]] = True
+    assert bool(y[bad].isnan().all(1).all()) or bool(y[bad].isnan().any(1).all())
+    assert torch.equal(y[~bad], good[~bad])
+
+
+def norm_gradient_reference(grad, x, w, mean, rstd):
+    grad, x = grad.double().cpu(), x.double().cpu()
+    m, r = mean.double().cpu()[:, None], rstd.double().cpu()[:, None]
+    D = x.shape[1]
+    w = torch.ones(D, dtype=torch.float64) if w is None else w.double().cpu()
+    h = (x - m) * r
+    g = grad * w
+    s1, s2 = g.mean(1, keepdim=True), (g * h).mean(1, keepdim=True)
+    dx = r * (g - s1 - h * s2)
+    tol = r * (6 * U * (g.abs() + s1.abs() + (h * s2).abs()) + (DEPTH + 2) * U * g.abs().mean(1, keepdim=True) +
+               (DEPTH + 5) * U * h.abs() * (g * h).abs().mean(1, keepdim=True))
+    n = x.shape[0]
+    return dx, tol, (grad * h).sum(0), (n + 4) * U * (grad * h).abs().sum(0), grad.sum(0), (n + 1) * U * grad.abs().sum(0)
+
+
+@gpu
+@pytest.mark.parametrize("rows,D,kind,out,param,pad", NORM)
+def test_layer_norm_gradient(rows, D, kind, out, param, pad):
+    x, w, _ = norm_inputs(rows, D, kind, param, pad)
+    grad = normal((rows, D), TYPES[kind], 77, pad)
+    _, mean, rstd = pqt.pqt_layer_norm(x, w, None)
+    for weight in (w, None):
+        view, check = guarded(rows, D, TYPES[kind])
+        dx, dw, db = pqt.pqt_layer_norm_gradient(grad, x, weight, mean, rstd, out=view)
+        wx, tx, ww, tw, wb, tb = norm_gradient_reference(grad, x, weight, mean, rstd)
+        within(dx, wx, tx, "dx")
+        within(dw, ww, tw, "dweight")
+        within(db, wb, tb, "dbias")
+        check()
+        again = pqt.pqt_layer_norm_gradient(grad, x, weight, mean, rstd)
+        assert torch.equal(again[0], dx) and torch.equal(again[1], dw) and torch.equal(again[2], db)
+
+
+@gpu
+def test_layer_norm_gradient_of_no_rows():
+    x = torch.zeros((0, 40), device=dev())
+    none = torch.zeros(0, device=dev())
+    dx, dw, db = pqt.pqt_layer_norm_gradient(x, x, None, none, none)
+    assert dx.shape == (0, 40) and not bool(dw.any()) and not bool(db.any())
+    assert pqt.pqt_layer_norm(x)[0].shape == (0, 40)
+
+
+@gpu
+def test_layer_norm_gradient_by_differences():
+    """Central differences of the definition in 64 bits along random directions."""
+    rows, D = 6, 50
+    x, w, b = norm_inputs(rows, D, "f32", "f32", 0)
+    grad = normal((rows, D), torch.float32, 5)
+    _, mean, rstd = pqt.pqt_layer_norm(x, w, b)
+    dx, dw, db = (t.double().cpu() for t in pqt.pqt_layer_norm_gradient(grad, x, w, mean, rstd))
+    X, W, B, G = (t.double().cpu() for t in (x, w, b, grad))
+
+    def loss(X, W, B):
+        m = X.mean(1, keepdim=True)
+        return float((G * ((X - m) / torch.sqrt(((X - m) ** 2).mean(1, keepdim=True) + 1e-5) * W + B)).sum())
+    d = 1e-5
+    for seed in range(3):
+        g = torch.Generator().manual_seed(seed)
+        E, F, H = (torch.randn(s, generator=g, dtype=torch.float64) for s in ((rows, D), (D,), (D,)))
+        for found, rise in (((dx * E).sum(), (loss(X + d * E, W, B) - loss(X - d * E, W, B)) / (2 * d)),
+                            ((dw * F).sum(), (loss(X, W + d * F, B) - loss(X, W - d * F, B)) / (2 * d)),
+                            ((db * H).sum(), (loss(X, W, B + d * H) - loss(X, W, B - d * H)) / (2 * d))):
+            # 300 gradients of fp32 accuracy (about 50 u of up to 10 each), differences d^2 off: 1e-9 of sums of about 1e3
+            assert abs(float(found) - rise) <= 300 * 50 * U * 10 + 1e-6
+
+
+# ---- 8-bit blocks ----------------------------------------------------------------------------------------------------
+def codes_table():
+    """The value of every e4m3 code."""
+    out = []
+    for c in range(256):
+        e, m = (c >> 3) & 15, c & 7
+        v = float("nan") if (c & 127) == 127 else (m / 8 * 2.0 ** -6 if e == 0 else (1 + m / 8) * 2.0 ** (e - 7))
+        out.append(-v if c & 128 else v)
+    return np.array(out)
+
+
+def blocks_reference(x):
+    """Codes and scale bytes of float64 rows by searching the table of codes: nearest value, ties to the even code."""
+    rows, cols = x.shape
+    kb = -(-cols // 128)
+    f = np.zeros((rows, kb * 128))
+    f[:, :cols] = x
+    f = f.reshape(rows, kb, 128)
+    top = np.where(np.isfinite(f), np.abs(f), 0).max(2)
+    with np.errstate(divide="ignore"):
+        e = np.where(top > 0, np.ceil(np.log2(top / 448)), -126)
+    e = np.where(448 * 2.0 ** (e - 1) >= top, e - 1, e)
+    e = np.maximum(np.where(448 * 2.0 ** e < top, e + 1, e), -126).astype(np.int64)
+    values = codes_table()[:127]                                  # ascending, 0 .. 448
+    v = np.abs(f) / 2.0 ** e[:, :, None].astype(np.float64)
+    finite = np.isfinite(v)
+    hi = np.clip(np.searchsorted(values, np.where(finite, v, 0)), 1, 126)
+    up, down = values[hi] - np.where(finite, v, 0), np.where(finite, v, 0) - values[hi - 1]
+    code = np.where((up < down) | ((up == down) & (hi % 2 == 0)), hi, hi - 1)
+    code = np.where(finite, code | (np.signbit(f) << 7), 127).astype(np.uint8)
+    return code.reshape(rows, -1), (e + 127).astype(np.uint8)
+
+
+def stand_for(blocks):
+    v = codes_table()[blocks.codes.view(torch.uint8).cpu().numpy()]
+    s = np.repeat(2.0 ** (blocks.scales.cpu().numpy().astype(np.float64) - 127), 128, 1)
+    return (v * s)[:, :blocks.cols]
+
+
+def check_blocks(got, x, what):
+    code, scale = blocks_reference(x)
+    assert np.array_equal(got.scales.cpu().numpy(), scale), what + ": scales"
+    mine = got.codes.view(torch.uint8).cpu().numpy()
+    assert np.array_equal(mine, code), (what, int((mine != code).sum()), np.argwhere(mine != code)[:3], mine[mine != code][:3], code[mine != code][:3])
+
+
+QUANTIZE = [(1, 1, "f32", 0), (1, 128, "bf16", 0), (3, 127, "f16", 0), (5, 129, "bf16", 3), (130, 300, "f32", 4), (128, 128, "bf16", 0), (257, 1000, "bf16", 0),
+            (129, 64, "f16", 5), (17, 2050, "f32", 1), (1000, 7, "bf16", 0)]
+
+
+@gpu
+@pytest.mark.parametrize("rows,cols,kind,pad", QUANTIZE)
+def test_block_quantize(rows, cols, kind, pad):
+    x = normal((rows, cols), TYPES[kind], rows + cols, pad)
+    x *= torch.exp(torch.linspace(-9, 3, cols, device=dev())).to(x.dtype)          # blocks of different sizes, subnormal codes
+    ref = x.double().cpu().numpy()
+    check_blocks(pqt.pqt_block_quantize(x), ref, "rows")
+    check_blocks(pqt.pqt_block_quantize(x, rows=False, columns=True), ref.T, "columns")
+    a, t = pqt.pqt_block_quantize(x, columns=True)
+    check_blocks(a, ref, "both: rows")
+    check_blocks(t, ref.T, "both: columns")
+
+
+@gpu
+def test_block_quantize_edges():
+    """Largest values at and next to 448 * 2^e, every tie between codes, signed zeros, infinities, NaN, numbers near both ends of fp32."""
+    x = torch.zeros((24, 256))
+    values = codes_table()[:127]
+    x[0, 0] = 448.0
+    x[1, 0] = float(np.nextafter(np.float32(448), np.float32(1e9)))
+    x[2, 0] = float(np.nextafter(np.float32(448), np.float32(0)))
+    x[3, 0] = 3.4028234e38
+    x[4, :2] = torch.tensor([1e-45, -1e-45])
+    x[5, :127] = torch.tensor((values[:-1] + values[1:]) / 2).float().repeat(2)[:127]           # halfway between codes ...
+    x[5, 127] = 448.0                                                                            # ... under the scale 1
+    x[6, :126] = -torch.tensor((values[:-1] + values[1:]) / 2).float()[:126]
+    x[6, 127] = -448.0
+    x[7, :127] = torch.tensor(np.nextafter(((values[:-1] + values[1:]) / 2).astype(np.float32), np.float32(1e9))).repeat(2)[:127]
+    x[7, 127] = 448.0
+    x[8, :5] = torch.tensor([float("inf"), 1.0, -2.0, -float("inf"), 0.3])
+    x[9, :4] = torch.tensor([float("nan"), 1e30, -float("nan"), 3.0])
+    x[10] = float("nan")
+    x[11] = float("inf")
+    x[12, ::2] = -0.0
+    x[13] = torch.linspace(-448, 448, 256)
+    x[14] = 2.0 ** -126
+    x[15] = 448 * 2.0 ** -126
+    x[16] = 449 * 2.0 ** -126
+    x[17, 5] = 2.0 ** 127
+    for i in range(18, 24):
+        x[i] = torch.randn(256, generator=torch.Generator().manual_seed(i)) * 10.0 ** (6 * (i - 20))
+    x = x.to(dev())
+    ref = x.double().cpu().numpy()
+    check_blocks(pqt.pqt_block_quantize(x), ref, "rows")
+    check_blocks(pqt.pqt_block_quantize(x.t().contiguous(), rows=False, columns=True), ref, "columns")
+
+
+PRODUCT = [  # m, n, k, output's type, bias, pad
+    (1, 1, 1, "f32", True, 0), (1, 128, 128, "bf16", True, 0), (1, 4096, 1000, "bf16", True, 0), (2, 37, 129, "f32", False, 3), (5, 300, 4096, "f16", True, 0),
+    (15, 17, 513, "f32", True, 1), (16, 16, 640, "bf16", False, 0), (17, 1000, 777, "f32", True, 0), (33, 65, 2000, "bf16", True, 5), (64, 64, 127, "f32", False, 0),
+    (100, 900, 1024, "f16", False, 0), (127, 129, 385, "f32", True, 0), (129, 127, 896, "bf16", True, 0), (255, 513, 300, "f32", False, 2), (512, 256, 512, "bf16", True, 0),
+    (1000, 128, 1000, "f32", True, 0), (960, 2000, 3000, "f32", False, 0), (3, 5, 20_000, "f32", True, 0), (700, 33, 9000, "bf16", False, 0), (1111, 1999, 200, "bf16", True, 1)]
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k,out,bias,pad", PRODUCT)
+def test_block_product(m, n, k, out, bias, pad):
+    x, w = normal((m, k), torch.float32, m + k), normal((n, k), torch.float32, n + k + 1, 0, 0.1)
+    x *= torch.exp(torch.linspace(-3, 3, k, device=dev()))
+    a, b = pqt.pqt_block_quantize(x), pqt.pqt_block_quantize(w)
+    v = normal((1, n), torch.float32, 5)[0].contiguous() if bias else None
+    view, check = guarded(m, n, TYPES[out], pad + 1)
+    got = pqt.pqt_block_product(a, b, bias=v, out=view)
+    A, B = stand_for(a), stand_for(b)
+    want = torch.from_numpy(A @ B.T)
+    # k additions, each taken to be off by at most 2^-23 of a partial sum, and the bias; results of 16 bits come from an instruction that
+    # cuts off what lies below 2^-13 of the largest of eight products
+    tol = torch.from_numpy(np.abs(A) @ np.abs(B).T) * (k * 2.0 ** -23 + (0.0 if out == "f32" else 8 * 2.0 ** -13))
+    if bias:
+        want = want + v.double().cpu()
+        tol = tol + U * (want.abs() + v.double().cpu().abs())
+    within(got, want, tol, "product")
+    check()
+    assert torch.equal(pqt.pqt_block_product(a, b, bias=v, out_dtype=TYPES[out]), got)
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k", [(1, 50, 700), (16, 100, 128), (40, 70, 513), (129, 257, 1000), (300, 1000, 4000), (513, 511, 3001)])
+def test_block_product_of_integers(m, n, k):
+    """Small whole numbers under scales 2^e: every sum is exact, and so is the result."""
+    g = torch.Generator().manual_seed(m)
+    x = torch.randint(-8, 9, (m, k), generator=g).float()
+    w = torch.randint(-8, 9, (n, k), generator=g).float()
+    for i in range(0, k, 128):                                    # a block's scale differs from its neighbours', both sides cancel
+        x[:, i:i + 128] *= 2.0 ** ((i // 128) % 5 - 2)
+        w[:, i:i + 128] /= 2.0 ** ((i // 128) % 5 - 2)
+    a, b = pqt.pqt_block_quantize(x.to(dev())), pqt.pqt_block_quantize(w.to(dev()))
+    assert np.array_equal(stand_for(a), x.double().numpy()) and np.array_equal(stand_for(b), w.double().numpy())
+    got = pqt.pqt_block_product(a, b, out_dtype=torch.float32)
+    assert torch.equal(got.double().cpu(), x.double() @ w.double().t())
+
+
+@gpu
+def test_block_product_keeps_bad_rows_to_themselves():
+    x, w = normal((70, 500), torch.float32, 1), normal((90, 500), torch.float32, 2)
+    good = pqt.pqt_block_product(pqt.pqt_block_quantize(x), pqt.pqt_block_quantize(w), out_dtype=torch.float32)
+    x[5, 499], w[60, 0] = float("nan"), float("inf")
+    got = pqt.pqt_block_product(pqt.pqt_block_quantize(x), pqt.pqt_block_quantize(w), out_dtype=torch.float32)
+    bad = torch.zeros((70, 90), dtype=torch.bool, device=dev())
+    bad[5] = True
+    bad[:, 60] = True
+    assert bool(got[bad].isnan().all()) and torch.equal(got[~bad], good[~bad])
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k", [(64, 100, 200), (301, 96, 1000)])
+def test_block_product_gradients(m, n, k):
+    """dx and dw of y = x w^T from blocks of the transposes, against g w and g^T x of the values that the blocks stand for, and
+    against differences: the product is linear in either side."""
+    x, w, grad = normal((m, k), torch.bfloat16, 1), normal((n, k), torch.bfloat16, 2), normal((m, n), torch.bfloat16, 3)
+    _, xt = pqt.pqt_block_quantize(x, columns=True)
+    _, wt = pqt.pqt_block_quantize(w, columns=True)
+    g, gt = pqt.pqt_block_quantize(grad, columns=True)
+    dx, dw = pqt.pqt_block_product(g, wt, out_dtype=torch.float32), pqt.pqt_block_product(gt, xt, out_dtype=torch.float32)
+    for got, a, b in ((dx, g, wt), (dw, gt, xt)):
+        A, B = stand_for(a), stand_for(b)
+        within(got, torch.from_numpy(A @ B.T), torch.from_numpy(np.abs(A) @ np.abs(B).T) * (A.shape[1] * 2.0 ** -23), "gradient")
+    # differences of <x w^T, grad> along E: 2 d <dx, E>, up to the rounding of the values to 8 bits (2^-4 of a value, each side)
+    X, W, G = (t.double().cpu() for t in (x, w, grad))
+    gen = torch.Generator().manual_seed(9)
+    for found, other, shape, along in ((dx, W, (m, k), lambda E: (E @ W.t() * G).sum()), (dw, X, (n, k), lambda E: (X @ E.t() * G).sum())):
+        E = torch.randn(shape, generator=gen, dtype=torch.float64)
+        slack = ((G.abs() @ W.abs()) if shape == (m, k) else (G.abs().t() @ X.abs())) * (2 * 2.0 ** -4 + 2.0 ** -8)
+        assert abs(float((found.double().cpu() * E).sum() - along(E))) <= float((slack * E.abs()).sum())
+        assert float(torch.nn.functional.cosine_similarity(found.double().cpu().flatten(), (G @ W if shape == (m, k) else G.t() @ X).flatten(), dim=0)) > 0.995
+
+
+@gpu
+def test_block_product_offsets_beyond_32_bits():
+    m, n, k = 70_000, 40, 32_000                                  # 2.2e9 codes
+    codes = torch.zeros((m, 32_000), dtype=torch.uint8, device=dev()).view(torch.float8_e4m3fn)
+    codes[-3:] = torch.tensor(2.0, device=dev()).to(torch.float8_e4m3fn)
+    a = pqt.Blocks(codes, torch.full((m, 250), 127, dtype=torch.uint8, device=dev()), k)
+    b = pqt.pqt_block_quantize(torch.ones((n, k), device=dev()))
+    got = pqt.pqt_block_product(a, b, out_dtype=torch.float32)
+    assert bool((got[-3:] == 64_000.0).all()) and not bool(got[:-3].any())
+    del codes, a
+
+
+# ---- streams, graphs -------------------------------------------------------------------------------------------------
+def encode(table, tok, w, b, blocks):
+    y = pqt.pqt_embed(table, tok, 4.0)
+    y, mean, rstd = pqt.pqt_layer_norm(y, w, b)
+    return pqt.pqt_block_product(pqt.pqt_block_quantize(y), blocks, out_dtype=torch.float32)
+
+
+@gpu
+def test_operators_on_another_stream():
+    table = normal((500, 256), torch.bfloat16, 1)
+    w, b = normal((1, 256), torch.bfloat16, 2)[0].contiguous(), normal((1, 256), torch.bfloat16, 3)[0].contiguous()
+    blocks = pqt.pqt_block_quantize(normal((96, 256), torch.bfloat16, 4))
+    tok = some_tokens(900, 500, 1)
+    want = encode(table, tok, w, b, blocks)
+    grad = normal((900, 256), torch.bfloat16, 6)
+    want_grad = pqt.pqt_embed_gradient(grad, tok, 500)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    late = torch.zeros_like(table)
+    with torch.cuda.stream(side):
+        busy = torch.randn(4096, 4096, device=dev())
+        for _ in range(20):
+            busy = busy @ busy * 1e-3
+        late.copy_(table)                                          # the table is there only when the stream gets to it
+    y = pqt.pqt_embed(late, tok, 4.0, stream=side)
+    y, mean, rstd = pqt.pqt_layer_norm(y, w, b, stream=side)
+    got = pqt.pqt_block_product(pqt.pqt_block_quantize(y, stream=side), blocks, out_dtype=torch.float32, stream=side)
+    got_grad = pqt.pqt_embed_gradient(grad, tok, 500, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want) and torch.equal(got_grad, want_grad)
+
+
+@gpu
+def test_operators_in_a_graph():
+    table = normal((500, 256), torch.bfloat16, 1)
+    w, b = normal((1, 256), torch.bfloat16, 2)[0].contiguous(), normal((1, 256), torch.bfloat16, 3)[0].contiguous()
+    weights = normal((96, 256), torch.bfloat16, 4)
+    tok, grad = some_tokens(20_000, 500, 1), normal((20_000, 256), torch.bfloat16, 6)
+
+    def step():
+        y = pqt.pqt_embed(table, tok, 4.0)
+        h, mean, rstd = pqt.pqt_layer_norm(y, w, b)
+        a, at = pqt.pqt_block_quantize(h, columns=True)
+        out = pqt.pqt_block_product(a, pqt.pqt_block_quantize(weights), out_dtype=torch.float32)
+        dh, dw, db = pqt.pqt_layer_norm_gradient(grad, y, w, mean, rstd)
+        return out, pqt.pqt_block_product(at, at, out_dtype=torch.float32), dh, dw, db, pqt.pqt_embed_gradient(dh, tok, 500)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in range(3):                                          # other inputs each time, eager work and synchronisations between
+        grad.copy_(normal((20_000, 256), torch.bfloat16, 100 + seed))
+        tok.copy_(some_tokens(20_000, 500, 50 + seed))
+        want = [t.clone() for t in step()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, w_ in zip(held, want):
+            assert torch.equal(got, w_)
+
+
+# ---- refusals --------------------------------------------------------------------------------------------------------
+def refused(fn, *args, code=pqt.PQT_EINVAL):
+    rc = fn(*args)
+    assert rc == code, (rc, pqt.last_error())
+    assert pqt.last_error()
+
+
+def test_refusals_of_the_library():
+    """Arguments are checked before anything touches a GPU (addresses here are never read)."""
+    lib, p, i64 = pqt._lib, 1 << 20, 1 << 40
+    ok = dict(table=p, type=0, V=10, D=8, step=8, tokens=p, size=8, n=4, scale=1.0, out=p, otype=0, ostep=8, device=0, stream=None)
+    call = lambda **kw: tuple({**ok, **kw}.values())                                                      # noqa: E731
+    for bad in (dict(type=3), dict(otype=-1), dict(V=0), dict(D=0), dict(n=-1), dict(step=7), dict(ostep=7), dict(size=2), dict(table=None), dict(tokens=None),
+                dict(out=None), dict(table=p + 2), dict(tokens=p + 4), dict(out=p + 1)):
+        refused(lib.pqt_embed, *call(**bad))
+    refused(lib.pqt_embed, *call(D=1 << 21, step=1 << 21, ostep=1 << 21), code=pqt.PQT_EUNSUPPORTED)
+    assert lib.pqt_embed(*call(n=0, table=None, out=None, tokens=None)) == pqt.PQT_OK
+
+    ok = dict(grad=p, type=1, step=8, tokens=p, size=4, n=4, V=10, D=8, scale=1.0, acc=0, out=p, otype=0, ostep=8, ws=p, wsn=i64, device=0, stream=None)
+    for bad in (dict(type=9), dict(otype=3), dict(V=0), dict(D=0), dict(n=-1), dict(step=1), dict(ostep=7), dict(size=1), dict(grad=None), dict(tokens=None),
+                dict(out=None), dict(ws=None), dict(wsn=10), dict(ws=p + 8), dict(grad=p + 1), dict(out=p + 2), dict(tokens=p + 2)):
+        refused(lib.pqt_embed_gradient, *call(**bad))
+    for bad in (dict(n=1 << 31), dict(V=1 << 30), dict(D=1 << 21, step=1 << 21, ostep=1 << 21)):
+        refused(lib.pqt_embed_gradient, *call(**bad), code=pqt.PQT_EUNSUPPORTED)
+    assert lib.pqt_embed_gradient(*call(n=0, acc=1, ws=None, wsn=0)) == pqt.PQT_OK
+
+    ok = dict(x=p, type=0, rows=4, D=8, xs=8, w=p, b=p, pt=0, eps=1e-5, y=p, ot=0, ys=8, mean=p, rstd=p, device=0, stream=None)
+    for bad in (dict(type=4), dict(pt=5), dict(ot=-2), dict(rows=-1), dict(D=0), dict(xs=7), dict(ys=7), dict(eps=-1.0), dict(eps=float("nan")), dict(x=None),
+                dict(y=None), dict(x=p + 2), dict(w=p + 1), dict(b=p + 2), dict(mean=p + 2), dict(rstd=p + 1)):
+        refused(lib.pqt_layer_norm, *call(**bad))
+    refused(lib.pqt_layer_norm, *call(D=32769, xs=40000, ys=40000), code=pqt.PQT_EUNSUPPORTED)
+    assert lib.pqt_layer_norm(*call(rows=0, x=None, y=None)) == pqt.PQT_OK
+
+    ok = dict(g=p, gs=8, x=p, xs=8, type=0, rows=4, D=8, w=p, pt=0, mean=p, rstd=p, dx=p, ds=8, dw=p, db=p, ws=p, wsn=i64, device=0, stream=None)
+    for bad in (dict(type=4), dict(pt=5), dict(rows=-1), dict(D=0), dict(gs=7), dict(xs=7), dict(ds=7), dict(g=None), dict(x=None), dict(mean=None), dict(rstd=None),
+                dict(dx=None), dict(ws=None), dict(wsn=4), dict(g=p + 1), dict(dw=p + 2), dict(ws=p + 4)):
+        refused(lib.pqt_layer_norm_gradient, *call(**bad))
+    refused(lib.pqt_layer_norm_gradient, *call(D=32769, xs=40000, gs=40000, ds=40000), code=pqt.PQT_EUNSUPPORTED)
+    assert lib.pqt_layer_norm_gradient(*call(rows=0, dw=None, db=None)) == pqt.PQT_OK
+
+    ok = dict(x=p, type=0, rows=4, cols=8, xs=8, c=p, s=p, ct=p, st=p, device=0, stream=None)
+    for bad in (dict(type=4), dict(rows=-1), dict(cols=0), dict(xs=7), dict(x=None), dict(c=None), dict(s=None), dict(ct=None), dict(st=None),
+                dict(c=None, s=None, ct=None, st=None), dict(c=p + 8), dict(ct=p + 1), dict(x=p + 2)):
+        refused(lib.pqt_block_quantize, *call(**bad))
+    refused(lib.pqt_block_quantize, *call(rows=1 << 31), code=pqt.PQT_EUNSUPPORTED)
+    assert lib.pqt_block_quantize(*call(rows=0)) == pqt.PQT_OK
+
+    ok = dict(a=p, sa=p, b=p, sb=p, m=4, n=8, k=100, bias=p, out=p, ot=0, os=8, ws=p, wsn=i64, device=0, stream=None)
+    for bad in (dict(m=-1), dict(n=-1), dict(k=0), dict(ot=3), dict(os=7), dict(a=None), dict(sa=None), dict(b=None), dict(sb=None), dict(out=None), dict(a=p + 8),
+                dict(b=p + 4), dict(bias=p + 2), dict(out=p + 1)):
+        refused(lib.pqt_block_product, *call(**bad))
+    refused(lib.pqt_block_product, *call(k=1 << 31), code=pqt.PQT_EUNSUPPORTED)
+    assert lib.pqt_block_product(*call(m=0)) == pqt.PQT_OK and lib.pqt_block_product(*call(n=0)) == pqt.PQT_OK
+    assert pqt.pqt_embed_gradient_workspace(-1, 5, 5) == 0 and pqt.pqt_layer_norm_gradient_workspace(0, 5) == 0
+    assert pqt.pqt_embed_gradient_workspace(1000, 50, 64) > 0 and pqt.pqt_block_product_workspace(-1, 2, 3) == 0
+
+
+def test_refusals_of_the_binding():
+    x = torch.zeros((4, 8))
+    for call in (lambda: pqt.pqt_embed(x, torch.zeros(3, dtype=torch.int64)), lambda: pqt.pqt_layer_norm(x), lambda: pqt.pqt_block_quantize(x),
+                 lambda: pqt.pqt_embed_gradient(x, torch.zeros(4, dtype=torch.int64), 5), lambda: pqt.pqt_layer_norm_gradient(x, x, None, x[:, 0], x[:, 0])):
+        with pytest.raises(ValueError):
+            call()                                                 # tensors of the CPU
+
+
+@gpu
+def test_refusals_of_shapes_and_types():
+    x = torch.zeros((4, 8), device=dev())
+    tok = torch.zeros(4, dtype=torch.int64, device=dev())
+    w = torch.zeros(8, device=dev())
+    blocks = pqt.pqt_block_quantize(x)
+    for call in (lambda: pqt.pqt_embed(x, tok.float()), lambda: pqt.pqt_embed(x.t(), tok), lambda: pqt.pqt_embed(x, tok, out=torch.zeros((3, 8), device=dev())),
+                 lambda: pqt.pqt_embed(x.double(), tok), lambda: pqt.pqt_embed(x, tok.cpu()), lambda: pqt.pqt_embed_gradient(x, tok[:3], 5),
+                 lambda: pqt.pqt_embed_gradient(x, tok, 5, accumulate=True), lambda: pqt.pqt_layer_norm(x, w[:7]), lambda: pqt.pqt_layer_norm(x, w, w.half()),
+                 lambda: pqt.pqt_layer_norm(x[:1].expand(4, 8)), lambda: pqt.pqt_layer_norm_gradient(x.half(), x, w, w[:4], w[:4]),
+                 lambda: pqt.pqt_layer_norm_gradient(x, x, w, w, w), lambda: pqt.pqt_block_quantize(x, rows=False),
+                 lambda: pqt.pqt_block_product(blocks, blocks._replace(cols=9)), lambda: pqt.pqt_block_product(blocks, blocks._replace(cols=129)),
+                 lambda: pqt.pqt_block_product(blocks, blocks._replace(scales=blocks.scales.int())), lambda: pqt.pqt_block_product(blocks, blocks, bias=w),
+                 lambda: pqt.pqt_block_product(blocks, blocks, out=x)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(pqt.PqtError):
+        pqt.pqt_embed_gradient(x, tok, 0)
