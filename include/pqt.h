@@ -455,7 +455,7 @@ int pqt_layer_norm_gradient(const void* grad, int64_t grad_stride, const void* x
  * a product may lose what lies below 2^-13 of the largest of eight neighbouring products (2^-10 of the sum of |A B| at
  * most; 1.4e-5 of the result's size on normal data, far below its rounding).  Values below 2^-126 may count as zero.  With x (m x k) and weights w
  * (n x k) in blocks: y = x w^T; dx = g w is the product of g's blocks with those of w's transpose; dw = g^T x that of the blocks
- * of g's transpose with those of x's.  m, n and k below 2^31, k at least 1.
+ * of g's transpose with those of x's.  m and n below 2^28, k from 1 to 2^22.
  */
 #define PQT_BLOCK 128
 int pqt_block_quantize(const void* x, int type, int64_t rows, int64_t cols, int64_t x_stride, uint8_t* codes, uint8_t* scales,

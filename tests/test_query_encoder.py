@@ -470,6 +470,31 @@ def test_block_product(m, n, k, out, bias, pad):
     assert torch.equal(pqt.pqt_block_product(a, b, bias=v, out_dtype=TYPES[out]), got)
 
 
+# Sizes that take the kernel of 256 x 256 tiles (odd numbers of blocks of k, edges inside tiles and fragments), the one of few rows and
+# many columns, and k shared out over workgroups.
+@gpu
+@pytest.mark.parametrize("m,n,k,out,bias,pad", [(4000, 3900, 1100, "bf16", True, 1), (4096, 3841, 1024, "f16", False, 0), (16_001, 1009, 1153, "bf16", True, 0),
+                                                (8191, 2000, 100, "bf16", False, 6), (3, 33_001, 300, "bf16", True, 0), (16, 40_000, 1290, "f32", True, 1),
+                                                (500, 700, 9999, "f32", True, 0), (130, 260, 20_001, "bf16", True, 3), (700, 40, 8193, "f16", False, 0)])
+def test_block_product_kernels(m, n, k, out, bias, pad):
+    test_block_product(m, n, k, out, bias, pad)
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k,out", [(4000, 3900, 1100, "bf16"), (4005, 3999, 2047, "f16"), (300, 520, 9000, "f32"), (290, 530, 9001, "bf16"), (9, 35_000, 900, "f32")])
+def test_block_product_of_integers_kernels(m, n, k, out):
+    """Sums of few small whole numbers, which 16 bits hold too: every result is exact."""
+    g = torch.Generator().manual_seed(k)
+    x, w = torch.zeros((m, k)), torch.zeros((n, k))
+    for t, rows in ((x, m), (w, n)):
+        t.scatter_(1, torch.randint(0, k, (rows, 40), generator=g), torch.randint(-3, 4, (rows, 40), generator=g).float())
+    t = 2 * torch.arange(-(-k // 128)) % 5 - 2.0                   # scales that differ from block to block, both sides cancel
+    s = torch.exp2(t).repeat_interleave(128)[:k]
+    a, b = pqt.pqt_block_quantize((x * s).to(dev())), pqt.pqt_block_quantize((w / s).to(dev()))
+    got = pqt.pqt_block_product(a, b, out_dtype=TYPES[out])
+    assert torch.equal(got.float().cpu(), x @ w.t())
+
+
 @gpu
 @pytest.mark.parametrize("m,n,k", [(1, 50, 700), (16, 100, 128), (40, 70, 513), (129, 257, 1000), (300, 1000, 4000), (513, 511, 3001)])
 def test_block_product_of_integers(m, n, k):
