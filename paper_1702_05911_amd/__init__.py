@@ -16,7 +16,10 @@ _BINDING_NAMES = ("Index", "Builder", "Blocks", "PqtError", "last_error")
 def __getattr__(name):
     if name in _BINDING_NAMES or name == "binding" or name.startswith("pqt_"):   # the C ABI's names
         mod = importlib.import_module(".binding", __name__)
-        return mod if name == "binding" else getattr(mod, name)
+        if name == "binding":
+            return mod
+        value = globals()[name] = getattr(mod, name)                            # found at once the next time
+        return value
     if name in ("builder", "buildlib"):
         return importlib.import_module("." + name, __name__)
     raise AttributeError(name)

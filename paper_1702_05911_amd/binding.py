@@ -437,7 +437,7 @@ def _vector(name, t, length, dtypes, device):
     """A contiguous vector, or None: its pointer."""
     if t is None:
         return None
-    if t.dtype not in dtypes or t.device != device or tuple(t.shape) != (length,) or not t.is_contiguous():
+    if t.dtype not in dtypes or t.device != device or t.shape != (length,) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous tensor of {length} values on {device}, of type {' or '.join(map(str, dtypes))}")
     return t.data_ptr()
 
@@ -448,22 +448,9 @@ def _same_device(device, **tensors):
             raise ValueError(f"{name} is on {t.device}, expected {device}")
 
 
-class _On:
-    """The stream of a call: what the call allocates belongs to it."""
-
-    def __init__(self, stream, device):
-        self.stream = torch.cuda.current_stream(device) if stream is None else stream
-        self.handle = self.stream.cuda_stream
-        self._given = None if stream is None else torch.cuda.stream(stream)
-
-    def __enter__(self):
-        if self._given is not None:
-            self._given.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self._given is not None:
-            self._given.__exit__(*exc)
+# The handle of the current stream of a GPU (torch.cuda.current_stream(device).cuda_stream, which makes an object first).  Every call below
+# runs on it; one that is given another stream makes that the current one, so that what it allocates belongs to it.
+_current = torch._C._cuda_getCurrentRawStream
 
 
 def _workspace(nbytes, device):
@@ -480,20 +467,25 @@ def _tokens(tokens, device):
 def pqt_embed(table, tokens, scale=1.0, out=None, out_dtype=None, stream=None):
     """pqt_embed.  table: (V, D); tokens: (n,) int32 or int64.  Returns (n, D): scale * table[tokens], rows of zeros for
     tokens outside the table."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return pqt_embed(table, tokens, scale, out, out_dtype)
     ptr, kind, step = _matrix("table", table)
     V, D = table.shape
     tok, size, n = _tokens(tokens, table.device)
-    with _On(stream, table.device) as on:
-        if out is None:
-            out = torch.empty((n, D), dtype=out_dtype or table.dtype, device=table.device)
-        _same_device(table.device, out=out)
-        optr, okind, ostep = _matrix("out", out, (n, D), out_dtype)
-        _check(_lib.pqt_embed(ptr, kind, V, D, step, tok, size, n, scale, optr, okind, ostep, table.device.index, on.handle))
+    if out is None:
+        out = torch.empty((n, D), dtype=out_dtype or table.dtype, device=table.device)
+    _same_device(table.device, out=out)
+    optr, okind, ostep = _matrix("out", out, (n, D), out_dtype)
+    _check(_lib.pqt_embed(ptr, kind, V, D, step, tok, size, n, scale, optr, okind, ostep, table.device.index, _current(table.device.index)))
     return out
 
 
 def pqt_embed_gradient(grad, tokens, V, scale=1.0, out=None, out_dtype=torch.float32, accumulate=False, stream=None):
     """pqt_embed_gradient.  grad: (n, D).  Returns (V, D): scale times the sum of every token's rows; accumulate adds it to `out`."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return pqt_embed_gradient(grad, tokens, V, scale, out, out_dtype, accumulate)
     ptr, kind, step = _matrix("grad", grad)
     n, D = grad.shape
     tok, size, nt = _tokens(tokens, grad.device)
@@ -501,56 +493,59 @@ def pqt_embed_gradient(grad, tokens, V, scale=1.0, out=None, out_dtype=torch.flo
         raise ValueError(f"{nt} tokens for {n} rows")
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
-    with _On(stream, grad.device) as on:
-        if out is None:
-            out = torch.empty((V, D), dtype=out_dtype, device=grad.device)
-        _same_device(grad.device, out=out)
-        optr, okind, ostep = _matrix("out", out, (V, D))
-        nbytes = _lib.pqt_embed_gradient_workspace(n, V, D)
-        ws = _workspace(nbytes, grad.device)
-        _check(_lib.pqt_embed_gradient(ptr, kind, step, tok, size, n, V, D, scale, 1 if accumulate else 0, optr, okind, ostep,
-                                       ws.data_ptr() if nbytes else None, nbytes, grad.device.index, on.handle))
+    if out is None:
+        out = torch.empty((V, D), dtype=out_dtype, device=grad.device)
+    _same_device(grad.device, out=out)
+    optr, okind, ostep = _matrix("out", out, (V, D))
+    nbytes = _lib.pqt_embed_gradient_workspace(n, V, D)
+    ws = _workspace(nbytes, grad.device)
+    _check(_lib.pqt_embed_gradient(ptr, kind, step, tok, size, n, V, D, scale, 1 if accumulate else 0, optr, okind, ostep,
+                                   ws.data_ptr() if nbytes else None, nbytes, grad.device.index, _current(grad.device.index)))
     return out
 
 
 def pqt_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, out_dtype=None, stream=None):
     """pqt_layer_norm.  x: (rows, D); weight, bias: (D,) of one type, or None.  Returns (y, mean, rstd)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return pqt_layer_norm(x, weight, bias, eps, out, out_dtype)
     ptr, kind, step = _matrix("x", x)
     rows, D = x.shape
     params = weight if weight is not None else bias
     ptype = _TYPES if params is None else (params.dtype,)
     w, b = _vector("weight", weight, D, ptype, x.device), _vector("bias", bias, D, ptype, x.device)
-    with _On(stream, x.device) as on:
-        if out is None:
-            out = torch.empty((rows, D), dtype=out_dtype or x.dtype, device=x.device)
-        _same_device(x.device, out=out)
-        optr, okind, ostep = _matrix("out", out, (rows, D), out_dtype)
-        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-        _check(_lib.pqt_layer_norm(ptr, kind, rows, D, step, w, b, PQT_F32 if params is None else _type_of(params), eps, optr, okind, ostep,
-                                   mean.data_ptr(), rstd.data_ptr(), x.device.index, on.handle))
+    if out is None:
+        out = torch.empty((rows, D), dtype=out_dtype or x.dtype, device=x.device)
+    _same_device(x.device, out=out)
+    optr, okind, ostep = _matrix("out", out, (rows, D), out_dtype)
+    mean, rstd = (torch.empty(rows, dtype=torch.float32, device=x.device) for _ in range(2))
+    _check(_lib.pqt_layer_norm(ptr, kind, rows, D, step, w, b, PQT_F32 if params is None else _type_of(params), eps, optr, okind, ostep,
+                               mean.data_ptr(), rstd.data_ptr(), x.device.index, _current(x.device.index)))
     return out, mean, rstd
 
 
 def pqt_layer_norm_gradient(grad, x, weight, mean, rstd, out=None, stream=None):
     """pqt_layer_norm_gradient.  grad, x: (rows, D) of one type; mean, rstd: what pqt_layer_norm returned.  Returns (dx, dweight,
     dbias), the last two float32."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return pqt_layer_norm_gradient(grad, x, weight, mean, rstd, out)
     ptr, kind, step = _matrix("x", x)
     rows, D = x.shape
     _same_device(x.device, grad=grad)
     gptr, _, gstep = _matrix("grad", grad, (rows, D), x.dtype)
     w = _vector("weight", weight, D, _TYPES, x.device)
     mptr, rptr = (_vector(name, t, rows, (torch.float32,), x.device) for name, t in (("mean", mean), ("rstd", rstd)))
-    with _On(stream, x.device) as on:
-        if out is None:
-            out = torch.empty((rows, D), dtype=x.dtype, device=x.device)
-        _same_device(x.device, out=out)
-        optr, _, ostep = _matrix("out", out, (rows, D), x.dtype)
-        dweight, dbias = torch.empty((2, D), dtype=torch.float32, device=x.device)
-        nbytes = _lib.pqt_layer_norm_gradient_workspace(rows, D)
-        ws = _workspace(nbytes, x.device)
-        _check(_lib.pqt_layer_norm_gradient(gptr, gstep, ptr, step, kind, rows, D, w, PQT_F32 if weight is None else _type_of(weight), mptr,
-                                            rptr, optr, ostep, dweight.data_ptr(), dbias.data_ptr(), ws.data_ptr() if nbytes else None,
-                                            nbytes, x.device.index, on.handle))
+    if out is None:
+        out = torch.empty((rows, D), dtype=x.dtype, device=x.device)
+    _same_device(x.device, out=out)
+    optr, _, ostep = _matrix("out", out, (rows, D), x.dtype)
+    dweight, dbias = (torch.empty(D, dtype=torch.float32, device=x.device) for _ in range(2))
+    nbytes = _lib.pqt_layer_norm_gradient_workspace(rows, D)
+    ws = _workspace(nbytes, x.device)
+    _check(_lib.pqt_layer_norm_gradient(gptr, gstep, ptr, step, kind, rows, D, w, PQT_F32 if weight is None else _type_of(weight), mptr,
+                                        rptr, optr, ostep, dweight.data_ptr(), dbias.data_ptr(), ws.data_ptr() if nbytes else None,
+                                        nbytes, x.device.index, _current(x.device.index)))
     return out, dweight, dbias
 
 
@@ -576,35 +571,39 @@ def _blocks(name, b):
 
 def pqt_block_quantize(x, rows=True, columns=False, stream=None):
     """pqt_block_quantize.  x: (r, c).  Returns the Blocks of x (rows), of its transpose (columns), or both as a pair."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return pqt_block_quantize(x, rows, columns)
     ptr, kind, step = _matrix("x", x)
     r, c = x.shape
     if not rows and not columns:
         raise ValueError("rows, columns, or both")
-    with _On(stream, x.device) as on:
-        a = _empty_blocks(r, c, x.device) if rows else None
-        t = _empty_blocks(c, r, x.device) if columns else None
-        _check(_lib.pqt_block_quantize(ptr, kind, r, c, step, a.codes.data_ptr() if rows else None, a.scales.data_ptr() if rows else None,
-                                       t.codes.data_ptr() if columns else None, t.scales.data_ptr() if columns else None, x.device.index,
-                                       on.handle))
+    a = _empty_blocks(r, c, x.device) if rows else None
+    t = _empty_blocks(c, r, x.device) if columns else None
+    _check(_lib.pqt_block_quantize(ptr, kind, r, c, step, a.codes.data_ptr() if rows else None, a.scales.data_ptr() if rows else None,
+                                   t.codes.data_ptr() if columns else None, t.scales.data_ptr() if columns else None, x.device.index,
+                                   _current(x.device.index)))
     return (a, t) if rows and columns else a if rows else t
 
 
 def pqt_block_product(a, b, bias=None, out=None, out_dtype=torch.bfloat16, stream=None):
     """pqt_block_product.  a, b: Blocks of m x k and n x k values; bias: (n,) float32 or None.  Returns (m, n): a b^T + bias."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return pqt_block_product(a, b, bias, out, out_dtype)
     m, n = _blocks("a", a), _blocks("b", b)
     device = a.codes.device
     if a.cols != b.cols:
         raise ValueError(f"a has {a.cols} columns, b {b.cols}")
     _same_device(device, b=b.codes, out=out)
     bptr = _vector("bias", bias, n, (torch.float32,), device)
-    with _On(stream, device) as on:
-        if out is None:
-            out = torch.empty((m, n), dtype=out_dtype, device=device)
-        optr, okind, ostep = _matrix("out", out, (m, n))
-        nbytes = _lib.pqt_block_product_workspace(m, n, a.cols)
-        ws = _workspace(nbytes, device)
-        _check(_lib.pqt_block_product(a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), m, n, a.cols, bptr,
-                                      optr, okind, ostep, ws.data_ptr() if nbytes else None, nbytes, device.index, on.handle))
+    if out is None:
+        out = torch.empty((m, n), dtype=out_dtype, device=device)
+    optr, okind, ostep = _matrix("out", out, (m, n))
+    nbytes = _lib.pqt_block_product_workspace(m, n, a.cols)
+    ws = _workspace(nbytes, device)
+    _check(_lib.pqt_block_product(a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), m, n, a.cols, bptr,
+                                  optr, okind, ostep, ws.data_ptr() if nbytes else None, nbytes, device.index, _current(device.index)))
     return out
 
 

@@ -32,9 +32,11 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 template <int N> struct Floats;
 template <> struct Floats<4> { typedef f32x4 type; };
 template <> struct Floats<8> { typedef f32x8 type; };
+template <typename T> struct Element { typedef T type; };
+template <> struct Element<Bf16> { typedef __bf16 type; };
 template <typename T, int N> struct Piece_;
-template <typename T> struct Piece_<T, 4> { typedef typename Vec<T>::v4 type; };
-template <typename T> struct Piece_<T, 8> { typedef typename Vec<T>::v8 type; };
+template <typename T> struct Piece_<T, 4> { typedef typename Vec<T>::v4 type; typedef typename Element<T>::type element; };
+template <typename T> struct Piece_<T, 8> { typedef typename Vec<T>::v8 type; typedef typename Element<T>::type element; };
 
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(Half v) { return (float)v; }
@@ -43,6 +45,18 @@ template <typename T> __device__ __forceinline__ T from_float(float v);         
 template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
 template <> __device__ __forceinline__ Half from_float<Half>(float v) { return (Half)v; }
 template <> __device__ __forceinline__ Bf16 from_float<Bf16>(float v) { return Bf16{__builtin_bit_cast(uint16_t, (__bf16)v)}; }
+
+// N elements at p as they are; `have` of them exist (the rest are zeros, not read from memory)
+template <typename T, int N>
+__device__ __forceinline__ typename Piece_<T, N>::type load_raw(const T* p, int have) {
+    typedef typename Piece_<T, N>::type V;
+    if (have >= N) return *reinterpret_cast<const V*>(p);
+    V out = {};
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (j < have) out[j] = __builtin_bit_cast(typename Piece_<T, N>::element, p[j]);
+    return out;
+}
 
 // N elements at p as floats; `have` of them exist (the rest are read as zeros, not at all from memory)
 template <typename T, int N>
@@ -91,11 +105,15 @@ inline size_t type_bytes(int type) { return type == PQT_F32 ? 4 : 2; }
 inline bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
 inline int check_device(int device, const char* who) {
-    int ndev = 0;
-    if (hipGetDeviceCount(&ndev) != hipSuccess || device < 0 || device >= ndev) {
-        (void)hipGetLastError();
-        return pqt_host::fail(PQT_EHIP, "%s: GPU %d is not available (%d visible)", who, device, ndev);
-    }
+    static const int ndev = [] {                               // (it does not change while a process runs)
+        int n = 0;
+        if (hipGetDeviceCount(&n) != hipSuccess) {
+            (void)hipGetLastError();
+            n = 0;
+        }
+        return n;
+    }();
+    if (device < 0 || device >= ndev) return pqt_host::fail(PQT_EHIP, "%s: GPU %d is not available (%d visible)", who, device, ndev);
     return PQT_OK;
 }
 

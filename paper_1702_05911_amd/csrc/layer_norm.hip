@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kNormE = 8;                  // values of a piece
 constexpr int64_t kMaxNormD = 32768;       // 1,024 lanes, four pieces
-constexpr int kGradThreads = 1024;
+constexpr int kGradThreads = 512;
 constexpr int64_t kGradD = 16384;          // longest row that the one-pass backward kernel takes
 constexpr unsigned kLongParts = 64;        // parts of the rows whose columns are added up one after the other beyond that
 constexpr unsigned kGradBlocks = 256;      // workgroups of the backward pass, at most: one a compute unit
@@ -96,15 +96,24 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_kernel(NormArgs 
             b[p] = param_piece(g.bias, g.param_type, c, have[p], 0.0f);
         }
     }
-    for (int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / G; r < g.rows; r += (int64_t)gridDim.x * kGroups) {
-        const TX* src = static_cast<const TX*>(g.x) + r * g.x_stride;
-        f32x8 x[NP];
-        float s = 0.0f;
+    typedef typename Piece_<TX, kNormE>::type Raw;
+    Raw next[NP];
+    auto fetch = [&](int64_t r) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            x[p] = 0.0f;
-            if (have[p]) x[p] = load_piece<TX, kNormE>(src + (p * G + l) * kNormE, have[p]);
+            next[p] = Raw{};
+            if (have[p] && r < g.rows) next[p] = load_raw<TX, kNormE>(static_cast<const TX*>(g.x) + r * g.x_stride + (p * G + l) * kNormE, have[p]);
         }
+    };
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / G;
+    fetch(r);
+    for (; r < g.rows; r += step) {
+        f32x8 x[NP];
+#pragma unroll
+        for (int p = 0; p < NP; ++p) x[p] = __builtin_convertvector(next[p], f32x8);
+        fetch(r + step);                                       // on its way while this row is worked on
+        float s = 0.0f;
 #pragma unroll
         for (int p = 0; p < NP; ++p) s += sum8(x[p]);
         const float mean = row_sum<G>(s, scratch, turn) / D;        // (a division: the mean of equal values is that value)
@@ -135,7 +144,9 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_kernel(NormArgs 
 template <typename T, int G, int NP>
 __global__ __launch_bounds__(kGradThreads) void layer_norm_gradient_kernel(NormArgs g) {
     constexpr int kGroups = kGradThreads / G;
-    extern __shared__ __align__(16) float sums[];              // D, where the workgroup has several groups
+    constexpr int kRowsOfSums = kGradThreads / (G < kWave ? kWave : G), kColumns = G * NP * kNormE;
+    typedef typename Piece_<T, kNormE>::type Raw;
+    __shared__ __align__(16) float sums[kRowsOfSums > 1 ? kRowsOfSums : 1][kRowsOfSums > 1 ? kColumns : 1];
     __shared__ float scratch[2][16];
     int turn = 0;
     const int l = threadIdx.x & (G - 1), group = threadIdx.x / G;
@@ -151,38 +162,47 @@ __global__ __launch_bounds__(kGradThreads) void layer_norm_gradient_kernel(NormA
         db[p] = 0.0f;
         if (have[p]) w[p] = param_piece(g.weight, g.param_type, c, have[p], 1.0f);
     }
-    // (every group of a workgroup makes as many rounds: there is a barrier in row_sum)
-    for (int64_t r0 = (int64_t)blockIdx.x * kGroups; r0 < g.rows; r0 += (int64_t)gridDim.x * kGroups) {
-        const int64_t r = r0 + group;
+    Raw next_x[NP], next_y[NP];
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    auto fetch = [&](int64_t r) __attribute__((always_inline)) {      // past the last row: zeros, which add nothing
         const bool mine = r < g.rows;
-        const T* xs = static_cast<const T*>(g.x) + (mine ? r : 0) * g.x_stride;
-        const T* gs = static_cast<const T*>(g.grad) + (mine ? r : 0) * g.grad_stride;
-        const float mean = mine ? g.mean[r] : 0.0f, rstd = mine ? g.rstd[r] : 0.0f;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            next_x[p] = Raw{};
+            next_y[p] = Raw{};
+            if (have[p] && mine) {
+                next_x[p] = load_raw<T, kNormE>(static_cast<const T*>(g.x) + r * g.x_stride + (p * G + l) * kNormE, have[p]);
+                next_y[p] = load_raw<T, kNormE>(static_cast<const T*>(g.grad) + r * g.grad_stride + (p * G + l) * kNormE, have[p]);
+            }
+        }
+        next_mean = mine ? g.mean[r] : 0.0f;
+        next_rstd = mine ? g.rstd[r] : 0.0f;
+    };
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    fetch((int64_t)blockIdx.x * kGroups + group);
+    // (every group of a workgroup makes as many rounds: there is a barrier in row_sum)
+    for (int64_t r0 = (int64_t)blockIdx.x * kGroups; r0 < g.rows; r0 += step) {
+        const int64_t r = r0 + group;
+        const float mean = next_mean, rstd = next_rstd;
         f32x8 h[NP], y[NP];
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            h[p] = 0.0f;
-            y[p] = 0.0f;
-            if (have[p] && mine) {
-                h[p] = load_piece<T, kNormE>(xs + (p * G + l) * kNormE, have[p]);
-                y[p] = load_piece<T, kNormE>(gs + (p * G + l) * kNormE, have[p]);
-            }
+            h[p] = (__builtin_convertvector(next_x[p], f32x8) - mean) * rstd;
+            y[p] = __builtin_convertvector(next_y[p], f32x8);
         }
+        fetch(r + step);                                       // on its way while this row is worked on
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            h[p] = (h[p] - mean) * rstd;                       // (past the row's end grad is zero, and what h is there counts for nothing)
-            if (mine) {
-                dw[p] = dw[p] + y[p] * h[p];
-                db[p] = db[p] + y[p];
-            }
+            dw[p] = dw[p] + y[p] * h[p];                       // (past the row's end grad is zero, and what h is there counts for nothing)
+            db[p] = db[p] + y[p];
             y[p] = y[p] * w[p];
             s1 += sum8(y[p]);
             s2 += sum8(y[p] * h[p]);
         }
         s1 = row_sum<G>(s1, scratch, turn) / D;
         s2 = row_sum<G>(s2, scratch, turn) / D;
-        if (mine) {
+        if (r < g.rows) {
             T* dst = static_cast<T*>(g.out) + r * g.out_stride;
 #pragma unroll
             for (int p = 0; p < NP; ++p)
@@ -190,24 +210,28 @@ __global__ __launch_bounds__(kGradThreads) void layer_norm_gradient_kernel(NormA
         }
     }
     if (!g.want_parts) return;
+    // The groups' sums, dweight's and then dbias's: over the groups of a wavefront by lanes, over its wavefronts in LDS.
     float* out = g.parts + (size_t)blockIdx.x * 2 * g.D;
-    if constexpr (kGroups > 1) {
-        for (int round = 0; round < 2; ++round) {              // dweight, then dbias
-            for (int at = 0; at < kGroups; ++at) {
-                if (group == at) {
+    if constexpr (kRowsOfSums > 1) {
+        const int row = threadIdx.x / (G < kWave ? kWave : G);
+        for (int round = 0; round < 2; ++round) {
 #pragma unroll
-                    for (int p = 0; p < NP; ++p) {
-                        const int c = (p * G + l) * kNormE;
+            for (int p = 0; p < NP; ++p) {
+                f32x8 v = round ? db[p] : dw[p];
 #pragma unroll
-                        for (int j = 0; j < kNormE; ++j) {
-                            const float v = round ? db[p][j] : dw[p][j];
-                            if (j < have[p]) sums[c + j] = at ? sums[c + j] + v : v;
-                        }
-                    }
+                for (int j = 0; j < kNormE; ++j) {
+#pragma unroll
+                    for (int off = G; off < kWave; off *= 2) v[j] += __shfl_xor(v[j], off, kWave);
                 }
-                __syncthreads();
+                if ((threadIdx.x & (kWave - 1)) < G || G >= kWave) *reinterpret_cast<f32x8*>(&sums[row][(p * G + l) * kNormE]) = v;
             }
-            for (int c = threadIdx.x; c < g.D; c += kGradThreads) out[(size_t)round * g.D + c] = sums[c];
+            __syncthreads();
+            for (int c = threadIdx.x; c < g.D; c += kGradThreads) {
+                float v = sums[0][c];
+#pragma unroll
+                for (int i = 1; i < kRowsOfSums; ++i) v += sums[i][c];
+                out[(size_t)round * g.D + c] = v;
+            }
             __syncthreads();
         }
     } else {
@@ -317,7 +341,7 @@ void with_gradient_shape(int64_t D, F&& f) {
     else if (pieces <= 256) f(Int<128>{}, Int<2>{});
     else if (pieces <= 512) f(Int<256>{}, Int<2>{});
     else if (pieces <= 1024) f(Int<512>{}, Int<2>{});
-    else f(Int<1024>{}, Int<2>{});
+    else f(Int<512>{}, Int<4>{});
 }
 
 unsigned gradient_blocks(int64_t rows, int groups) {
@@ -435,9 +459,8 @@ int pqt_layer_norm_gradient(const void* grad, int64_t grad_stride, const void* x
         HIP_TRY(hipGetLastError());
     } else if (rows) {
         with_gradient_shape(D, [&](auto G, auto NP) {
-            const size_t lds = kGradThreads > G.value && sums ? sizeof(float) * (size_t)D : 0;
             with_type(type, [&](auto t) {
-                hipLaunchKernelGGL((layer_norm_gradient_kernel<decltype(t), G.value, NP.value>), dim3(blocks), dim3(kGradThreads), lds, st, g);
+                hipLaunchKernelGGL((layer_norm_gradient_kernel<decltype(t), G.value, NP.value>), dim3(blocks), dim3(kGradThreads), 0, st, g);
             });
         });
         HIP_TRY(hipGetLastError());

@@ -24,12 +24,14 @@ int fail(int code, const char* fmt, ...);
 
 struct DeviceGuard {   // make the index's GPU current for the duration of a call
     int prev = -1;
-    bool ok = false;
+    bool ok = false, changed = false;
     explicit DeviceGuard(int dev) {
-        if (hipGetDevice(&prev) == hipSuccess && hipSetDevice(dev) == hipSuccess) ok = true;
+        if (hipGetDevice(&prev) != hipSuccess) return;
+        changed = prev != dev;
+        ok = !changed || hipSetDevice(dev) == hipSuccess;
     }
     ~DeviceGuard() {
-        if (prev >= 0) (void)hipSetDevice(prev);
+        if (changed && prev >= 0) (void)hipSetDevice(prev);
     }
 };
 
