@@ -24,7 +24,7 @@ constexpr int kEmbedThreads = 256;
 constexpr int64_t kMaxEmbedD = 1 << 20;    // (sections of a row are the grid's second dimension: 2^16 - 1 at most)
 constexpr int64_t kMaxPlaces = 0x7fffffff; // places are 32-bit numbers
 constexpr int64_t kMaxRows = 1 << 29;      // of a gradient (64 a workgroup of 256, of 2^32 threads in all)
-constexpr int kEmbedPieces = 2;            // pieces of a row a lane has
+constexpr int kEmbedBlocks = 2048;         // workgroups of a lookup: what fits the compute units, each walks the tokens
 
 struct EmbedArgs {
     const void* table;
@@ -40,28 +40,35 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, int wide, int64_
     return wide ? static_cast<const int64_t*>(tokens)[i] : (int64_t) static_cast<const int32_t*>(tokens)[i];
 }
 
-template <typename TX, typename TY>
+// NP: pieces of a row that a lane has
+template <typename TX, typename TY, int NP>
 __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs g) {
     constexpr int E = sizeof(TX) == 2 && sizeof(TY) == 2 ? 8 : 4;           // elements of a piece
     const int lanes = 1 << g.log_lanes, l = threadIdx.x & (lanes - 1);
     const int64_t per_block = kEmbedThreads >> g.log_lanes;
-    const int64_t col = ((int64_t)blockIdx.y * kEmbedPieces * lanes + l) * E;
-    for (int64_t t = (int64_t)blockIdx.x * per_block + (threadIdx.x >> g.log_lanes); t < g.n; t += (int64_t)gridDim.x * per_block) {
-        const int64_t v = token_at(g.tokens, g.wide_tokens, t);
+    const int64_t col = ((int64_t)blockIdx.y * NP * lanes + l) * E, step = (int64_t)gridDim.x * per_block;
+    int64_t t = (int64_t)blockIdx.x * per_block + (threadIdx.x >> g.log_lanes);
+    int64_t next = t < g.n ? token_at(g.tokens, g.wide_tokens, t) : 0;
+    for (; t < g.n; t += step) {
+        const int64_t v = next;
         const bool have = v >= 0 && v < g.V;
         const TX* src = static_cast<const TX*>(g.table) + (have ? v : 0) * g.table_stride;
         TY* dst = static_cast<TY*>(g.out) + t * g.out_stride;
-        typename Floats<E>::type r[kEmbedPieces];
-#pragma unroll
-        for (int p = 0; p < kEmbedPieces; ++p) {
-            const int64_t c = col + (int64_t)p * lanes * E;
-            r[p] = 0.0f;
-            if (have && c < g.D) r[p] = load_piece<TX, E>(src + c, (int)min(g.D - c, (int64_t)E)) * g.scale;
+        next = token_at(g.tokens, g.wide_tokens, min(t + step, g.n - 1));
+        if (g.D < E) {                                                         // a row of fewer values than a piece
+            for (int j = 0; j < (int)g.D; ++j)
+                if (l == 0) dst[j] = from_float<TY>(have ? to_float(src[j]) * g.scale : 0.0f);
+            continue;
         }
+        typename Piece_<TX, E>::type r[NP];
 #pragma unroll
-        for (int p = 0; p < kEmbedPieces; ++p) {
+        for (int p = 0; p < NP; ++p) r[p] = WholePiece<E>(col + (int64_t)p * lanes * E, g.D).template load<TX>(src);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
             const int64_t c = col + (int64_t)p * lanes * E;
-            if (c < g.D) store_piece<TY, E>(dst + c, r[p], (int)min(g.D - c, (int64_t)E));
+            typename Floats<E>::type f = __builtin_convertvector(r[p], typename Floats<E>::type) * g.scale;
+            if (!have) f = 0.0f;                                               // (row 0 stood in)
+            if (c < g.D) WholePiece<E>(c, g.D).template store<TY>(dst, f);
         }
     }
 }
@@ -69,7 +76,8 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs g) {
 // ---- gradient: places by token ---------------------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kSortBits = 10, kSortBins = 1 << kSortBits;
-constexpr uint32_t kSortTiles = 128;       // tiles of the sort, at most: a tile adds up the counts of all of them itself
+constexpr int64_t kSortTile = 4096;        // places of a tile of the sort, more where there would be ...
+constexpr int64_t kSortTiles = 128;        // ... more tiles than this: a tile adds up the counts of all of them itself
 constexpr uint32_t kSortAlone = 8192;      // places that one workgroup sorts in one launch
 
 struct SortArgs {
@@ -153,10 +161,15 @@ __global__ __launch_bounds__(kSortThreads) void token_places_kernel(SortArgs g, 
     __shared__ uint32_t next[kSortWaves][kSortBins];
     __shared__ uint32_t part[kSortWaves];
     uint32_t before = 0, all = 0;
-    for (uint32_t t = 0; t < gridDim.x; ++t) {
-        const uint32_t c = g.counts[(size_t)t * kSortBins + threadIdx.x];
-        before += t < blockIdx.x ? c : 0u;
-        all += c;
+    for (uint32_t t = 0; t < gridDim.x; t += 16) {            // sixteen tiles' counts on their way
+        uint32_t c[16];
+#pragma unroll
+        for (uint32_t u = 0; u < 16; ++u) c[u] = g.counts[(size_t)min(t + u, gridDim.x - 1) * kSortBins + threadIdx.x];
+#pragma unroll
+        for (uint32_t u = 0; u < 16; ++u) {
+            before += t + u < blockIdx.x ? c[u] : 0u;
+            all += t + u < gridDim.x ? c[u] : 0u;
+        }
     }
     place_digits(g, pass, blockIdx.x * g.tile, before, all, next, part);
 }
@@ -176,6 +189,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(SortArgs g) {
 
 // ---- gradient: sums ----------------------------------------------------------------------------------------------------
 constexpr int kSumThreads = 256;
+constexpr int kSumE = 4;                   // columns of a lane: sums are mostly written as floats, 16 bytes a lane then
 constexpr int kSumRows = 8;                // rows on their way at a time
 constexpr int kClearRows = 64;             // table rows a workgroup looks up and clears
 
@@ -186,7 +200,7 @@ struct SumArgs {
     void* out;
     float* parts;                          // chunks x 2 x D: of the token that began before the chunk, of the one that goes on after it
     uint32_t n, V, chunk;                  // chunk: places of a group
-    uint32_t chunk_blocks;                 // workgroups with chunks; those behind them clear rows
+    uint32_t chunk_blocks, sections;       // workgroups with chunks, for each section of columns; those behind them clear rows
     int64_t D, grad_stride, out_stride;
     float scale;
     int log_lanes, accumulate;
@@ -200,79 +214,104 @@ __device__ __forceinline__ uint32_t first_not_below(const uint32_t* key, uint32_
     return lo;
 }
 
+// the values of one lane: a piece, or of rows shorter than one the row's
+template <int E>
+struct Lane {
+    WholePiece<E> at;
+    int narrow;                            // values of such a row, else 0
+    __device__ __forceinline__ Lane(int64_t col, int64_t D) : at(D < E ? 0 : col, D < E ? E : D), narrow(D < E ? (int)D : 0) {}
+    template <typename T>
+    __device__ __forceinline__ typename Piece_<T, E>::type load(const T* row) const { return narrow ? load_raw<T, E>(row, narrow) : at.template load<T>(row); }
+    template <typename T>
+    __device__ __forceinline__ void store(T* row, typename Floats<E>::type v) const {
+        if (narrow) store_piece<T, E>(row, v, narrow);
+        else at.template store<T>(row, v);
+    }
+};
+
 template <typename TY, int E>
-__device__ __forceinline__ void finish_row(const SumArgs& g, uint32_t v, int64_t col, int have, typename Floats<E>::type sum) {
-    TY* dst = static_cast<TY*>(g.out) + (int64_t)v * g.out_stride + col;
+__device__ __forceinline__ void finish_row(const SumArgs& g, uint32_t v, const Lane<E>& lane, typename Floats<E>::type sum) {
+    TY* dst = static_cast<TY*>(g.out) + (int64_t)v * g.out_stride;
     sum = sum * g.scale;
-    if (g.accumulate) sum = sum + load_piece<TY, E>(dst, have);
-    store_piece<TY, E>(dst, sum, have);
+    if (g.accumulate) sum = sum + __builtin_convertvector(lane.template load<TY>(dst), typename Floats<E>::type);
+    lane.template store<TY>(dst, sum);
 }
 
 template <typename TX, typename TY>
 __global__ __launch_bounds__(kSumThreads) void sum_rows_kernel(SumArgs g) {
-    constexpr int E = 16 / sizeof(TX);
+    constexpr int E = kSumE;
     typedef typename Floats<E>::type F;
     const int tid = threadIdx.x;
-    if (blockIdx.x >= g.chunk_blocks) {                       // rows of tokens that have no place
+    const uint32_t chunk_work = g.chunk_blocks * g.sections;
+    if (blockIdx.x >= chunk_work) {                           // rows of tokens that have no place
         __shared__ uint32_t absent[kClearRows];
-        const uint32_t v0 = (blockIdx.x - g.chunk_blocks) * kClearRows;
+        const uint32_t v0 = (blockIdx.x - chunk_work) * kClearRows;
         if (tid < kClearRows) {
             const uint32_t v = v0 + tid;
             const uint32_t at = first_not_below(g.key, 0, g.n, v);
             absent[tid] = v < g.V && (at >= g.n || g.key[at] != v);
         }
         __syncthreads();
-        const int64_t col = ((int64_t)blockIdx.y << g.log_lanes) * E;     // the section of columns of this workgroup
-        const int64_t cols = min((int64_t)E << g.log_lanes, g.D - col);
-        const int pieces = (int)((cols + 3) / 4), total = pieces * kClearRows;
-        const float per = 1.0f / (float)pieces;
-        for (int e = tid; e < total; e += kSumThreads) {
-            const int r = (int)(((float)e + 0.5f) * per), c = (e - r * pieces) * 4;
-            if (absent[r]) store_piece<TY, 4>(static_cast<TY*>(g.out) + (int64_t)(v0 + r) * g.out_stride + col + c, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, (int)min((int64_t)4, cols - c));
+        for (int r = tid / kWave; r < kClearRows; r += kSumThreads / kWave) {
+            if (!absent[r]) continue;
+            TY* row = static_cast<TY*>(g.out) + (int64_t)(v0 + r) * g.out_stride;
+            for (int64_t c = (tid & (kWave - 1)) * E; c < g.D; c += kWave * E) store_piece<TY, E>(row + c, F{0.0f, 0.0f, 0.0f, 0.0f}, (int)min((int64_t)E, g.D - c));
         }
         return;
     }
     const int lanes = 1 << g.log_lanes, l = tid & (lanes - 1);
-    const uint32_t c = blockIdx.x * (kSumThreads >> g.log_lanes) + (tid >> g.log_lanes);
+    const uint32_t block = blockIdx.x / g.sections, section = blockIdx.x - block * g.sections;
+    const uint32_t c = block * (kSumThreads >> g.log_lanes) + (tid >> g.log_lanes);
     const uint64_t start = (uint64_t)c * g.chunk;
-    const int64_t col = (((int64_t)blockIdx.y << g.log_lanes) + l) * E;
+    const int64_t col = (((int64_t)section << g.log_lanes) + l) * E;
     if (start >= g.n || col >= g.D) return;
     const uint32_t j0 = (uint32_t)start, j1 = (uint32_t)min((uint64_t)g.n, start + g.chunk);
-    const int have = (int)min((int64_t)E, g.D - col);
-    const TX* grad = static_cast<const TX*>(g.grad) + col;
+    const Lane<E> lane(col, g.D);
+    const TX* grad = static_cast<const TX*>(g.grad);
+    float* part = g.parts + (size_t)c * 2 * g.D;
     uint32_t cur = g.key[j0];
     bool from_before = j0 > 0 && g.key[j0 - 1] == cur;
     F sum;
     sum = 0.0f;
-    for (uint32_t j = j0; j < j1; j += kSumRows) {
-        F r[kSumRows];
-        uint32_t key[kSumRows];
+    // (no load stands behind a condition: what is past the chunk's end repeats its last row, which is not added)
+    uint32_t key[kSumRows], place[kSumRows];
+    auto look = [&](uint32_t j) {
 #pragma unroll
         for (int u = 0; u < kSumRows; ++u) {
             const uint32_t at = min(j + u, j1 - 1);
             key[u] = g.key[at];
-            r[u] = 0.0f;
-            if (j + u < j1 && key[u] < g.V) r[u] = load_piece<TX, E>(grad + (int64_t)g.place[at] * g.grad_stride, have);
+            place[u] = g.place[at];
         }
+    };
+    look(j0);
+    for (uint32_t j = j0; j < j1; j += kSumRows) {
+        typename Piece_<TX, E>::type r[kSumRows];
+        uint32_t token[kSumRows];
+#pragma unroll
+        for (int u = 0; u < kSumRows; ++u) {
+            r[u] = lane.template load<TX>(grad + (int64_t)place[u] * g.grad_stride);
+            token[u] = key[u];
+        }
+        look(j + kSumRows);                                   // the next rows' places, while these rows are on their way
 #pragma unroll
         for (int u = 0; u < kSumRows; ++u) {
             if (j + u < j1) {
-                if (key[u] != cur) {
-                    if (from_before) store_piece<float, E>(g.parts + (size_t)c * 2 * g.D + col, sum, have);
-                    else finish_row<TY, E>(g, cur, col, have, sum);      // (cur < V: a larger key follows it, and V is the largest)
+                if (token[u] != cur) {
+                    if (from_before) lane.template store<float>(part, sum);
+                    else finish_row<TY, E>(g, cur, lane, sum);           // (cur < V: a larger token follows it, and V is the largest)
                     from_before = false;
-                    cur = key[u];
+                    cur = token[u];
                     sum = 0.0f;
                 }
-                sum = sum + r[u];
+                if (cur < g.V) sum = sum + __builtin_convertvector(r[u], F);
             }
         }
     }
     if (cur >= g.V) return;
     const bool goes_on = j1 < g.n && g.key[j1] == cur;
-    if (from_before) store_piece<float, E>(g.parts + (size_t)c * 2 * g.D + col, sum, have);
-    else if (goes_on) store_piece<float, E>(g.parts + ((size_t)c * 2 + 1) * g.D + col, sum, have);
-    else finish_row<TY, E>(g, cur, col, have, sum);
+    if (from_before) lane.template store<float>(part, sum);
+    else if (goes_on) lane.template store<float>(part + g.D, sum);
+    else finish_row<TY, E>(g, cur, lane, sum);
 }
 
 // The token that goes on after chunk c, if it began there: its parts, four wavefronts a quarter each.
@@ -288,23 +327,31 @@ __global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs g) {
     const uint32_t v = g.key[j1 - 1];
     if (v >= g.V || g.key[j1] != v) return;
     if (g.key[j0] == v && j0 > 0 && g.key[j0 - 1] == v) return;       // an earlier chunk's
-    const uint32_t last = (first_not_below(g.key, j1, g.n, v + 1) - 1) / g.chunk;
-    // part 0 is chunk c's own, part i the i-th chunk's after it
-    const uint32_t parts = last - c + 1, per = (parts + kWaves - 1) / kWaves;
+    // part 0 is chunk c's own, part i that of the i-th chunk after it: as many as begin with the token
+    uint32_t parts = 1;
+    while (true) {
+        const uint64_t at = ((uint64_t)c + parts + lane) * g.chunk;
+        const unsigned long long more = __ballot(at < g.n && g.key[min(at, (uint64_t)g.n - 1)] == v);
+        const uint32_t run = more == ~0ull ? kWave : (uint32_t)__ffsll((long long)~more) - 1u;
+        parts += run;
+        if (run < kWave) break;
+    }
+    const uint32_t per = (parts + kWaves - 1) / kWaves;
     const int64_t col = ((int64_t)blockIdx.y * kWave + lane) * E;
-    const int have = (int)min((int64_t)E, g.D - col);
+    const Lane<E> own(col, g.D);
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
     if (col < g.D) {
         const uint32_t hi = min(parts, (wave + 1) * per);
         for (uint32_t i = wave * per; i < hi; i += kSumRows) {
-            f32x4 r[kSumRows];
+            typename Piece_<float, E>::type r[kSumRows];
 #pragma unroll
             for (int u = 0; u < kSumRows; ++u) {
-                r[u] = 0.0f;
-                if (i + u < hi) r[u] = load_piece<float, E>(g.parts + ((size_t)(c + i + u) * 2 + (i + u == 0 ? 1 : 0)) * g.D + col, have);
+                const uint32_t at = min(i + u, hi - 1);
+                r[u] = own.template load<float>(g.parts + ((size_t)(c + at) * 2 + (at == 0 ? 1 : 0)) * g.D);
             }
 #pragma unroll
-            for (int u = 0; u < kSumRows; ++u) sum = sum + r[u];
+            for (int u = 0; u < kSumRows; ++u)
+                if (i + u < hi) sum = sum + r[u];
         }
     }
     sums[wave][lane] = sum;
@@ -312,7 +359,7 @@ __global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs g) {
     if (wave || col >= g.D) return;
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) sum = sum + sums[w][lane];
-    finish_row<TY, E>(g, v, col, have, sum);
+    finish_row<TY, E>(g, v, own, sum);
 }
 
 // Places of a chunk: about 2,048 groups' worth, at least 16 so that few tokens are in parts, at most 256
@@ -328,8 +375,8 @@ struct GradientSpace {                     // byte offsets of the workspace
 };
 GradientSpace gradient_space(int64_t n, int64_t D) {
     GradientSpace s{};
-    s.tile = (uint32_t)((n + kSortTiles - 1) / kSortTiles + kSortThreads - 1) / kSortThreads * kSortThreads;
-    if (n <= kSortAlone) s.tile = (uint32_t)(n + kSortThreads - 1) / kSortThreads * kSortThreads;
+    const int64_t least = n <= kSortAlone ? n : std::max<int64_t>(kSortTile, (n + kSortTiles - 1) / kSortTiles);
+    s.tile = (uint32_t)((least + kSortThreads - 1) / kSortThreads * kSortThreads);
     s.tiles = (uint32_t)((n + s.tile - 1) / s.tile);
     s.chunk = chunk_places(n);
     s.chunks = (uint32_t)((n + s.chunk - 1) / s.chunk);
@@ -372,12 +419,18 @@ int pqt_embed(const void* table, int type, int64_t V, int64_t D, int64_t table_s
     if (!guard.ok) return fail(PQT_EHIP, "cannot select GPU %d", device);
     const int E = type_bytes(type) == 2 && type_bytes(out_type) == 2 ? 8 : 4;
     EmbedArgs g{table, tokens, out, V, D, table_stride, n, out_stride, scale, log_lanes_for((D + E - 1) / E), token_bytes == 8};
-    const int64_t per_block = kEmbedThreads >> g.log_lanes, section = ((int64_t)kEmbedPieces << g.log_lanes) * E;
-    const dim3 grid((unsigned)std::min<int64_t>((n + per_block - 1) / per_block, 1 << 20), (unsigned)((D + section - 1) / section));
+    const int64_t pieces = (D + E - 1) / E, per_block = kEmbedThreads >> g.log_lanes;
+    const int np = pieces <= 64 ? 1 : pieces <= 128 ? 2 : 4;
+    const int64_t section = ((int64_t)np << g.log_lanes) * E;
+    const dim3 grid((unsigned)std::min<int64_t>((n + per_block - 1) / per_block, kEmbedBlocks), (unsigned)((D + section - 1) / section));
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     with_type(type, [&](auto x) {
         with_type(out_type, [&](auto y) {
-            hipLaunchKernelGGL((embed_kernel<decltype(x), decltype(y)>), grid, dim3(kEmbedThreads), 0, st, g);
+            using X = decltype(x);
+            using Y = decltype(y);
+            if (np == 1) hipLaunchKernelGGL((embed_kernel<X, Y, 1>), grid, dim3(kEmbedThreads), 0, st, g);
+            else if (np == 2) hipLaunchKernelGGL((embed_kernel<X, Y, 2>), grid, dim3(kEmbedThreads), 0, st, g);
+            else hipLaunchKernelGGL((embed_kernel<X, Y, 4>), grid, dim3(kEmbedThreads), 0, st, g);
         });
     });
     HIP_TRY(hipGetLastError());
@@ -406,6 +459,13 @@ int pqt_embed_gradient(const void* grad, int grad_type, int64_t grad_stride, con
     const GradientSpace s = n ? gradient_space(n, D) : GradientSpace{};
     if (s.total && (!workspace || workspace_bytes < s.total || !aligned_to(workspace, 16)))
         return fail(PQT_EINVAL, "pqt_embed_gradient: workspace of %zu bytes, aligned to 16, needed (%zu given)", s.total, workspace_bytes);
+    const int log_lanes = log_lanes_for((D + kSumE - 1) / kSumE);
+    const uint32_t groups = kSumThreads >> log_lanes;
+    const int64_t section = (int64_t)kSumE << log_lanes;
+    const uint32_t chunk_blocks = (s.chunks + groups - 1) / groups;
+    const uint32_t sections = (uint32_t)((D + section - 1) / section);
+    const int64_t clear = accumulate ? 0 : (V + kClearRows - 1) / kClearRows, work = (int64_t)chunk_blocks * sections + clear;
+    if (work > 0xffffff) return fail(PQT_EUNSUPPORTED, "pqt_embed_gradient: n=%lld V=%lld D=%lld together beyond the grid", (long long)n, (long long)V, (long long)D);
     if (n == 0 && accumulate) return PQT_OK;
     if (const int rc = check_device(device, "pqt_embed_gradient")) return rc;
     DeviceGuard guard(device);
@@ -454,13 +514,10 @@ int pqt_embed_gradient(const void* grad, int grad_type, int64_t grad_stride, con
     g.out_stride = out_stride;
     g.scale = scale;
     g.accumulate = accumulate != 0;
-    const int E = 16 / (int)type_bytes(grad_type);
-    g.log_lanes = log_lanes_for((D + E - 1) / E);
-    const uint32_t groups = kSumThreads >> g.log_lanes;
-    const int64_t section = (int64_t)E << g.log_lanes;
-    g.chunk_blocks = (s.chunks + groups - 1) / groups;
-    const uint32_t clear = accumulate ? 0 : (uint32_t)((V + kClearRows - 1) / kClearRows);
-    const dim3 grid(g.chunk_blocks + clear, (unsigned)((D + section - 1) / section));
+    g.log_lanes = log_lanes;
+    g.chunk_blocks = chunk_blocks;
+    g.sections = sections;
+    const dim3 grid((unsigned)work);
     with_type(grad_type, [&](auto x) {
         with_type(out_type, [&](auto y) {
             hipLaunchKernelGGL((sum_rows_kernel<decltype(x), decltype(y)>), grid, dim3(kSumThreads), 0, st, g);

@@ -81,6 +81,29 @@ __device__ __forceinline__ void store_piece(T* p, typename Floats<N>::type v, in
         if (j < have) p[j] = from_float<T>(v[j]);
 }
 
+// The piece of N values that a lane reads of a row of D >= N where its own values begin at c: the last piece begins earlier, so that it is
+// whole and no lane takes another path; values before `own` are a neighbour's too, and are not stored.
+template <int N>
+struct WholePiece {
+    int64_t c;
+    int own;
+    __device__ __forceinline__ WholePiece(int64_t from, int64_t D) : c(from < D - N ? from : D - N), own((int)min(from - c, (int64_t)N)) {}
+    template <typename T>
+    __device__ __forceinline__ typename Piece_<T, N>::type load(const T* row) const {
+        return *reinterpret_cast<const typename Piece_<T, N>::type*>(row + c);
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(T* row, typename Floats<N>::type v) const {
+        if (own == 0) {
+            *reinterpret_cast<typename Piece_<T, N>::type*>(row + c) = __builtin_convertvector(v, typename Piece_<T, N>::type);
+            return;
+        }
+#pragma unroll
+        for (int j = 1; j < N; ++j)
+            if (j >= own) row[c + j] = from_float<T>(v[j]);
+    }
+};
+
 // Sum over the G lanes of a group (G a power of two up to 64, groups aligned), in every lane; the order of the additions is
 // fixed.
 template <int CTRL>
