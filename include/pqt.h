@@ -407,7 +407,7 @@ int pqt_measure_peaks(int device, double* hbm_read_gb_per_s, double* mfma_f32_tf
  * of fixed size, for all v in 0 .. V-1 (zeros where v has no place); tokens outside 0 .. V-1 add to nothing.
  * With accumulate != 0 that is added to what out holds, and rows without a place are not touched.  grad is n x D of
  * `grad_type`, out V x D of `out_type`.
- * D up to 2^20; for the gradient n below 2^31, V up to 2^29 and n * D up to about 2^41 (beyond: PQT_EUNSUPPORTED).
+ * D up to 2^20; for the gradient n below 2^31, V up to 2^28 and n * D up to about 2^41 (beyond: PQT_EUNSUPPORTED).
  */
 int pqt_embed(const void* table, int type, int64_t V, int64_t D, int64_t table_stride, const void* tokens, int token_bytes,
               int64_t n, float scale, void* out, int out_type, int64_t out_stride, int device, void* hip_stream);

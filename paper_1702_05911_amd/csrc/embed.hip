@@ -23,7 +23,7 @@ namespace {
 constexpr int kEmbedThreads = 256;
 constexpr int64_t kMaxEmbedD = 1 << 20;    // (sections of a row are the grid's second dimension: 2^16 - 1 at most)
 constexpr int64_t kMaxPlaces = 0x7fffffff; // places are 32-bit numbers
-constexpr int64_t kMaxRows = 1 << 29;      // of a gradient (64 a workgroup of 256, of 2^32 threads in all)
+constexpr int64_t kMaxRows = 1 << 28;      // of a gradient (32 a workgroup of 256, of 2^32 threads in all)
 constexpr int kEmbedBlocks = 2048;         // workgroups of a lookup: what fits the compute units, each walks the tokens
 
 struct EmbedArgs {
@@ -34,6 +34,7 @@ struct EmbedArgs {
     float scale;
     int log_lanes;                         // lanes of a row's section, log2
     int wide_tokens;
+    int stream;                            // store past the caches
 };
 
 __device__ __forceinline__ int64_t token_at(const void* tokens, int wide, int64_t i) {
@@ -68,7 +69,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs g) {
             const int64_t c = col + (int64_t)p * lanes * E;
             typename Floats<E>::type f = __builtin_convertvector(r[p], typename Floats<E>::type) * g.scale;
             if (!have) f = 0.0f;                                               // (row 0 stood in)
-            if (c < g.D) WholePiece<E>(c, g.D).template store<TY>(dst, f);
+            if (c < g.D) WholePiece<E>(c, g.D).template store<TY>(dst, f, g.stream);
         }
     }
 }
@@ -90,11 +91,39 @@ struct SortArgs {
     int passes, bits;                      // bits of a digit
 };
 
+// Zeros for the whole gradient, written beside the sort, whose workgroups leave most of the compute units idle; what has a sum is
+// written again later.  In units of a row, or where rows follow each other of kClearUnit bytes.
+constexpr int64_t kClearUnit = 4096;
+constexpr int64_t kClearBlocks = 448;      // two workgroups on most compute units
+struct ClearArgs {
+    unsigned char* out;
+    int64_t unit, step, total;             // bytes of a unit, from unit to unit, of all units (the last may be shorter)
+    int64_t first, last;                   // units of this launch
+    int stream;
+};
+
+// by workgroup `block` of `blocks`, a unit a wavefront
+__device__ __forceinline__ void clear_units(const ClearArgs& c, uint32_t block, uint32_t blocks) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+    const int lane = threadIdx.x & (kWave - 1), waves = blockDim.x / kWave;
+    for (int64_t u = c.first + (int64_t)block * waves + threadIdx.x / kWave; u < c.last; u += (int64_t)blocks * waves) {
+        unsigned char* p = c.out + u * c.step;
+        const int64_t len = min(c.unit, c.total - u * c.unit);
+        for (int64_t at = lane * 16; at < len; at += kWave * 16) {
+            if (at + 16 <= len) store_vector(reinterpret_cast<u32x4*>(p + at), u32x4{0u, 0u, 0u, 0u}, c.stream);
+            else
+                for (int64_t b = at; b < len; b += 2) *reinterpret_cast<uint16_t*>(p + b) = 0;
+        }
+    }
+}
+
 __device__ __forceinline__ uint32_t key_of(const SortArgs& g, int pass, uint32_t i) {
     if (pass) return g.key[(pass - 1) & 1][i];
     const int64_t v = token_at(g.tokens, g.wide_tokens, i);
     return v >= 0 && v < (int64_t)g.V ? (uint32_t)v : g.V;
 }
+
+constexpr int kSortE = 4;                  // keys of a thread on their way at a time
 
 // how often every digit occurs in the tile
 __device__ void count_digits(const SortArgs& g, int pass, uint32_t first, uint32_t* hist) {
@@ -102,8 +131,14 @@ __device__ void count_digits(const SortArgs& g, int pass, uint32_t first, uint32
     const uint32_t mask = (1u << g.bits) - 1u;
     for (uint32_t b = threadIdx.x; b < kSortBins; b += kSortThreads) hist[b] = 0u;
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < g.tile; i += kSortThreads)
-        if (first + i < g.n) atomicAdd(&hist[(key_of(g, pass, first + i) >> shift) & mask], 1u);
+    for (uint32_t i = first + threadIdx.x; i < first + g.tile; i += kSortThreads * kSortE) {
+        uint32_t key[kSortE];
+#pragma unroll
+        for (uint32_t u = 0; u < kSortE; ++u) key[u] = key_of(g, pass, min(i + u * kSortThreads, g.n - 1));
+#pragma unroll
+        for (uint32_t u = 0; u < kSortE; ++u)
+            if (i + u * kSortThreads < min(g.n, first + g.tile)) atomicAdd(&hist[(key[u] >> shift) & mask], 1u);
+    }
     __syncthreads();
 }
 
@@ -117,9 +152,15 @@ __device__ void place_digits(const SortArgs& g, int pass, uint32_t first, uint32
     uint32_t* out_place = g.place[pass & 1];
     for (uint32_t b = tid; b < kSortWaves * kSortBins; b += kSortThreads) (&next[0][0])[b] = 0u;
     __syncthreads();
-    const uint32_t lo = first + wave * len;
-    for (uint32_t i = lane; i < len; i += kWave)
-        if (lo + i < g.n) atomicAdd(&next[wave][(key_of(g, pass, lo + i) >> shift) & mask], 1u);
+    const uint32_t lo = first + wave * len, end = min(g.n, lo + len);     // (lo may lie past the last place)
+    for (uint32_t i = lo + lane; i < end; i += kWave * kSortE) {
+        uint32_t key[kSortE];
+#pragma unroll
+        for (uint32_t u = 0; u < kSortE; ++u) key[u] = key_of(g, pass, min(i + u * kWave, g.n - 1));
+#pragma unroll
+        for (uint32_t u = 0; u < kSortE; ++u)
+            if (i + u * kWave < end) atomicAdd(&next[wave][(key[u] >> shift) & mask], 1u);
+    }
     uint32_t total;
     uint32_t at = block_exclusive_sum(all, part, total) + before;         // (a barrier inside)
     __syncthreads();
@@ -129,56 +170,77 @@ __device__ void place_digits(const SortArgs& g, int pass, uint32_t first, uint32
         at += c;
     }
     __syncthreads();
-    for (uint32_t i = lane; i < len; i += kWave) {
-        const bool have = lo + i < g.n;
-        const uint32_t key = have ? key_of(g, pass, lo + i) : 0u;
-        const uint32_t place = have ? (pass ? g.place[(pass - 1) & 1][lo + i] : lo + i) : 0u;
-        const uint32_t digit = (key >> shift) & mask;
-        unsigned long long same = __ballot(have);
-        for (int b = 0; b < g.bits; ++b) {
-            const unsigned long long one = __ballot((digit >> b) & 1u);
-            same &= (digit >> b) & 1u ? one : ~one;
+    for (uint32_t i = lo + lane; i - lane < end; i += kWave * kSortE) {
+        uint32_t key[kSortE], place[kSortE];
+#pragma unroll
+        for (uint32_t u = 0; u < kSortE; ++u) {
+            const uint32_t from = min(i + u * kWave, g.n - 1);
+            key[u] = key_of(g, pass, from);
+            place[u] = pass ? g.place[(pass - 1) & 1][from] : from;
         }
-        const uint32_t rank = (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
-        const uint32_t from = have ? next[wave][digit] : 0u;
-        wave_lds_order();
-        if (have) {
-            if (rank == 0) next[wave][digit] = from + (uint32_t)__popcll(same);
-            out_key[from + rank] = key;
-            out_place[from + rank] = place;
+#pragma unroll
+        for (uint32_t u = 0; u < kSortE; ++u) {
+            const bool have = i + u * kWave < end;
+            const uint32_t digit = (key[u] >> shift) & mask;
+            unsigned long long same = __ballot(have);
+            for (int b = 0; b < g.bits; ++b) {
+                const unsigned long long one = __ballot((digit >> b) & 1u);
+                same &= (digit >> b) & 1u ? one : ~one;
+            }
+            const uint32_t rank = (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
+            const uint32_t from = have ? next[wave][digit] : 0u;
+            wave_lds_order();
+            if (have) {
+                if (rank == 0) next[wave][digit] = from + (uint32_t)__popcll(same);
+                out_key[from + rank] = key[u];
+                out_place[from + rank] = place[u];
+            }
+            wave_lds_order();
         }
-        wave_lds_order();
     }
 }
 
-__global__ __launch_bounds__(kSortThreads) void token_counts_kernel(SortArgs g, int pass) {
+__global__ __launch_bounds__(kSortThreads) void token_counts_kernel(SortArgs g, int pass, uint32_t tiles, ClearArgs clear) {
     __shared__ uint32_t hist[kSortBins];
+    if (blockIdx.x >= tiles) {
+        clear_units(clear, blockIdx.x - tiles, gridDim.x - tiles);
+        return;
+    }
     count_digits(g, pass, blockIdx.x * g.tile, hist);
     for (uint32_t b = threadIdx.x; b < kSortBins; b += kSortThreads) g.counts[(size_t)blockIdx.x * kSortBins + b] = hist[b];
 }
 
-__global__ __launch_bounds__(kSortThreads) void token_places_kernel(SortArgs g, int pass) {
+__global__ __launch_bounds__(kSortThreads) void token_places_kernel(SortArgs g, int pass, uint32_t tiles, ClearArgs clear) {
     __shared__ uint32_t next[kSortWaves][kSortBins];
     __shared__ uint32_t part[kSortWaves];
+    if (blockIdx.x >= tiles) {
+        clear_units(clear, blockIdx.x - tiles, gridDim.x - tiles);
+        return;
+    }
     uint32_t before = 0, all = 0;
-    for (uint32_t t = 0; t < gridDim.x; t += 16) {            // sixteen tiles' counts on their way
+    for (uint32_t t = 0; t < tiles; t += 16) {                // sixteen tiles' counts on their way
         uint32_t c[16];
 #pragma unroll
-        for (uint32_t u = 0; u < 16; ++u) c[u] = g.counts[(size_t)min(t + u, gridDim.x - 1) * kSortBins + threadIdx.x];
+        for (uint32_t u = 0; u < 16; ++u) c[u] = g.counts[(size_t)min(t + u, tiles - 1) * kSortBins + threadIdx.x];
 #pragma unroll
         for (uint32_t u = 0; u < 16; ++u) {
             before += t + u < blockIdx.x ? c[u] : 0u;
-            all += t + u < gridDim.x ? c[u] : 0u;
+            all += t + u < tiles ? c[u] : 0u;
         }
     }
     place_digits(g, pass, blockIdx.x * g.tile, before, all, next, part);
 }
 
-// few places: all passes by one workgroup
-__global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(SortArgs g) {
+// few places (or none: zeros only): all passes by one workgroup
+__global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(SortArgs g, ClearArgs clear) {
     __shared__ uint32_t next[kSortWaves][kSortBins];
     __shared__ uint32_t part[kSortWaves];
     __shared__ uint32_t hist[kSortBins];
+    if (blockIdx.x >= 1) {
+        clear_units(clear, blockIdx.x - 1, gridDim.x - 1);
+        return;
+    }
+    if (g.n == 0) return;
     for (int pass = 0; pass < g.passes; ++pass) {
         count_digits(g, pass, 0, hist);
         place_digits(g, pass, 0, 0, hist[threadIdx.x], next, part);
@@ -191,7 +253,6 @@ __global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(SortArgs g) {
 constexpr int kSumThreads = 256;
 constexpr int kSumE = 4;                   // columns of a lane: sums are mostly written as floats, 16 bytes a lane then
 constexpr int kSumRows = 8;                // rows on their way at a time
-constexpr int kClearRows = 64;             // table rows a workgroup looks up and clears
 
 struct SumArgs {
     const uint32_t* key;                   // n, ascending
@@ -200,19 +261,11 @@ struct SumArgs {
     void* out;
     float* parts;                          // chunks x 2 x D: of the token that began before the chunk, of the one that goes on after it
     uint32_t n, V, chunk;                  // chunk: places of a group
-    uint32_t chunk_blocks, sections;       // workgroups with chunks, for each section of columns; those behind them clear rows
+    uint32_t sections;                     // workgroups follow each other by chunk, then by section of columns
     int64_t D, grad_stride, out_stride;
     float scale;
-    int log_lanes, accumulate;
+    int log_lanes, accumulate, stream;
 };
-
-__device__ __forceinline__ uint32_t first_not_below(const uint32_t* key, uint32_t lo, uint32_t hi, uint32_t v) {
-    while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        if (key[mid] < v) lo = mid + 1; else hi = mid;
-    }
-    return lo;
-}
 
 // the values of one lane: a piece, or of rows shorter than one the row's
 template <int E>
@@ -223,9 +276,9 @@ struct Lane {
     template <typename T>
     __device__ __forceinline__ typename Piece_<T, E>::type load(const T* row) const { return narrow ? load_raw<T, E>(row, narrow) : at.template load<T>(row); }
     template <typename T>
-    __device__ __forceinline__ void store(T* row, typename Floats<E>::type v) const {
+    __device__ __forceinline__ void store(T* row, typename Floats<E>::type v, bool stream = false) const {
         if (narrow) store_piece<T, E>(row, v, narrow);
-        else at.template store<T>(row, v);
+        else at.template store<T>(row, v, stream);
     }
 };
 
@@ -234,7 +287,7 @@ __device__ __forceinline__ void finish_row(const SumArgs& g, uint32_t v, const L
     TY* dst = static_cast<TY*>(g.out) + (int64_t)v * g.out_stride;
     sum = sum * g.scale;
     if (g.accumulate) sum = sum + __builtin_convertvector(lane.template load<TY>(dst), typename Floats<E>::type);
-    lane.template store<TY>(dst, sum);
+    lane.template store<TY>(dst, sum, g.stream);
 }
 
 template <typename TX, typename TY>
@@ -242,23 +295,6 @@ __global__ __launch_bounds__(kSumThreads) void sum_rows_kernel(SumArgs g) {
     constexpr int E = kSumE;
     typedef typename Floats<E>::type F;
     const int tid = threadIdx.x;
-    const uint32_t chunk_work = g.chunk_blocks * g.sections;
-    if (blockIdx.x >= chunk_work) {                           // rows of tokens that have no place
-        __shared__ uint32_t absent[kClearRows];
-        const uint32_t v0 = (blockIdx.x - chunk_work) * kClearRows;
-        if (tid < kClearRows) {
-            const uint32_t v = v0 + tid;
-            const uint32_t at = first_not_below(g.key, 0, g.n, v);
-            absent[tid] = v < g.V && (at >= g.n || g.key[at] != v);
-        }
-        __syncthreads();
-        for (int r = tid / kWave; r < kClearRows; r += kSumThreads / kWave) {
-            if (!absent[r]) continue;
-            TY* row = static_cast<TY*>(g.out) + (int64_t)(v0 + r) * g.out_stride;
-            for (int64_t c = (tid & (kWave - 1)) * E; c < g.D; c += kWave * E) store_piece<TY, E>(row + c, F{0.0f, 0.0f, 0.0f, 0.0f}, (int)min((int64_t)E, g.D - c));
-        }
-        return;
-    }
     const int lanes = 1 << g.log_lanes, l = tid & (lanes - 1);
     const uint32_t block = blockIdx.x / g.sections, section = blockIdx.x - block * g.sections;
     const uint32_t c = block * (kSumThreads >> g.log_lanes) + (tid >> g.log_lanes);
@@ -362,6 +398,93 @@ __global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs g) {
     finish_row<TY, E>(g, v, own, sum);
 }
 
+// ---- gradient of few places --------------------------------------------------------------------------------------------
+// Up to kFewPlaces places need no sort: every workgroup looks through all the tokens by itself.  A workgroup for each place (and section of
+// columns) sums its token's rows if no earlier place has it, its wavefronts a quarter of them each; workgroups behind those clear the
+// rows that no token names.  One launch: the sorting ones take three, which wait for memory a few times each.
+constexpr uint32_t kFewPlaces = 512;
+constexpr int kFewClear = 32;              // table rows a workgroup clears
+
+struct FewArgs {
+    SumArgs sum;
+    const void* tokens;
+    int wide_tokens;
+    uint32_t sum_blocks;
+};
+
+template <typename TX, typename TY>
+__global__ __launch_bounds__(kSumThreads) void few_places_kernel(FewArgs f) {
+    constexpr int E = kSumE, kWaves = kSumThreads / kWave;
+    static_assert(kFewPlaces == 2 * kSumThreads, "two tokens a thread");
+    const SumArgs& g = f.sum;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    int64_t mine[2];                                           // the tokens of places tid and kSumThreads + tid
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t i = h * kSumThreads + tid;
+        mine[h] = token_at(f.tokens, f.wide_tokens, min(i, g.n - 1));
+        if (i >= g.n) mine[h] = -1;
+    }
+    if (blockIdx.x >= f.sum_blocks) {
+        __shared__ uint32_t named;
+        const int64_t v0 = (int64_t)(blockIdx.x - f.sum_blocks) * kFewClear;
+        if (tid == 0) named = 0u;
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (mine[h] >= v0 && mine[h] < v0 + kFewClear) atomicOr(&named, 1u << (int)(mine[h] - v0));
+        __syncthreads();
+        for (int r = wave; r < kFewClear; r += kWaves) {
+            if (((named >> r) & 1u) || v0 + r >= g.V) continue;
+            TY* row = static_cast<TY*>(g.out) + (v0 + r) * g.out_stride;
+            for (int64_t c = lane * E; c < g.D; c += kWave * E) store_piece<TY, E>(row + c, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, (int)min((int64_t)E, g.D - c));
+        }
+        return;
+    }
+    __shared__ uint32_t places[kFewPlaces];
+    __shared__ uint32_t counts[2 * kWaves];
+    __shared__ f32x4 sums[kWaves][kWave];
+    const uint32_t t = blockIdx.x / g.sections, section = blockIdx.x - t * g.sections;
+    const int64_t v = token_at(f.tokens, f.wide_tokens, t);
+    if (v < 0 || v >= g.V) return;
+    // the token's places in order
+    unsigned long long same[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        same[h] = __ballot(mine[h] == v);
+        if (lane == 0) counts[h * kWaves + wave] = (uint32_t)__popcll(same[h]);
+    }
+    __syncthreads();
+    uint32_t total = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t before = 0;
+        for (int w = 0; w < 2 * kWaves; ++w) before += w < h * kWaves + wave ? counts[w] : 0u;
+        if (mine[h] == v) places[before + (uint32_t)__popcll(same[h] & ((1ull << lane) - 1ull))] = h * kSumThreads + tid;
+    }
+    for (int w = 0; w < 2 * kWaves; ++w) total += counts[w];
+    __syncthreads();
+    if (places[0] != t) return;                                // an earlier place's workgroup has it
+    const uint32_t per = (total + kWaves - 1) / kWaves, hi = min(total, (wave + 1) * per);
+    const int64_t col = ((int64_t)section * kWave + lane) * E;
+    const Lane<E> own(col < g.D ? col : 0, g.D);
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t i = wave * per; i < hi; i += kSumRows) {
+        typename Piece_<TX, E>::type r[kSumRows];
+#pragma unroll
+        for (int u = 0; u < kSumRows; ++u) r[u] = own.template load<TX>(static_cast<const TX*>(g.grad) + (int64_t)places[min(i + u, hi - 1)] * g.grad_stride);
+#pragma unroll
+        for (int u = 0; u < kSumRows; ++u)
+            if (i + u < hi) sum = sum + __builtin_convertvector(r[u], f32x4);
+    }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave || col >= g.D) return;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) sum = sum + sums[w][lane];
+    finish_row<TY, E>(g, (uint32_t)v, own, sum);
+}
+
 // Places of a chunk: about 2,048 groups' worth, at least 16 so that few tokens are in parts, at most 256
 uint32_t chunk_places(int64_t n) {
     uint32_t c = 16;
@@ -418,7 +541,8 @@ int pqt_embed(const void* table, int type, int64_t V, int64_t D, int64_t table_s
     DeviceGuard guard(device);
     if (!guard.ok) return fail(PQT_EHIP, "cannot select GPU %d", device);
     const int E = type_bytes(type) == 2 && type_bytes(out_type) == 2 ? 8 : 4;
-    EmbedArgs g{table, tokens, out, V, D, table_stride, n, out_stride, scale, log_lanes_for((D + E - 1) / E), token_bytes == 8};
+    EmbedArgs g{table, tokens, out, V, D, table_stride, n, out_stride, scale, log_lanes_for((D + E - 1) / E), token_bytes == 8,
+                (double)n * D * type_bytes(out_type) > kStreamBytes};
     const int64_t pieces = (D + E - 1) / E, per_block = kEmbedThreads >> g.log_lanes;
     const int np = pieces <= 64 ? 1 : pieces <= 128 ? 2 : 4;
     const int64_t section = ((int64_t)np << g.log_lanes) * E;
@@ -438,7 +562,7 @@ int pqt_embed(const void* table, int type, int64_t V, int64_t D, int64_t table_s
 }
 
 size_t pqt_embed_gradient_workspace(int64_t n, int64_t V, int64_t D) {
-    if (n < 1 || V < 1 || D < 1 || n > pqt::kMaxPlaces || V > pqt::kMaxRows || D > pqt::kMaxEmbedD) return 0;
+    if (n <= pqt::kFewPlaces || V < 1 || D < 1 || n > pqt::kMaxPlaces || V > pqt::kMaxRows || D > pqt::kMaxEmbedD) return 0;
     return pqt::gradient_space(n, D).total;
 }
 
@@ -456,67 +580,96 @@ int pqt_embed_gradient(const void* grad, int grad_type, int64_t grad_stride, con
     if (!out || (n > 0 && (!grad || !tokens))) return fail(PQT_EINVAL, "pqt_embed_gradient: null pointer");
     if (!aligned_to(grad, type_bytes(grad_type)) || !aligned_to(out, type_bytes(out_type)) || !aligned_to(tokens, (size_t)token_bytes))
         return fail(PQT_EINVAL, "pqt_embed_gradient: a pointer is not aligned to its element");
-    const GradientSpace s = n ? gradient_space(n, D) : GradientSpace{};
+    const GradientSpace s = n > kFewPlaces ? gradient_space(n, D) : GradientSpace{};
     if (s.total && (!workspace || workspace_bytes < s.total || !aligned_to(workspace, 16)))
         return fail(PQT_EINVAL, "pqt_embed_gradient: workspace of %zu bytes, aligned to 16, needed (%zu given)", s.total, workspace_bytes);
     const int log_lanes = log_lanes_for((D + kSumE - 1) / kSumE);
     const uint32_t groups = kSumThreads >> log_lanes;
-    const int64_t section = (int64_t)kSumE << log_lanes;
-    const uint32_t chunk_blocks = (s.chunks + groups - 1) / groups;
-    const uint32_t sections = (uint32_t)((D + section - 1) / section);
-    const int64_t clear = accumulate ? 0 : (V + kClearRows - 1) / kClearRows, work = (int64_t)chunk_blocks * sections + clear;
-    if (work > 0xffffff) return fail(PQT_EUNSUPPORTED, "pqt_embed_gradient: n=%lld V=%lld D=%lld together beyond the grid", (long long)n, (long long)V, (long long)D);
+    const int64_t section = (int64_t)kSumE << log_lanes, sections = (D + section - 1) / section, work = (s.chunks + groups - 1) / groups * sections;
+    if (work > 0xffffff) return fail(PQT_EUNSUPPORTED, "pqt_embed_gradient: n=%lld D=%lld together beyond the grid", (long long)n, (long long)D);
     if (n == 0 && accumulate) return PQT_OK;
     if (const int rc = check_device(device, "pqt_embed_gradient")) return rc;
     DeviceGuard guard(device);
     if (!guard.ok) return fail(PQT_EHIP, "cannot select GPU %d", device);
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-    unsigned char* ws = static_cast<unsigned char*>(workspace);
     SumArgs g{};
-    if (n) {
-        SortArgs o{};
-        o.tokens = tokens;
-        o.wide_tokens = token_bytes == 8;
-        o.n = (uint32_t)n;
-        o.V = (uint32_t)V;
-        o.tile = s.tile;
-        for (int i = 0; i < 2; ++i) {
-            o.key[i] = reinterpret_cast<uint32_t*>(ws + s.key[i]);
-            o.place[i] = reinterpret_cast<uint32_t*>(ws + s.place[i]);
-        }
-        o.counts = reinterpret_cast<uint32_t*>(ws + s.counts);
-        int bits = 1;
-        while (bits < 32 && ((uint64_t)V >> bits) != 0) ++bits;             // V itself is a key
-        o.passes = (bits + kSortBits - 1) / kSortBits;
-        o.bits = (bits + o.passes - 1) / o.passes;
-        if (s.tiles == 1) {
-            hipLaunchKernelGGL(sort_tokens_kernel, dim3(1), dim3(kSortThreads), 0, st, o);
-            HIP_TRY(hipGetLastError());
-        } else {
-            for (int pass = 0; pass < o.passes; ++pass) {
-                hipLaunchKernelGGL(token_counts_kernel, dim3(s.tiles), dim3(kSortThreads), 0, st, o, pass);
-                HIP_TRY(hipGetLastError());
-                hipLaunchKernelGGL(token_places_kernel, dim3(s.tiles), dim3(kSortThreads), 0, st, o, pass);
-                HIP_TRY(hipGetLastError());
-            }
-        }
-        g.key = o.key[(o.passes - 1) & 1];
-        g.place = o.place[(o.passes - 1) & 1];
-    }
     g.grad = grad;
     g.out = out;
-    g.parts = reinterpret_cast<float*>(ws + s.parts);
     g.n = (uint32_t)n;
     g.V = (uint32_t)V;
-    g.chunk = n ? s.chunk : 1;
     g.D = D;
     g.grad_stride = grad_stride;
     g.out_stride = out_stride;
     g.scale = scale;
     g.accumulate = accumulate != 0;
+    g.stream = (double)V * D * type_bytes(out_type) > kStreamBytes;
+    if (n > 0 && n <= kFewPlaces) {
+        FewArgs f{g, tokens, token_bytes == 8, 0};
+        f.sum.sections = (uint32_t)((D + kWave * kSumE - 1) / (kWave * kSumE));
+        f.sum_blocks = (uint32_t)n * f.sum.sections;
+        const uint32_t clear = accumulate ? 0u : (uint32_t)((V + kFewClear - 1) / kFewClear);
+        with_type(grad_type, [&](auto x) {
+            with_type(out_type, [&](auto y) {
+                hipLaunchKernelGGL((few_places_kernel<decltype(x), decltype(y)>), dim3(f.sum_blocks + clear), dim3(kSumThreads), 0, st, f);
+            });
+        });
+        HIP_TRY(hipGetLastError());
+        return PQT_OK;
+    }
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    SortArgs o{};
+    o.tokens = tokens;
+    o.wide_tokens = token_bytes == 8;
+    o.n = (uint32_t)n;
+    o.V = (uint32_t)V;
+    o.tile = s.tile;
+    for (int i = 0; i < 2; ++i) {
+        o.key[i] = reinterpret_cast<uint32_t*>(ws + s.key[i]);
+        o.place[i] = reinterpret_cast<uint32_t*>(ws + s.place[i]);
+    }
+    o.counts = reinterpret_cast<uint32_t*>(ws + s.counts);
+    int bits = 1;
+    while (bits < 32 && ((uint64_t)V >> bits) != 0) ++bits;                 // V itself is a key
+    o.passes = (bits + kSortBits - 1) / kSortBits;
+    o.bits = (bits + o.passes - 1) / o.passes;
+    // the zeros, in shares as long as the launches they go with take: a pass's counting one part, its placing two
+    const int64_t row = D * (int64_t)type_bytes(out_type), step = out_stride * (int64_t)type_bytes(out_type);
+    ClearArgs clear{};
+    clear.out = static_cast<unsigned char*>(out);
+    clear.total = V * row;
+    clear.unit = row == step ? kClearUnit : row;
+    clear.step = row == step ? kClearUnit : step;
+    clear.stream = g.stream;
+    const int64_t units = accumulate ? 0 : (clear.total + clear.unit - 1) / clear.unit;
+    int part = 0;
+    const int parts = s.tiles <= 1 ? 1 : 3 * o.passes;
+    auto share = [&](int of) {                                              // the next `of` parts; returns their workgroups
+        clear.first = units / parts * part + std::min<int64_t>(part, units % parts);
+        part += of;
+        clear.last = units / parts * part + std::min<int64_t>(part, units % parts);
+        return (uint32_t)std::min<int64_t>((clear.last - clear.first + kSortWaves - 1) / kSortWaves, kClearBlocks);
+    };
+    if (s.tiles <= 1) {
+        const uint32_t more = share(1);
+        hipLaunchKernelGGL(sort_tokens_kernel, dim3(1 + more), dim3(kSortThreads), 0, st, o, clear);
+        HIP_TRY(hipGetLastError());
+    } else {
+        for (int pass = 0; pass < o.passes; ++pass) {
+            uint32_t more = share(1);
+            hipLaunchKernelGGL(token_counts_kernel, dim3(s.tiles + more), dim3(kSortThreads), 0, st, o, pass, s.tiles, clear);
+            HIP_TRY(hipGetLastError());
+            more = share(2);
+            hipLaunchKernelGGL(token_places_kernel, dim3(s.tiles + more), dim3(kSortThreads), 0, st, o, pass, s.tiles, clear);
+            HIP_TRY(hipGetLastError());
+        }
+    }
+    if (n == 0) return PQT_OK;
+    g.key = o.key[(o.passes - 1) & 1];
+    g.place = o.place[(o.passes - 1) & 1];
+    g.parts = reinterpret_cast<float*>(ws + s.parts);
+    g.chunk = s.chunk;
+    g.sections = (uint32_t)sections;
     g.log_lanes = log_lanes;
-    g.chunk_blocks = chunk_blocks;
-    g.sections = sections;
     const dim3 grid((unsigned)work);
     with_type(grad_type, [&](auto x) {
         with_type(out_type, [&](auto y) {

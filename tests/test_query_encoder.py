@@ -119,7 +119,7 @@ def test_embed_offsets_beyond_32_bits():
 
 GRADIENT = [  # n, V, D, gradient's type, output's, ids, pad
     (1, 1, 1, "f32", "f32", 64, 0), (1, 200, 9, "bf16", "f32", 32, 0), (7, 5, 130, "f16", "f16", 64, 2), (333, 8192, 512, "f32", "f32", 64, 0),
-    (1000, 3, 64, "bf16", "bf16", 32, 0), (1025, 1023, 33, "f32", "f32", 64, 5), (8192, 1024, 40, "bf16", "f32", 64, 0), (8193, 70_000, 72, "f32", "bf16", 32, 0),
+    (512, 100, 700, "bf16", "f32", 64, 0), (513, 3000, 70, "f16", "bf16", 32, 1), (500, 2, 1030, "f32", "f32", 64, 0), (1000, 3, 64, "bf16", "bf16", 32, 0), (1025, 1023, 33, "f32", "f32", 64, 5), (8192, 1024, 40, "bf16", "f32", 64, 0), (8193, 70_000, 72, "f32", "bf16", 32, 0),
     (40_000, 50, 257, "bf16", "f32", 64, 3), (150_001, 2_000_000, 12, "f16", "f32", 64, 0), (300_000, 1, 8, "bf16", "f32", 32, 0)]
 
 
@@ -640,7 +640,7 @@ def test_refusals_of_the_library():
     refused(lib.pqt_embed, *call(D=1 << 21, step=1 << 21, ostep=1 << 21), code=pqt.PQT_EUNSUPPORTED)
     assert lib.pqt_embed(*call(n=0, table=None, out=None, tokens=None)) == pqt.PQT_OK
 
-    ok = dict(grad=p, type=1, step=8, tokens=p, size=4, n=4, V=10, D=8, scale=1.0, acc=0, out=p, otype=0, ostep=8, ws=p, wsn=i64, device=0, stream=None)
+    ok = dict(grad=p, type=1, step=8, tokens=p, size=4, n=1000, V=10, D=8, scale=1.0, acc=0, out=p, otype=0, ostep=8, ws=p, wsn=i64, device=0, stream=None)
     for bad in (dict(type=9), dict(otype=3), dict(V=0), dict(D=0), dict(n=-1), dict(step=1), dict(ostep=7), dict(size=1), dict(grad=None), dict(tokens=None),
                 dict(out=None), dict(ws=None), dict(wsn=10), dict(ws=p + 8), dict(grad=p + 1), dict(out=p + 2), dict(tokens=p + 2)):
         refused(lib.pqt_embed_gradient, *call(**bad))
@@ -676,7 +676,7 @@ def test_refusals_of_the_library():
     refused(lib.pqt_block_product, *call(k=1 << 31), code=pqt.PQT_EUNSUPPORTED)
     assert lib.pqt_block_product(*call(m=0)) == pqt.PQT_OK and lib.pqt_block_product(*call(n=0)) == pqt.PQT_OK
     assert pqt.pqt_embed_gradient_workspace(-1, 5, 5) == 0 and pqt.pqt_layer_norm_gradient_workspace(0, 5) == 0
-    assert pqt.pqt_embed_gradient_workspace(1000, 50, 64) > 0 and pqt.pqt_block_product_workspace(-1, 2, 3) == 0
+    assert pqt.pqt_embed_gradient_workspace(1000, 50, 64) > 0 and pqt.pqt_embed_gradient_workspace(512, 50, 64) == 0 and pqt.pqt_block_product_workspace(-1, 2, 3) == 0
 
 
 def test_refusals_of_the_binding():
