@@ -66,18 +66,31 @@ __device__ __forceinline__ uint32_t max_of_16(uint32_t v) {
     return max(v, dpp_take<0x140, 0xf>(v, v));
 }
 
-// blocks along rows
+// Eight values of a row from column c on, zeros past its end.  The load is unconditional, so that several of a thread's are on their way at once:
+// a piece that is not whole is read from an earlier column first, and again by the lanes that have one.
+template <typename T>
+__device__ __forceinline__ typename Piece_<T, 8>::type eight_of(const T* row, int64_t c, int64_t cols) {
+    return cols >= 8 ? WholePiece<8>(c, cols).template load<T>(row) : typename Piece_<T, 8>::type{};
+}
+template <typename T>
+__device__ __forceinline__ typename Piece_<T, 8>::type put_right(typename Piece_<T, 8>::type v, const T* row, int64_t c, int64_t cols) {
+    if (c + 8 > cols) v = load_raw<T, 8>(row + (c < cols ? c : 0), (int)max(cols - c, (int64_t)0));
+    return v;
+}
+
+// blocks along rows, one by sixteen lanes
+constexpr int64_t kRowsGrid = 1 << 20;
+
 template <typename T>
 __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(QuantizeArgs g, int blocks_of_row) {
     const int64_t total = g.rows * blocks_of_row;
     const int l = threadIdx.x & (kLanesOfBlock - 1);
     const int64_t step = (int64_t)gridDim.x * (kQuantThreads / kLanesOfBlock);
     for (int64_t i = (int64_t)blockIdx.x * (kQuantThreads / kLanesOfBlock) + threadIdx.x / kLanesOfBlock; i < total; i += step) {
-        const int64_t r = i / blocks_of_row;
+        const int64_t r = total <= 0xffffffff ? (int64_t)((uint32_t)i / (uint32_t)blocks_of_row) : i / blocks_of_row;
         const int64_t c = (i - r * blocks_of_row) * kBlock + l * 8;
-        f32x8 v;
-        v = 0.0f;
-        if (c < g.cols) v = load_piece<T, 8>(static_cast<const T*>(g.x) + r * g.x_stride + c, (int)min((int64_t)8, g.cols - c));
+        const T* row = static_cast<const T*>(g.x) + r * g.x_stride;
+        const f32x8 v = __builtin_convertvector(put_right(eight_of(row, c, g.cols), row, c, g.cols), f32x8);
         float e[8];
         uint32_t m = 0;
 #pragma unroll
@@ -97,44 +110,46 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(QuantizeAr
     }
 }
 
-// a tile of 128 x 128, blocks down its columns and, where codes is not null, along its rows
+// A tile of 128 x 128, blocks down its columns and, where codes is not null, along its rows.  A thread has four rows of eight columns.
+constexpr int kTileThreads = 512, kTileRows = 4;
+
 template <typename T>
-__global__ __launch_bounds__(kQuantThreads) void quantize_tile_kernel(QuantizeArgs g, int blocks_of_row, int blocks_of_col) {
-    constexpr int kPitch = kBlock + 8;                         // (a column's bytes: eight apart, eight columns fall into different banks)
+__global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantizeArgs g, int blocks_of_row, int blocks_of_col) {
+    constexpr int kPitch = kBlock + 4;                         // (of a column's bytes: eight columns apart is eight banks apart)
+    constexpr int kWaves = kTileThreads / kWave;
     __shared__ __align__(16) uint8_t turned[kBlock * kPitch];
-    __shared__ uint32_t maxima[kQuantThreads / kWave][kBlock];
+    __shared__ uint32_t maxima[kWaves][kBlock];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-    const int pc = tid & 15, pr = tid >> 4;                    // the thread's eight columns and eight rows
+    const int pc = tid & 15, pr = tid >> 4;
     const int bc = (int)(blockIdx.x % (unsigned)blocks_of_row);
     const int64_t br = blockIdx.x / (unsigned)blocks_of_row;
-    const int64_t r0 = br * kBlock + pr * 8, c0 = (int64_t)bc * kBlock + pc * 8;
-    f32x8 v[8];
+    const int64_t r0 = br * kBlock + pr * kTileRows, c0 = (int64_t)bc * kBlock + pc * 8;
+    typename Piece_<T, 8>::type raw[kTileRows];
+    const T* x = static_cast<const T*>(g.x);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        v[i] = 0.0f;
-        if (r0 + i < g.rows && c0 < g.cols)
-            v[i] = load_piece<T, 8>(static_cast<const T*>(g.x) + (r0 + i) * g.x_stride + c0, (int)min((int64_t)8, g.cols - c0));
-    }
+    for (int i = 0; i < kTileRows; ++i) raw[i] = eight_of(x + min(r0 + i, g.rows - 1) * g.x_stride, c0, g.cols);
+    float v[kTileRows][8];
     uint32_t all = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < kTileRows; ++i) {
+        raw[i] = put_right(raw[i], x + min(r0 + i, g.rows - 1) * g.x_stride, c0, g.cols);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) all = max(all, magnitude(v[i][j]));
+        for (int j = 0; j < 8; ++j) {
+            v[i][j] = r0 + i < g.rows ? (float)raw[i][j] : 0.0f;
+            all = max(all, magnitude(v[i][j]));
+        }
+    }
     const bool all_finite = __ballot(all >= kNotFinite) == 0;
     if (g.codes) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float e[8];
+        for (int i = 0; i < kTileRows; ++i) {
             uint32_t m = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                e[j] = v[i][j];
-                m = max(m, all_finite ? magnitude(e[j]) : finite_magnitude(e[j]));
-            }
+            for (int j = 0; j < 8; ++j) m = max(m, all_finite ? magnitude(v[i][j]) : finite_magnitude(v[i][j]));
             const uint32_t byte = scale_byte(max_of_16(m));
             if (r0 + i < g.rows) {
                 const int64_t at = (r0 + i) * blocks_of_row + bc;
-                *reinterpret_cast<uint2*>(g.codes + at * kBlock + pc * 8) = eight_codes(e, inverse_scale(byte), all_finite);
+                *reinterpret_cast<uint2*>(g.codes + at * kBlock + pc * 8) = eight_codes(v[i], inverse_scale(byte), all_finite);
                 if (pc == 0) g.scales[at] = (uint8_t)byte;
             }
         }
@@ -144,7 +159,7 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_tile_kernel(QuantizeAr
     for (int j = 0; j < 8; ++j) {
         uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, all_finite ? magnitude(v[i][j]) : finite_magnitude(v[i][j]));
+        for (int i = 0; i < kTileRows; ++i) m = max(m, all_finite ? magnitude(v[i][j]) : finite_magnitude(v[i][j]));
         m = max(m, (uint32_t)__builtin_amdgcn_ds_swizzle((int)m, (16 << 10) | 0x1f));
         top[j] = max(m, (uint32_t)__shfl_xor((int)m, 32, kWave));
     }
@@ -153,25 +168,35 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_tile_kernel(QuantizeAr
         for (int j = 0; j < 8; ++j) maxima[wave][pc * 8 + j] = top[j];
     }
     __syncthreads();
+    if (tid < kBlock) {                                        // the columns' scales, in the first wavefront's row
+        uint32_t m = maxima[0][tid];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        uint32_t m = maxima[0][pc * 8 + j];
-#pragma unroll
-        for (int w = 1; w < kQuantThreads / kWave; ++w) m = max(m, maxima[w][pc * 8 + j]);
+        for (int w = 1; w < kWaves; ++w) m = max(m, maxima[w][tid]);
         const uint32_t byte = scale_byte(m);
-        float e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = v[i][j];
-        *reinterpret_cast<uint2*>(turned + (pc * 8 + j) * kPitch + pr * 8) = eight_codes(e, inverse_scale(byte), all_finite);
-        if (pr == 0 && c0 + j < g.cols) g.scales_t[(c0 + j) * blocks_of_col + br] = (uint8_t)byte;
+        maxima[0][tid] = byte;
+        const int64_t c = (int64_t)bc * kBlock + tid;
+        if (c < g.cols) g.scales_t[c * blocks_of_col + br] = (uint8_t)byte;
     }
     __syncthreads();
-    for (int e = tid; e < kBlock * (kBlock / 8); e += kQuantThreads) {          // 8 bytes of a column
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {                           // two columns' four rows
+        float e[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float inv = inverse_scale(maxima[0][pc * 8 + j + h]);
+#pragma unroll
+            for (int i = 0; i < kTileRows; ++i) e[h * kTileRows + i] = magnitude(v[i][j + h]) >= kNotFinite ? v[i][j + h] : v[i][j + h] * inv;
+        }
+        const uint2 out = eight_codes(e, 1.0f, all_finite);
+        *reinterpret_cast<uint32_t*>(turned + (pc * 8 + j) * kPitch + pr * kTileRows) = out.x;
+        *reinterpret_cast<uint32_t*>(turned + (pc * 8 + j + 1) * kPitch + pr * kTileRows) = out.y;
+    }
+    __syncthreads();
+    for (int e = tid; e < kBlock * (kBlock / 8); e += kTileThreads) {           // 8 bytes of a column
         const int col = e / (kBlock / 8), part = e & (kBlock / 8 - 1);
         const int64_t c = (int64_t)bc * kBlock + col;
-        if (c < g.cols)
-            *reinterpret_cast<uint2*>(g.codes_t + (c * blocks_of_col + br) * kBlock + part * 8) =
-                *reinterpret_cast<const uint2*>(turned + col * kPitch + part * 8);
+        const uint32_t* from = reinterpret_cast<const uint32_t*>(turned + col * kPitch + part * 8);
+        if (c < g.cols) *reinterpret_cast<uint2*>(g.codes_t + (c * blocks_of_col + br) * kBlock + part * 8) = uint2{from[0], from[1]};
     }
 }
 
@@ -190,7 +215,7 @@ extern "C" int pqt_block_quantize(const void* x, int type, int64_t rows, int64_t
     if (!aligned_to(x, type_bytes(type)) || !aligned_to(codes, 16) || !aligned_to(codes_t, 16))
         return fail(PQT_EINVAL, "pqt_block_quantize: a pointer is not aligned (x to its element, codes to 16 bytes)");
     const int64_t of_row = (cols + kBlock - 1) / kBlock, of_col = (rows + kBlock - 1) / kBlock;
-    if (codes_t && of_row * of_col > 0xffffff) return fail(PQT_EUNSUPPORTED, "pqt_block_quantize: a transpose of %lld x %lld blocks", (long long)of_col, (long long)of_row);
+    if (codes_t && of_row * of_col > 0x7fffff) return fail(PQT_EUNSUPPORTED, "pqt_block_quantize: a transpose of %lld x %lld blocks", (long long)of_col, (long long)of_row);
     if (const int rc = check_device(device, "pqt_block_quantize")) return rc;
     DeviceGuard guard(device);
     if (!guard.ok) return fail(PQT_EHIP, "cannot select GPU %d", device);
@@ -198,10 +223,10 @@ extern "C" int pqt_block_quantize(const void* x, int type, int64_t rows, int64_t
     const QuantizeArgs g{x, rows, cols, x_stride, codes, scales, codes_t, scales_t};
     with_type(type, [&](auto t) {
         if (codes_t) {
-            hipLaunchKernelGGL((quantize_tile_kernel<decltype(t)>), dim3((unsigned)(of_row * of_col)), dim3(kQuantThreads), 0, st, g, (int)of_row, (int)of_col);
+            hipLaunchKernelGGL((quantize_tile_kernel<decltype(t)>), dim3((unsigned)(of_row * of_col)), dim3(kTileThreads), 0, st, g, (int)of_row, (int)of_col);
         } else {
             const int64_t blocks = (rows * of_row + kQuantThreads / kLanesOfBlock - 1) / (kQuantThreads / kLanesOfBlock);
-            hipLaunchKernelGGL((quantize_rows_kernel<decltype(t)>), dim3((unsigned)std::min<int64_t>(blocks, 1 << 20)), dim3(kQuantThreads), 0, st, g, (int)of_row);
+            hipLaunchKernelGGL((quantize_rows_kernel<decltype(t)>), dim3((unsigned)std::min<int64_t>(blocks, kRowsGrid)), dim3(kQuantThreads), 0, st, g, (int)of_row);
         }
     });
     HIP_TRY(hipGetLastError());
