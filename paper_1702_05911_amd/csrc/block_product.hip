@@ -87,6 +87,21 @@ __device__ __forceinline__ typename Operand<EXACT>::type operand(i32x8 codes, ui
     else return codes;
 }
 
+// Fragments of A's rows with one of B's.  bf16: a sum's four multiplications wait for each other, so the others come in between.
+template <bool EXACT, int F>
+__device__ __forceinline__ void multiply_row(f32x4 (&acc)[F], const typename Operand<EXACT>::type& b, const typename Operand<EXACT>::type (&a)[F],
+                                             uint32_t sb, const uint32_t (&sa)[F]) {
+    if constexpr (EXACT) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int j = 0; j < F; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.part[p], a[j].part[p], acc[j], 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int j = 0; j < F; ++j) acc[j] = mfma_blocks(b, a[j], acc[j], sb, sa[j]);
+    }
+}
+
 // vmcnt(N) lgkmcnt(0)
 template <int N>
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x70); }
@@ -192,40 +207,59 @@ __global__ __launch_bounds__(256, B == 128 ? 2 : 4) void product_tile_kernel(Pro
     EightScales ha = scales_of(g.as, m0 + wm * of_wave + (lane & (of_wave - 1)), g.m, k0, g.kb), hb = scales_of(g.bs, n0 + wn * of_wave + (lane & (of_wave - 1)), g.n, k0, g.kb);
     uint64_t va = ha.value(), vb = hb.value();
     const int p0 = (q ^ ((fr >> 1) & 7)) * 16, p1 = ((q + 4) ^ ((fr >> 1) & 7)) * 16;
-    auto step = [&](int k, const uint8_t* cur, uint8_t* next) __attribute__((always_inline)) {
-        __builtin_amdgcn_s_waitcnt(0);                          // this block is there ...
-        __syncthreads();                                        // ... for all, and nobody reads the one before any more
-        fetch(next, k + 1);
-        uint32_t sa[F], sb[F];
+    const int row_a = wm * of_wave + fr, row_b = B + wn * of_wave + fr;
+    uint32_t sa[F], sb[F];
+    auto pass_scales = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < F; ++i) {
             sa[i] = (uint32_t)__builtin_amdgcn_ds_bpermute((i * 16 + fr) * 4, (int)va);
             sb[i] = (uint32_t)__builtin_amdgcn_ds_bpermute((i * 16 + fr) * 4, (int)vb);
         }
-        typename Operand<kExact>::type fa[F];
-#pragma unroll
-        for (int j = 0; j < F; ++j) fa[j] = operand<kExact>(fragment(cur, wm * of_wave + j * 16 + fr, p0, p1), sa[j]);
-#pragma unroll
-        for (int i = 0; i < F; ++i) {
-            const auto fb = operand<kExact>(fragment(cur, B + wn * of_wave + i * 16 + fr, p0, p1), sb[i]);
-#pragma unroll
-            for (int j = 0; j < F; ++j) acc[i][j] = mfma_blocks(fb, fa[j], acc[i][j], sb[i], sa[j]);
-        }
         va >>= 8;
         vb >>= 8;
     };
+    typename Operand<kExact>::type fa[F], fb;
+    // One block, whose fragments of A and first of B are there: while one of B is multiplied the next is read.  The last one's time
+    // goes with the next block's, so the workgroup meets before that: the next block is there, and nobody reads this one any more.
+    auto step = [&](int k, uint8_t* cur, const uint8_t* next) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i + 1 < F; ++i) {
+            const i32x8 b = fragment(cur, row_b + (i + 1) * 16, p0, p1);
+            multiply_row<kExact, F>(acc[i], fb, fa, sb[i], sa);
+            fb = operand<kExact>(b, sb[i + 1]);
+        }
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        fetch(cur, k + 2);
+        i32x8 a[F];
+#pragma unroll
+        for (int j = 0; j < F; ++j) a[j] = fragment(next, row_a + j * 16, p0, p1);
+        const i32x8 b = fragment(next, row_b, p0, p1);
+        multiply_row<kExact, F>(acc[F - 1], fb, fa, sb[F - 1], sa);
+        pass_scales();
+#pragma unroll
+        for (int j = 0; j < F; ++j) fa[j] = operand<kExact>(a[j], sa[j]);
+        fb = operand<kExact>(b, sb[0]);
+    };
     fetch(even, k0);
+    fetch(odd, k0 + 1);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    pass_scales();
+#pragma unroll
+    for (int j = 0; j < F; ++j) fa[j] = operand<kExact>(fragment(even, row_a + j * 16, p0, p1), sa[j]);
+    fb = operand<kExact>(fragment(even, row_b, p0, p1), sb[0]);
     for (int k = k0; k < k1; k += 2) {
-        if (((k - k0) & 7) == 6) {                              // two blocks before they are needed
-            ha = scales_of(g.as, m0 + wm * of_wave + (lane & (of_wave - 1)), g.m, k + 2, g.kb);
-            hb = scales_of(g.bs, n0 + wn * of_wave + (lane & (of_wave - 1)), g.n, k + 2, g.kb);
+        if (((k - k0) & 7) == 4) {                              // two blocks before they are taken
+            ha = scales_of(g.as, m0 + wm * of_wave + (lane & (of_wave - 1)), g.m, k + 4, g.kb);
+            hb = scales_of(g.bs, n0 + wn * of_wave + (lane & (of_wave - 1)), g.n, k + 4, g.kb);
         }
         step(k, even, odd);
-        step(k + 1, odd, even);
-        if (((k - k0) & 7) == 6) {
+        if (((k - k0) & 7) == 6) {                              // (the block after the next begins eight new ones)
             va = ha.value();
             vb = hb.value();
         }
+        step(k + 1, odd, even);
     }
     __builtin_amdgcn_s_waitcnt(0);                              // (what was fetched past the end)
 #pragma unroll
