@@ -413,6 +413,7 @@ def pqt_measure_peaks(device=0):
 PQT_F32, PQT_BF16, PQT_F16 = 0, 1, 2
 PQT_BLOCK = 128
 _TYPES = {torch.float32: PQT_F32, torch.bfloat16: PQT_BF16, torch.float16: PQT_F16}
+_FLOATS = (torch.float32,)
 _TOKEN_BYTES = {torch.int32: 4, torch.int64: 8}
 
 # A matrix in 8-bit blocks: codes (rows, cols rounded up to 128) float8_e4m3fn, scales (rows, blocks) uint8, cols.
@@ -518,7 +519,7 @@ def pqt_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, out_dtype=None
         out = torch.empty((rows, D), dtype=out_dtype or x.dtype, device=x.device)
     _same_device(x.device, out=out)
     optr, okind, ostep = _matrix("out", out, (rows, D), out_dtype)
-    mean, rstd = (torch.empty(rows, dtype=torch.float32, device=x.device) for _ in range(2))
+    mean, rstd = torch.empty(rows, dtype=torch.float32, device=x.device), torch.empty(rows, dtype=torch.float32, device=x.device)
     _check(_lib.pqt_layer_norm(ptr, kind, rows, D, step, w, b, PQT_F32 if params is None else _type_of(params), eps, optr, okind, ostep,
                                mean.data_ptr(), rstd.data_ptr(), x.device.index, _current(x.device.index)))
     return out, mean, rstd
@@ -535,12 +536,12 @@ def pqt_layer_norm_gradient(grad, x, weight, mean, rstd, out=None, stream=None):
     _same_device(x.device, grad=grad)
     gptr, _, gstep = _matrix("grad", grad, (rows, D), x.dtype)
     w = _vector("weight", weight, D, _TYPES, x.device)
-    mptr, rptr = (_vector(name, t, rows, (torch.float32,), x.device) for name, t in (("mean", mean), ("rstd", rstd)))
+    mptr, rptr = _vector("mean", mean, rows, _FLOATS, x.device), _vector("rstd", rstd, rows, _FLOATS, x.device)
     if out is None:
         out = torch.empty((rows, D), dtype=x.dtype, device=x.device)
     _same_device(x.device, out=out)
     optr, _, ostep = _matrix("out", out, (rows, D), x.dtype)
-    dweight, dbias = (torch.empty(D, dtype=torch.float32, device=x.device) for _ in range(2))
+    dweight, dbias = torch.empty(D, dtype=torch.float32, device=x.device), torch.empty(D, dtype=torch.float32, device=x.device)
     nbytes = _lib.pqt_layer_norm_gradient_workspace(rows, D)
     ws = _workspace(nbytes, x.device)
     _check(_lib.pqt_layer_norm_gradient(gptr, gstep, ptr, step, kind, rows, D, w, PQT_F32 if weight is None else _type_of(weight), mptr,
@@ -596,7 +597,7 @@ def pqt_block_product(a, b, bias=None, out=None, out_dtype=torch.bfloat16, strea
     if a.cols != b.cols:
         raise ValueError(f"a has {a.cols} columns, b {b.cols}")
     _same_device(device, b=b.codes, out=out)
-    bptr = _vector("bias", bias, n, (torch.float32,), device)
+    bptr = _vector("bias", bias, n, _FLOATS, device)
     if out is None:
         out = torch.empty((m, n), dtype=out_dtype, device=device)
     optr, okind, ostep = _matrix("out", out, (m, n))

@@ -622,6 +622,19 @@ def test_operators_in_a_graph():
             assert torch.equal(got, w_)
 
 
+@gpu
+def test_example_trains_and_finds():
+    """examples/query_encoder.py: the loss falls, and the index finds the topics of passages that the encoder has not seen."""
+    import importlib.util
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "query_encoder.py")
+    spec = importlib.util.spec_from_file_location("query_encoder", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    first, last, right = example.run(steps=30, topics=16, say=lambda *a: None)
+    assert last < 0.8 * first, (first, last)
+    assert right > 0.8, right                                      # one in sixteen by chance
+
+
 # ---- refusals --------------------------------------------------------------------------------------------------------
 def refused(fn, *args, code=pqt.PQT_EINVAL):
     rc = fn(*args)
