@@ -458,6 +458,20 @@ def _workspace(nbytes, device):
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
+def _result(out, shape, dtype, device, fixed=True):
+    """The matrix a call writes, the caller's or a new one: (tensor, pointer, type, elements from row to row).  fixed: the caller's has
+    to be of that dtype."""
+    if out is None:
+        kind = _TYPES.get(dtype)
+        if kind is None:
+            raise ValueError(f"results are float32, bfloat16 or float16, not {dtype}")
+        out = torch.empty(shape, dtype=dtype, device=device)
+        return out, out.data_ptr(), kind, shape[1]
+    if out.device != device:
+        raise ValueError(f"out is on {out.device}, expected {device}")
+    return (out,) + _matrix("out", out, shape, dtype if fixed else None)
+
+
 def _tokens(tokens, device):
     size = _TOKEN_BYTES.get(tokens.dtype)
     if size is None or tokens.device != device or tokens.dim() != 1 or not tokens.is_contiguous():
@@ -473,12 +487,10 @@ def pqt_embed(table, tokens, scale=1.0, out=None, out_dtype=None, stream=None):
             return pqt_embed(table, tokens, scale, out, out_dtype)
     ptr, kind, step = _matrix("table", table)
     V, D = table.shape
-    tok, size, n = _tokens(tokens, table.device)
-    if out is None:
-        out = torch.empty((n, D), dtype=out_dtype or table.dtype, device=table.device)
-    _same_device(table.device, out=out)
-    optr, okind, ostep = _matrix("out", out, (n, D), out_dtype)
-    _check(_lib.pqt_embed(ptr, kind, V, D, step, tok, size, n, scale, optr, okind, ostep, table.device.index, _current(table.device.index)))
+    device = table.device
+    tok, size, n = _tokens(tokens, device)
+    out, optr, okind, ostep = _result(out, (n, D), out_dtype or table.dtype, device, out_dtype is not None)
+    _check(_lib.pqt_embed(ptr, kind, V, D, step, tok, size, n, scale, optr, okind, ostep, device.index, _current(device.index)))
     return out
 
 
@@ -489,19 +501,17 @@ def pqt_embed_gradient(grad, tokens, V, scale=1.0, out=None, out_dtype=torch.flo
             return pqt_embed_gradient(grad, tokens, V, scale, out, out_dtype, accumulate)
     ptr, kind, step = _matrix("grad", grad)
     n, D = grad.shape
-    tok, size, nt = _tokens(tokens, grad.device)
+    device = grad.device
+    tok, size, nt = _tokens(tokens, device)
     if nt != n:
         raise ValueError(f"{nt} tokens for {n} rows")
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
-    if out is None:
-        out = torch.empty((V, D), dtype=out_dtype, device=grad.device)
-    _same_device(grad.device, out=out)
-    optr, okind, ostep = _matrix("out", out, (V, D))
+    out, optr, okind, ostep = _result(out, (V, D), out_dtype, device, False)
     nbytes = _lib.pqt_embed_gradient_workspace(n, V, D)
-    ws = _workspace(nbytes, grad.device)
+    ws = _workspace(nbytes, device)
     _check(_lib.pqt_embed_gradient(ptr, kind, step, tok, size, n, V, D, scale, 1 if accumulate else 0, optr, okind, ostep,
-                                   ws.data_ptr() if nbytes else None, nbytes, grad.device.index, _current(grad.device.index)))
+                                   ws.data_ptr() if nbytes else None, nbytes, device.index, _current(device.index)))
     return out
 
 
@@ -514,14 +524,12 @@ def pqt_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, out_dtype=None
     rows, D = x.shape
     params = weight if weight is not None else bias
     ptype = _TYPES if params is None else (params.dtype,)
-    w, b = _vector("weight", weight, D, ptype, x.device), _vector("bias", bias, D, ptype, x.device)
-    if out is None:
-        out = torch.empty((rows, D), dtype=out_dtype or x.dtype, device=x.device)
-    _same_device(x.device, out=out)
-    optr, okind, ostep = _matrix("out", out, (rows, D), out_dtype)
-    mean, rstd = torch.empty(rows, dtype=torch.float32, device=x.device), torch.empty(rows, dtype=torch.float32, device=x.device)
+    device = x.device
+    w, b = _vector("weight", weight, D, ptype, device), _vector("bias", bias, D, ptype, device)
+    out, optr, okind, ostep = _result(out, (rows, D), out_dtype or x.dtype, device, out_dtype is not None)
+    mean, rstd = torch.empty(rows, dtype=torch.float32, device=device), torch.empty(rows, dtype=torch.float32, device=device)
     _check(_lib.pqt_layer_norm(ptr, kind, rows, D, step, w, b, PQT_F32 if params is None else _type_of(params), eps, optr, okind, ostep,
-                               mean.data_ptr(), rstd.data_ptr(), x.device.index, _current(x.device.index)))
+                               mean.data_ptr(), rstd.data_ptr(), device.index, _current(device.index)))
     return out, mean, rstd
 
 
@@ -533,20 +541,18 @@ def pqt_layer_norm_gradient(grad, x, weight, mean, rstd, out=None, stream=None):
             return pqt_layer_norm_gradient(grad, x, weight, mean, rstd, out)
     ptr, kind, step = _matrix("x", x)
     rows, D = x.shape
-    _same_device(x.device, grad=grad)
+    device = x.device
+    _same_device(device, grad=grad)
     gptr, _, gstep = _matrix("grad", grad, (rows, D), x.dtype)
-    w = _vector("weight", weight, D, _TYPES, x.device)
-    mptr, rptr = _vector("mean", mean, rows, _FLOATS, x.device), _vector("rstd", rstd, rows, _FLOATS, x.device)
-    if out is None:
-        out = torch.empty((rows, D), dtype=x.dtype, device=x.device)
-    _same_device(x.device, out=out)
-    optr, _, ostep = _matrix("out", out, (rows, D), x.dtype)
-    dweight, dbias = torch.empty(D, dtype=torch.float32, device=x.device), torch.empty(D, dtype=torch.float32, device=x.device)
+    w = _vector("weight", weight, D, _TYPES, device)
+    mptr, rptr = _vector("mean", mean, rows, _FLOATS, device), _vector("rstd", rstd, rows, _FLOATS, device)
+    out, optr, _, ostep = _result(out, (rows, D), x.dtype, device)
+    dweight, dbias = torch.empty(D, dtype=torch.float32, device=device), torch.empty(D, dtype=torch.float32, device=device)
     nbytes = _lib.pqt_layer_norm_gradient_workspace(rows, D)
-    ws = _workspace(nbytes, x.device)
+    ws = _workspace(nbytes, device)
     _check(_lib.pqt_layer_norm_gradient(gptr, gstep, ptr, step, kind, rows, D, w, PQT_F32 if weight is None else _type_of(weight), mptr,
                                         rptr, optr, ostep, dweight.data_ptr(), dbias.data_ptr(), ws.data_ptr() if nbytes else None,
-                                        nbytes, x.device.index, _current(x.device.index)))
+                                        nbytes, device.index, _current(device.index)))
     return out, dweight, dbias
 
 
@@ -561,12 +567,13 @@ def _empty_blocks(rows, cols, device):
 
 
 def _blocks(name, b):
-    rows, kp = b.codes.shape
-    kb = -(-b.cols // PQT_BLOCK)
-    if b.codes.dtype != torch.float8_e4m3fn or b.scales.dtype != torch.uint8 or not b.codes.is_cuda or b.scales.device != b.codes.device or \
-            kp != kb * PQT_BLOCK or tuple(b.scales.shape) != (rows, kb) or not b.codes.is_contiguous() or not b.scales.is_contiguous():
+    codes, scales, cols = b
+    kb = -(-cols // PQT_BLOCK)
+    rows = codes.shape[0]
+    if codes.dtype != torch.float8_e4m3fn or scales.dtype != torch.uint8 or not codes.is_cuda or scales.device != codes.device or \
+            codes.shape != (rows, kb * PQT_BLOCK) or scales.shape != (rows, kb) or not codes.is_contiguous() or not scales.is_contiguous():
         raise ValueError(f"{name} must be Blocks: contiguous float8_e4m3fn codes (rows, {kb * PQT_BLOCK}) and uint8 scales (rows, {kb}) "
-                         f"for {b.cols} columns")
+                         f"for {cols} columns")
     return rows
 
 
@@ -596,11 +603,10 @@ def pqt_block_product(a, b, bias=None, out=None, out_dtype=torch.bfloat16, strea
     device = a.codes.device
     if a.cols != b.cols:
         raise ValueError(f"a has {a.cols} columns, b {b.cols}")
-    _same_device(device, b=b.codes, out=out)
+    if b.codes.device != device:
+        raise ValueError(f"b is on {b.codes.device}, expected {device}")
     bptr = _vector("bias", bias, n, _FLOATS, device)
-    if out is None:
-        out = torch.empty((m, n), dtype=out_dtype, device=device)
-    optr, okind, ostep = _matrix("out", out, (m, n))
+    out, optr, okind, ostep = _result(out, (m, n), out_dtype, device, False)
     nbytes = _lib.pqt_block_product_workspace(m, n, a.cols)
     ws = _workspace(nbytes, device)
     _check(_lib.pqt_block_product(a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), m, n, a.cols, bptr,
