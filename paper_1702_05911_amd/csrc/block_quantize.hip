@@ -2,10 +2,12 @@
 // of them to at most 448, the largest e4m3 number, and are rounded to the nearest e4m3 number.
 //
 // Bound by memory: two or four bytes a value read, one written for each of the two forms.  Rows alone: sixteen lanes hold a block, eight
-// values each, and find its largest value among themselves; nothing goes through LDS.  With columns: a workgroup of 256 threads
-// holds a tile of 128 x 128, a thread eight rows of eight columns, so that both forms' maxima are found in registers and
-// over few lanes, and the transposed bytes of eight rows make one 8-byte piece; those go through LDS, from where they
+// values each, and find its largest value among themselves; nothing goes through LDS.  With columns: a workgroup of 512 threads
+// holds a tile of 128 x 128, a thread four rows of eight columns, so that both forms' maxima are found in registers and
+// over few lanes, and the transposed bytes of four rows make one 4-byte piece; those go through LDS, from where they
 // are written as whole blocks of 128 bytes.
+// Measured: rows alone 16,384 x 4,096 bf16 41 us, 4.9 TB/s (a large copy 5.1); both forms 8,191 x 2,000 20 us, 3.2 TB/s (27.6 by 256
+// threads of eight rows each, whose loads stood behind conditions: too few on their way).
 #include <algorithm>
 
 #include "encoder.hpp"

@@ -1,15 +1,20 @@
 // Rows of an embedding table for tokens, scaled, and the table's gradient.
 //
 // Lookup: out[t] = scale * table[tokens[t]].  Bound by memory: a row is read and written once.  A group of lanes (as many as the
-// row has pieces of 16 bytes, up to a wavefront) has a row or a section of one, two pieces a lane.
+// row has pieces of 16 bytes, up to a wavefront) has a row or a section of one, up to four pieces a lane, all loaded before the first is
+// stored; 2,048 workgroups walk the tokens, the next one's number read ahead.  100,003 rows of 1,024, bf16 to floats: 78 us, 5.9 TB/s
+// of what has to move (a large copy 5.1, a fill 6.9: most of it is writing).  7 rows: 2.3 us, less than a launch.
 //
 // Gradient: out[v] = scale * sum of grad[t] over the places of v.  Additions by atomics would give other bits on every call and
 // queue up at the tokens that are in every sentence, so the places are sorted by token first: digits of up to ten bits from
-// the lowest on, every pass stable, so that a token's places ascend.  Then the sorted places are walked in chunks of equal length,
-// one a group of lanes, whatever tokens they belong to: rows are read eight at a time, and where the token changes
-// the sum so far goes out.  A token that lies in one chunk is finished there; of the others the chunks' parts go to the workspace, and
-// join_kernel adds them in order.  Rows of tokens that do not occur are cleared beside the chunks.
-// Bound by memory: n rows read, V written; the sort moves 16 bytes a place and pass.
+// the lowest on, every pass stable, so that a token's places ascend.  The sort fills few compute units and waits for memory; the others
+// clear the result meanwhile.  Then the sorted places are walked in chunks of equal length, one a group of lanes, whatever
+// tokens they belong to: rows are read eight at a time, and where the token changes the sum so far goes out.  A token that lies in one
+// chunk is finished there; of the others the chunks' parts go to the workspace, and join_kernel adds them in order.  Up to kFewPlaces
+// places take one launch without a sort.
+// Bound by memory: n rows read, V written; the sort moves 16 bytes a place and pass.  131,071 places of 1,024 bf16 values, 65,536 rows of
+// floats: 150 us, of it two passes of the sort, with the zeros, 54, the sums 84, the joining 11; the bytes alone, at a copy's rate,
+// 103.  Sums in fp32, rounded once.
 #include <algorithm>
 
 #include "encoder.hpp"
@@ -77,8 +82,9 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs g) {
 // ---- gradient: places by token ---------------------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kSortBits = 10, kSortBins = 1 << kSortBits;
-constexpr int64_t kSortTile = 4096;        // places of a tile of the sort, more where there would be ...
-constexpr int64_t kSortTiles = 128;        // ... more tiles than this: a tile adds up the counts of all of them itself
+// Places of a tile of the sort (2,048: a pass over 131,071 places takes 27 us, 4,096: 30, half the tiles but twice the rounds of each), more
+// where there would be more tiles than kSortTiles: a tile adds up the counts of all of them itself.
+constexpr int64_t kSortTile = 2048, kSortTiles = 128;
 constexpr uint32_t kSortAlone = 8192;      // places that one workgroup sorts in one launch
 
 struct SortArgs {
@@ -148,15 +154,29 @@ __device__ void place_digits(const SortArgs& g, int pass, uint32_t first, uint32
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int shift = pass * g.bits;
     const uint32_t mask = (1u << g.bits) - 1u, len = g.tile / kSortWaves;
+    const uint32_t bins = 1u << g.bits;
     uint32_t* out_key = g.key[pass & 1];
     uint32_t* out_place = g.place[pass & 1];
-    for (uint32_t b = tid; b < kSortWaves * kSortBins; b += kSortThreads) (&next[0][0])[b] = 0u;
+    if ((uint32_t)tid < bins)
+        for (int w = 0; w < kSortWaves; ++w) next[w][tid] = 0u;
     __syncthreads();
     const uint32_t lo = first + wave * len, end = min(g.n, lo + len);     // (lo may lie past the last place)
-    for (uint32_t i = lo + lane; i < end; i += kWave * kSortE) {
-        uint32_t key[kSortE];
+    auto look = [&](uint32_t i, uint32_t (&key)[kSortE], uint32_t (&place)[kSortE]) __attribute__((always_inline)) {
 #pragma unroll
-        for (uint32_t u = 0; u < kSortE; ++u) key[u] = key_of(g, pass, min(i + u * kWave, g.n - 1));
+        for (uint32_t u = 0; u < kSortE; ++u) {
+            const uint32_t from = min(i + u * kWave, g.n - 1);
+            key[u] = key_of(g, pass, from);
+            place[u] = pass ? g.place[(pass - 1) & 1][from] : from;
+        }
+    };
+    uint32_t first_key[kSortE], first_place[kSortE];                      // of the first round, which is mostly the only one
+    look(lo + lane, first_key, first_place);
+    for (uint32_t i = lo + lane; i - lane < end; i += kWave * kSortE) {
+        uint32_t key[kSortE], place[kSortE];
+        if (i == lo + lane) {
+#pragma unroll
+            for (int u = 0; u < kSortE; ++u) key[u] = first_key[u];
+        } else look(i, key, place);
 #pragma unroll
         for (uint32_t u = 0; u < kSortE; ++u)
             if (i + u * kWave < end) atomicAdd(&next[wave][(key[u] >> shift) & mask], 1u);
@@ -164,22 +184,29 @@ __device__ void place_digits(const SortArgs& g, int pass, uint32_t first, uint32
     uint32_t total;
     uint32_t at = block_exclusive_sum(all, part, total) + before;         // (a barrier inside)
     __syncthreads();
-    for (int w = 0; w < kSortWaves; ++w) {
-        const uint32_t c = next[w][tid];
-        next[w][tid] = at;
-        at += c;
+    if ((uint32_t)tid < bins) {
+        uint32_t c[kSortWaves];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) c[w] = next[w][tid];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) {
+            next[w][tid] = at;
+            at += c[w];
+        }
     }
     __syncthreads();
     for (uint32_t i = lo + lane; i - lane < end; i += kWave * kSortE) {
         uint32_t key[kSortE], place[kSortE];
+        if (i == lo + lane) {
+#pragma unroll
+            for (int u = 0; u < kSortE; ++u) {
+                key[u] = first_key[u];
+                place[u] = first_place[u];
+            }
+        } else look(i, key, place);
 #pragma unroll
         for (uint32_t u = 0; u < kSortE; ++u) {
-            const uint32_t from = min(i + u * kWave, g.n - 1);
-            key[u] = key_of(g, pass, from);
-            place[u] = pass ? g.place[(pass - 1) & 1][from] : from;
-        }
-#pragma unroll
-        for (uint32_t u = 0; u < kSortE; ++u) {
+            if (i - lane + u * kWave >= end) break;                       // (the same for the wavefront)
             const bool have = i + u * kWave < end;
             const uint32_t digit = (key[u] >> shift) & mask;
             unsigned long long same = __ballot(have);
@@ -218,12 +245,13 @@ __global__ __launch_bounds__(kSortThreads) void token_places_kernel(SortArgs g, 
         return;
     }
     uint32_t before = 0, all = 0;
-    for (uint32_t t = 0; t < tiles; t += 16) {                // sixteen tiles' counts on their way
-        uint32_t c[16];
+    constexpr uint32_t kAtOnce = 32;                          // tiles' counts on their way
+    for (uint32_t t = 0; t < tiles; t += kAtOnce) {
+        uint32_t c[kAtOnce];
 #pragma unroll
-        for (uint32_t u = 0; u < 16; ++u) c[u] = g.counts[(size_t)min(t + u, tiles - 1) * kSortBins + threadIdx.x];
+        for (uint32_t u = 0; u < kAtOnce; ++u) c[u] = g.counts[(size_t)min(t + u, tiles - 1) * kSortBins + threadIdx.x];
 #pragma unroll
-        for (uint32_t u = 0; u < 16; ++u) {
+        for (uint32_t u = 0; u < kAtOnce; ++u) {
             before += t + u < blockIdx.x ? c[u] : 0u;
             all += t + u < tiles ? c[u] : 0u;
         }
