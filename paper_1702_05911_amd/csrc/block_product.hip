@@ -5,6 +5,10 @@
 // accumulators from the first block to the last, in fp32.  B's rows are its first operand: a lane then holds four
 // consecutive columns of the result.
 //
+// fp32 results: that instruction keeps of each product only what reaches 2^-13 of the largest of eight neighbouring products (measured:
+// 1.4e-5 of the result's size on normal data; bf16 results lose 500 times as much when they are rounded).  So the codes become bf16
+// numbers under their scale, which loses nothing, and the bf16 instruction multiplies them, at half the rate; its sums are fp32 ones (9e-9).
+//
 // Three kernels, by the size of the result (plan_of):
 //   wide   256 x 256 a workgroup of four wavefronts, one a SIMD, 128 x 128 each: half the bytes from LDS per multiplication of smaller ones
 //   tile   128 x 128 or 64 x 64 a workgroup, two or four workgroups a compute unit; where there are few tiles, the blocks of k are shared
@@ -166,7 +170,8 @@ __device__ __forceinline__ void store_result(const ProductArgs& g, int row, int 
 
 // ---- tile -----------------------------------------------------------------------------------------------------------
 // Four wavefronts, each a quarter of the tile.  A block of k is multiplied while the next is on its way; with two to four workgroups a
-// compute unit others multiply while this one waits.
+// compute unit others multiply while this one waits.  fp32 results: half of the rate of the bf16 instructions (8192 x 8192 x 8192 1.2 PFLOP/s);
+// the conversions, two a multiplication, hide beside them, the waits of a step do not.
 template <typename TY, int B>
 __global__ __launch_bounds__(256, B == 128 ? 2 : 4) void product_tile_kernel(ProductArgs g) {
     constexpr bool kExact = sizeof(TY) == 4;
@@ -275,8 +280,10 @@ __global__ __launch_bounds__(256, B == 128 ? 2 : 4) void product_tile_kernel(Pro
 //   first half   barrier; loads lo of k + 2; reads hi of k; multiplies A lo with B lo, then with B hi
 //   second half  barrier; loads hi of k + 2; reads lo of k + 1; multiplies A hi with B lo, then with B hi
 // so that a load has one and a half blocks of time, and 16 loads (of the two halves after it) may still be out when it is waited for.
-// 8192 x 8192 x 8192 2.78 PFLOP/s, 16384 x 4096 x 4096 2.45; this card's instruction by itself 4.0 on such data (its clock falls), with
-// wavefronts of 64 x 128, two a SIMD, whose fragments take all of LDS's rate, 1.9.
+// 8192 x 8192 x 8192 2.9 PFLOP/s, 16384 x 4096 x 4096 2.5 (216 us by itself, 220 to 260 in a row of them); this card's instruction by itself
+// 4.0 on such data (its clock falls), with wavefronts of 64 x 128, two a SIMD, whose fragments take all of LDS's rate, 1.9.  A block of k
+// takes 1.26 us, the first loads and the result of a tile 14, in which nothing is multiplied: tiles in one long-lived workgroup with stores
+// straight from the registers were slower (249), as their sums did not stay in registers.
 template <typename TY>
 __global__ __launch_bounds__(256, 1) void product_wide_kernel(ProductArgs g) {
     constexpr int B = 256, F = 8, kHalf = B * kBlock;
@@ -473,7 +480,8 @@ __global__ __launch_bounds__(256) void join_splits_kernel(ProductArgs g) {
 constexpr int kFewRows = 16, kFewWaves = 8, kFewRun = 4;
 
 // A wavefront multiplies 16 NF rows of B with all of A's over every kFewWaves-th run of four blocks, all of whose loads are sent first; the sums
-// of the wavefronts are added in order.  Bound by the reading of B.
+// of the wavefronts are added in order.  Bound by the reading of B: 1 x 4096 x 4096 4.8 us with B in the caches, 6.8 from memory (2.5 TB/s: one
+// round of loads, whose latency it is); 16 x 32768 x 4096 24.6, 5.5 TB/s (NF = 1: 35.1).
 template <typename TY, int NF>
 __global__ __launch_bounds__(kFewWaves * kWave) void product_few_kernel(ProductArgs g) {
     constexpr bool kExact = sizeof(TY) == 4;
