@@ -401,12 +401,16 @@ __global__ __launch_bounds__(256, 1) void product_wide_kernel(ProductArgs g) {
     fetch_scales(0);
 #pragma unroll
     for (int e = 0; e < 8; ++e) fetch(lo_even, a_lo, b_lo, 0, e);
+    __builtin_amdgcn_sched_barrier(0);                          // (loads are waited for by their number: the halves stay in order)
 #pragma unroll
     for (int e = 0; e < 8; ++e) fetch(hi_even, a_hi, b_hi, 0, e);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int e = 0; e < 8; ++e) fetch(lo_odd, a_lo, b_lo, 1, e);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int e = 0; e < 8; ++e) fetch(hi_odd, a_hi, b_hi, 1, e);
+    __builtin_amdgcn_sched_barrier(0);
     wait_loads<24>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);

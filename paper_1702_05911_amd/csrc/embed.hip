@@ -378,35 +378,21 @@ __global__ __launch_bounds__(kSumThreads) void sum_rows_kernel(SumArgs g) {
     else finish_row<TY, E>(g, cur, lane, sum);
 }
 
-// The token that goes on after chunk c, if it began there: its parts, four wavefronts a quarter each.
+// Tokens that go on after the chunk they began in: a wavefront looks at the end of one chunk and adds up the token's parts if they
+// are few; of those with more, the workgroup's four wavefronts take a quarter of the parts each.  2,048 chunks of 1,024 columns
+// take 10.6 us, the chain of reads to a token's end and parts (a workgroup a chunk: 11.6, of 512 threads 17.5, for starting many that find nothing).
 template <typename TY>
 __global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs g) {
     constexpr int E = 4, kWaves = kSumThreads / kWave;
     __shared__ f32x4 sums[kWaves][kWave];
+    __shared__ uint32_t many[kWaves];                          // parts of the wavefronts' tokens, where the workgroup adds them up
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const uint32_t c = blockIdx.x;
-    const uint64_t end = ((uint64_t)c + 1) * g.chunk;
-    if (end >= g.n) return;
-    const uint32_t j1 = (uint32_t)end, j0 = j1 - g.chunk;
-    const uint32_t v = g.key[j1 - 1];
-    if (v >= g.V || g.key[j1] != v) return;
-    if (g.key[j0] == v && j0 > 0 && g.key[j0 - 1] == v) return;       // an earlier chunk's
-    // part 0 is chunk c's own, part i that of the i-th chunk after it: as many as begin with the token
-    uint32_t parts = 1;
-    while (true) {
-        const uint64_t at = ((uint64_t)c + parts + lane) * g.chunk;
-        const unsigned long long more = __ballot(at < g.n && g.key[min(at, (uint64_t)g.n - 1)] == v);
-        const uint32_t run = more == ~0ull ? kWave : (uint32_t)__ffsll((long long)~more) - 1u;
-        parts += run;
-        if (run < kWave) break;
-    }
-    const uint32_t per = (parts + kWaves - 1) / kWaves;
     const int64_t col = ((int64_t)blockIdx.y * kWave + lane) * E;
-    const Lane<E> own(col, g.D);
-    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (col < g.D) {
-        const uint32_t hi = min(parts, (wave + 1) * per);
-        for (uint32_t i = wave * per; i < hi; i += kSumRows) {
+    const Lane<E> own(col < g.D ? col : 0, g.D);
+    // parts lo .. hi - 1 of the token that began in chunk c: part 0 is chunk c's own, part i that of the i-th chunk after it
+    auto add_parts = [&](uint32_t c, uint32_t lo, uint32_t hi) {
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (uint32_t i = lo; i < hi; i += kSumRows) {
             typename Piece_<float, E>::type r[kSumRows];
 #pragma unroll
             for (int u = 0; u < kSumRows; ++u) {
@@ -417,13 +403,47 @@ __global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs g) {
             for (int u = 0; u < kSumRows; ++u)
                 if (i + u < hi) sum = sum + r[u];
         }
-    }
-    sums[wave][lane] = sum;
+        return sum;
+    };
+    // how many parts the token that goes on after chunk c has, if it began there: one more than chunks after c begin with it
+    auto parts_of = [&](uint32_t c, uint32_t& v) -> uint32_t {
+        const uint64_t end = ((uint64_t)c + 1) * g.chunk;
+        if (end >= g.n) return 0;
+        const uint32_t j1 = (uint32_t)end, j0 = j1 - g.chunk;
+        v = g.key[j1 - 1];
+        const uint32_t after = g.key[j1], first = g.key[j0], before = g.key[max(j0, 1u) - 1u];
+        if (v >= g.V || after != v) return 0;
+        if (first == v && j0 > 0 && before == v) return 0;     // an earlier chunk's
+        uint32_t parts = 1;
+        while (true) {
+            const uint64_t at = ((uint64_t)c + parts + lane) * g.chunk;
+            const unsigned long long more = __ballot(at < g.n && g.key[min(at, (uint64_t)g.n - 1)] == v);
+            const uint32_t run = more == ~0ull ? kWave : (uint32_t)__ffsll((long long)~more) - 1u;
+            parts += run;
+            if (run < kWave) return parts;
+        }
+    };
+    const uint32_t c0 = blockIdx.x * kWaves;
+    uint32_t v = 0;
+    const uint32_t parts = parts_of(c0 + wave, v);
+    if (lane == 0) many[wave] = parts > kSumRows ? parts : 0u;
+    if (parts > 0 && parts <= kSumRows && col < g.D) finish_row<TY, E>(g, v, own, add_parts(c0 + wave, 0, parts));
     __syncthreads();
-    if (wave || col >= g.D) return;
+    for (int w = 0; w < kWaves; ++w) {
+        const uint32_t all = many[w];
+        if (all == 0) continue;                                // (the same for the workgroup)
+        const uint32_t per = (all + kWaves - 1) / kWaves;
+        f32x4 sum = add_parts(c0 + w, min(all, wave * per), min(all, (wave + 1) * per));
+        sums[wave][lane] = sum;
+        __syncthreads();
+        if (wave == w && col < g.D) {
+            sum = sums[0][lane];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) sum = sum + sums[w][lane];
-    finish_row<TY, E>(g, v, own, sum);
+            for (int o = 1; o < kWaves; ++o) sum = sum + sums[o][lane];
+            finish_row<TY, E>(g, v, own, sum);
+        }
+        __syncthreads();
+    }
 }
 
 // ---- gradient of few places --------------------------------------------------------------------------------------------
@@ -706,7 +726,7 @@ int pqt_embed_gradient(const void* grad, int grad_type, int64_t grad_stride, con
     });
     HIP_TRY(hipGetLastError());
     if (s.chunks > 1) {
-        const dim3 join(s.chunks - 1, (unsigned)((D + 4 * kWave - 1) / (4 * kWave)));
+        const dim3 join((s.chunks - 1 + kSumThreads / kWave - 1) / (kSumThreads / kWave), (unsigned)((D + 4 * kWave - 1) / (4 * kWave)));
         with_type(out_type, [&](auto y) { hipLaunchKernelGGL((join_kernel<decltype(y)>), join, dim3(kSumThreads), 0, st, g); });
         HIP_TRY(hipGetLastError());
     }
