@@ -718,3 +718,13 @@ def test_refusals_of_shapes_and_types():
             call()
     with pytest.raises(pqt.PqtError):
         pqt.pqt_embed_gradient(x, tok, 0)
+
+
+@gpu
+def test_refusals_of_parameter_types():
+    x = torch.zeros((4, 8), device=dev())
+    for t in (torch.zeros(8, device=dev(), dtype=torch.int32), torch.zeros(8, device=dev(), dtype=torch.float64)):
+        for call in (lambda: pqt.pqt_layer_norm(x, t), lambda: pqt.pqt_layer_norm(x, None, t), lambda: pqt.pqt_layer_norm(x, t, t),
+                     lambda: pqt.pqt_layer_norm_gradient(x, x, t, x[:, 0].contiguous(), x[:, 0].contiguous())):
+            with pytest.raises(ValueError):
+                call()
