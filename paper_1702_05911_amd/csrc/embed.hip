@@ -10,8 +10,8 @@
 // the lowest on, every pass stable, so that a token's places ascend.  The sort fills few compute units and waits for memory; the others
 // clear the result meanwhile.  Then the sorted places are walked in chunks of equal length, one a group of lanes, whatever
 // tokens they belong to: rows are read eight at a time, and where the token changes the sum so far goes out.  A token that lies in one
-// chunk is finished there; of the others the chunks' parts go to the workspace, and join_kernel adds them in order.  Up to kFewPlaces
-// places take one launch without a sort.
+// chunk is finished there; of the others the chunks' parts go to the workspace, and join_kernel adds them in order.  Up to kRankPlaces are
+// put in order by one launch, and a few places need none (few_places).
 // Bound by memory: n rows read, V written; the sort moves 16 bytes a place and pass.  131,071 places of 1,024 bf16 values, 65,536 rows of
 // floats: 150 us, of it two passes of the sort, with the zeros, 54, the sums 84, the joining 11; the bytes alone, at a copy's rate,
 // 103.  Sums in fp32, rounded once.
@@ -85,7 +85,6 @@ constexpr int kSortBits = 10, kSortBins = 1 << kSortBits;
 // Places of a tile of the sort (2,048: a pass over 131,071 places takes 27 us, 4,096: 30, half the tiles but twice the rounds of each), more
 // where there would be more tiles than kSortTiles: a tile adds up the counts of all of them itself.
 constexpr int64_t kSortTile = 2048, kSortTiles = 128;
-constexpr uint32_t kSortAlone = 8192;      // places that one workgroup sorts in one launch
 
 struct SortArgs {
     const void* tokens;
@@ -259,21 +258,62 @@ __global__ __launch_bounds__(kSortThreads) void token_places_kernel(SortArgs g, 
     place_digits(g, pass, blockIdx.x * g.tile, before, all, next, part);
 }
 
-// few places (or none: zeros only): all passes by one workgroup
-__global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(SortArgs g, ClearArgs clear) {
-    __shared__ uint32_t next[kSortWaves][kSortBins];
-    __shared__ uint32_t part[kSortWaves];
-    __shared__ uint32_t hist[kSortBins];
-    if (blockIdx.x >= 1) {
-        clear_units(clear, blockIdx.x - 1, gridDim.x - 1);
+// Fewer places are put in order by one launch that counts: a token's rank is the number of smaller ones and of equal ones before it.  A
+// workgroup has kRankTile places, each wavefront all of them twice: its halves look through other blocks of 64 tokens, from LDS.  Without
+// places: zeros only.  n^2 comparisons, bound by their instructions and LDS reads: 2,000 places 5.7 us, 8,000 10.0 (with 20 MB of zeros beside them
+// 7.2 and 13.2; workgroups of 16 places 7.0 and 15.3); the passes above take 23 for 8,193, two of one workgroup 27 for 8,000.
+constexpr uint32_t kRankPlaces = 8192, kRankTile = 32, kRankBlock = 64;
+
+__global__ __launch_bounds__(kSortThreads) void rank_tokens_kernel(SortArgs g, uint32_t tiles, ClearArgs clear) {
+    constexpr uint32_t kParts = kWave / kRankTile, kPitch = kRankBlock + 4;         // (the parts' reads in different banks)
+    __shared__ __align__(16) uint32_t keys[kRankPlaces / kRankBlock * kPitch];
+    __shared__ uint32_t ranks[kRankTile];
+    if (blockIdx.x >= tiles) {
+        clear_units(clear, blockIdx.x - tiles, gridDim.x - tiles);
         return;
     }
-    if (g.n == 0) return;
-    for (int pass = 0; pass < g.passes; ++pass) {
-        count_digits(g, pass, 0, hist);
-        place_digits(g, pass, 0, 0, hist[threadIdx.x], next, part);
-        __threadfence_block();
-        __syncthreads();                                      // the next pass reads what other wavefronts wrote
+    const uint32_t tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const uint32_t blocks = (g.n + kRankBlock - 1) / kRankBlock;
+    auto fill = [&](const auto* tokens) __attribute__((always_inline)) {    // (all of a thread's tokens on their way at once)
+        int64_t v[kRankPlaces / kSortThreads];
+#pragma unroll
+        for (uint32_t u = 0; u < kRankPlaces / kSortThreads; ++u) v[u] = tokens[min(u * kSortThreads + tid, g.n - 1)];
+#pragma unroll
+        for (uint32_t u = 0; u < kRankPlaces / kSortThreads; ++u) {
+            const uint32_t i = u * kSortThreads + tid;
+            const uint32_t key = v[u] >= 0 && v[u] < (int64_t)g.V ? (uint32_t)v[u] : g.V;
+            if (i < blocks * kRankBlock) keys[i / kRankBlock * kPitch + i % kRankBlock] = i < g.n ? key : ~0u;      // (past the last place: after all)
+        }
+    };
+    if (g.wide_tokens) fill(static_cast<const int64_t*>(g.tokens));
+    else fill(static_cast<const int32_t*>(g.tokens));
+    if (tid < kRankTile) ranks[tid] = 0u;
+    __syncthreads();
+    const uint32_t i = blockIdx.x * kRankTile + lane % kRankTile, own = i / kRankBlock, mine = keys[own * kPitch + i % kRankBlock];
+    uint32_t rank = 0;
+    for (uint32_t b0 = wave * kParts; b0 < blocks; b0 += kSortWaves * kParts) {
+        const uint32_t b = b0 + lane / kRankTile;
+        if (b >= blocks) break;
+        const uint32_t* block = keys + b * kPitch;
+        auto count = [&](auto smaller) __attribute__((always_inline)) {
+#pragma unroll
+            for (uint32_t e = 0; e < kRankBlock; e += 4) {
+                const uint4 k = *reinterpret_cast<const uint4*>(block + e);
+                const uint32_t other[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u) rank += smaller(other[u], e + u) ? 1u : 0u;
+            }
+        };
+        const uint32_t below = mine + (b < own ? 1u : 0u);     // of the blocks before, equal ones count too
+        if (own < b0 || own >= b0 + kParts) count([&](uint32_t other, uint32_t) { return other < below; });
+        else count([&](uint32_t other, uint32_t at) { return other < (b == own && at < i % kRankBlock ? mine + 1u : below); });
+    }
+    atomicAdd(&ranks[lane % kRankTile], rank);
+    __syncthreads();
+    if (tid < kRankTile && i < g.n) {
+        const uint32_t to = ranks[tid];
+        g.key[0][to] = mine;
+        g.place[0][to] = i;
     }
 }
 
@@ -447,11 +487,14 @@ __global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs g) {
 }
 
 // ---- gradient of few places --------------------------------------------------------------------------------------------
-// Up to kFewPlaces places need no sort: every workgroup looks through all the tokens by itself.  A workgroup for each place (and section of
-// columns) sums its token's rows if no earlier place has it, its wavefronts a quarter of them each; workgroups behind those clear the
-// rows that no token names.  One launch: the sorting ones take three, which wait for memory a few times each.
-constexpr uint32_t kFewPlaces = 512;
-constexpr int kFewClear = 32;              // table rows a workgroup clears
+// Up to kFewPlaces places need no order: every workgroup looks through all the tokens by itself.  A workgroup for each place (and section of
+// columns) sums its token's rows if no earlier place has it, its wavefronts a share of them each; workgroups behind those clear the
+// rows that no token names.  One launch; the three with an order wait for memory a few times each, but start fewer wavefronts.  Measured (by one,
+// by three): 300 places x 1,024 columns 6.9 and 15.2 us, 1,000 x 256 6.2 and 15.2, 1,000 x 1,024 14.8 and 16.0, 512 x 4,096 (8,192
+// workgroups) 21.8 and 19.6, 1,000 x 4,096 47 and 20; 1,000 places of one token 21 and 14.
+constexpr uint32_t kFewPlaces = 1024;      // two tokens a thread
+constexpr int64_t kFewBlocks = 4096;       // workgroups for places and sections
+constexpr int kFewClear = 8;               // table rows a wavefront clears
 
 struct FewArgs {
     SumArgs sum;
@@ -460,36 +503,37 @@ struct FewArgs {
     uint32_t sum_blocks;
 };
 
-template <typename TX, typename TY>
-__global__ __launch_bounds__(kSumThreads) void few_places_kernel(FewArgs f) {
-    constexpr int E = kSumE, kWaves = kSumThreads / kWave;
-    static_assert(kFewPlaces == 2 * kSumThreads, "two tokens a thread");
+// NT: 256 threads for up to 512 places, 512 for more
+template <typename TX, typename TY, int NT>
+__global__ __launch_bounds__(NT) void few_places_kernel(FewArgs f) {
+    constexpr int E = kSumE, kWaves = NT / kWave;
     const SumArgs& g = f.sum;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-    int64_t mine[2];                                           // the tokens of places tid and kSumThreads + tid
+    int64_t mine[2];                                           // the tokens of places tid and NT + tid
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const uint32_t i = h * kSumThreads + tid;
+        const uint32_t i = h * NT + tid;
         mine[h] = token_at(f.tokens, f.wide_tokens, min(i, g.n - 1));
         if (i >= g.n) mine[h] = -1;
     }
     if (blockIdx.x >= f.sum_blocks) {
-        __shared__ uint32_t named;
-        const int64_t v0 = (int64_t)(blockIdx.x - f.sum_blocks) * kFewClear;
+        constexpr int kClear = kFewClear * kWaves;
+        __shared__ unsigned long long named;
+        const int64_t v0 = (int64_t)(blockIdx.x - f.sum_blocks) * kClear;
         if (tid == 0) named = 0u;
         __syncthreads();
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            if (mine[h] >= v0 && mine[h] < v0 + kFewClear) atomicOr(&named, 1u << (int)(mine[h] - v0));
+            if (mine[h] >= v0 && mine[h] < v0 + kClear) atomicOr(&named, 1ull << (int)(mine[h] - v0));
         __syncthreads();
-        for (int r = wave; r < kFewClear; r += kWaves) {
+        for (int r = wave; r < kClear; r += kWaves) {
             if (((named >> r) & 1u) || v0 + r >= g.V) continue;
             TY* row = static_cast<TY*>(g.out) + (v0 + r) * g.out_stride;
             for (int64_t c = lane * E; c < g.D; c += kWave * E) store_piece<TY, E>(row + c, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, (int)min((int64_t)E, g.D - c));
         }
         return;
     }
-    __shared__ uint32_t places[kFewPlaces];
+    __shared__ uint32_t places[2 * NT];
     __shared__ uint32_t counts[2 * kWaves];
     __shared__ f32x4 sums[kWaves][kWave];
     const uint32_t t = blockIdx.x / g.sections, section = blockIdx.x - t * g.sections;
@@ -508,7 +552,7 @@ __global__ __launch_bounds__(kSumThreads) void few_places_kernel(FewArgs f) {
     for (int h = 0; h < 2; ++h) {
         uint32_t before = 0;
         for (int w = 0; w < 2 * kWaves; ++w) before += w < h * kWaves + wave ? counts[w] : 0u;
-        if (mine[h] == v) places[before + (uint32_t)__popcll(same[h] & ((1ull << lane) - 1ull))] = h * kSumThreads + tid;
+        if (mine[h] == v) places[before + (uint32_t)__popcll(same[h] & ((1ull << lane) - 1ull))] = h * NT + tid;
     }
     for (int w = 0; w < 2 * kWaves; ++w) total += counts[w];
     __syncthreads();
@@ -533,6 +577,8 @@ __global__ __launch_bounds__(kSumThreads) void few_places_kernel(FewArgs f) {
     finish_row<TY, E>(g, (uint32_t)v, own, sum);
 }
 
+bool few_places(int64_t n, int64_t D) { return n <= kFewPlaces && n * ((D + kWave * kSumE - 1) / (kWave * kSumE)) <= kFewBlocks; }
+
 // Places of a chunk: about 2,048 groups' worth, at least 16 so that few tokens are in parts, at most 256
 uint32_t chunk_places(int64_t n) {
     uint32_t c = 16;
@@ -546,7 +592,7 @@ struct GradientSpace {                     // byte offsets of the workspace
 };
 GradientSpace gradient_space(int64_t n, int64_t D) {
     GradientSpace s{};
-    const int64_t least = n <= kSortAlone ? n : std::max<int64_t>(kSortTile, (n + kSortTiles - 1) / kSortTiles);
+    const int64_t least = n <= kRankPlaces ? n : std::max<int64_t>(kSortTile, (n + kSortTiles - 1) / kSortTiles);
     s.tile = (uint32_t)((least + kSortThreads - 1) / kSortThreads * kSortThreads);
     s.tiles = (uint32_t)((n + s.tile - 1) / s.tile);
     s.chunk = chunk_places(n);
@@ -610,7 +656,7 @@ int pqt_embed(const void* table, int type, int64_t V, int64_t D, int64_t table_s
 }
 
 size_t pqt_embed_gradient_workspace(int64_t n, int64_t V, int64_t D) {
-    if (n <= pqt::kFewPlaces || V < 1 || D < 1 || n > pqt::kMaxPlaces || V > pqt::kMaxRows || D > pqt::kMaxEmbedD) return 0;
+    if (n < 1 || V < 1 || D < 1 || pqt::few_places(n, D) || n > pqt::kMaxPlaces || V > pqt::kMaxRows || D > pqt::kMaxEmbedD) return 0;
     return pqt::gradient_space(n, D).total;
 }
 
@@ -628,7 +674,7 @@ int pqt_embed_gradient(const void* grad, int grad_type, int64_t grad_stride, con
     if (!out || (n > 0 && (!grad || !tokens))) return fail(PQT_EINVAL, "pqt_embed_gradient: null pointer");
     if (!aligned_to(grad, type_bytes(grad_type)) || !aligned_to(out, type_bytes(out_type)) || !aligned_to(tokens, (size_t)token_bytes))
         return fail(PQT_EINVAL, "pqt_embed_gradient: a pointer is not aligned to its element");
-    const GradientSpace s = n > kFewPlaces ? gradient_space(n, D) : GradientSpace{};
+    const GradientSpace s = n > 0 && !few_places(n, D) ? gradient_space(n, D) : GradientSpace{};
     if (s.total && (!workspace || workspace_bytes < s.total || !aligned_to(workspace, 16)))
         return fail(PQT_EINVAL, "pqt_embed_gradient: workspace of %zu bytes, aligned to 16, needed (%zu given)", s.total, workspace_bytes);
     const int log_lanes = log_lanes_for((D + kSumE - 1) / kSumE);
@@ -651,14 +697,16 @@ int pqt_embed_gradient(const void* grad, int grad_type, int64_t grad_stride, con
     g.scale = scale;
     g.accumulate = accumulate != 0;
     g.stream = (double)V * D * type_bytes(out_type) > kStreamBytes;
-    if (n > 0 && n <= kFewPlaces) {
+    if (n > 0 && few_places(n, D)) {
         FewArgs f{g, tokens, token_bytes == 8, 0};
         f.sum.sections = (uint32_t)((D + kWave * kSumE - 1) / (kWave * kSumE));
         f.sum_blocks = (uint32_t)n * f.sum.sections;
-        const uint32_t clear = accumulate ? 0u : (uint32_t)((V + kFewClear - 1) / kFewClear);
+        const int threads = n <= 512 ? 256 : 512, rows = kFewClear * (threads / kWave);
+        const uint32_t clear = accumulate ? 0u : (uint32_t)((V + rows - 1) / rows);
         with_type(grad_type, [&](auto x) {
             with_type(out_type, [&](auto y) {
-                hipLaunchKernelGGL((few_places_kernel<decltype(x), decltype(y)>), dim3(f.sum_blocks + clear), dim3(kSumThreads), 0, st, f);
+                if (threads == 256) hipLaunchKernelGGL((few_places_kernel<decltype(x), decltype(y), 256>), dim3(f.sum_blocks + clear), dim3(256), 0, st, f);
+                else hipLaunchKernelGGL((few_places_kernel<decltype(x), decltype(y), 512>), dim3(f.sum_blocks + clear), dim3(512), 0, st, f);
             });
         });
         HIP_TRY(hipGetLastError());
@@ -698,8 +746,8 @@ int pqt_embed_gradient(const void* grad, int grad_type, int64_t grad_stride, con
         return (uint32_t)std::min<int64_t>((clear.last - clear.first + kSortWaves - 1) / kSortWaves, kClearBlocks);
     };
     if (s.tiles <= 1) {
-        const uint32_t more = share(1);
-        hipLaunchKernelGGL(sort_tokens_kernel, dim3(1 + more), dim3(kSortThreads), 0, st, o, clear);
+        const uint32_t more = share(1), blocks = (uint32_t)((n + kRankTile - 1) / kRankTile);
+        hipLaunchKernelGGL(rank_tokens_kernel, dim3(blocks + more), dim3(kSortThreads), 0, st, o, blocks, clear);
         HIP_TRY(hipGetLastError());
     } else {
         for (int pass = 0; pass < o.passes; ++pass) {
@@ -712,8 +760,9 @@ int pqt_embed_gradient(const void* grad, int grad_type, int64_t grad_stride, con
         }
     }
     if (n == 0) return PQT_OK;
-    g.key = o.key[(o.passes - 1) & 1];
-    g.place = o.place[(o.passes - 1) & 1];
+    const int last = s.tiles <= 1 ? 0 : (o.passes - 1) & 1;
+    g.key = o.key[last];
+    g.place = o.place[last];
     g.parts = reinterpret_cast<float*>(ws + s.parts);
     g.chunk = s.chunk;
     g.sections = (uint32_t)sections;

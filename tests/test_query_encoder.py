@@ -728,3 +728,23 @@ def test_refusals_of_parameter_types():
                      lambda: pqt.pqt_layer_norm_gradient(x, x, t, x[:, 0].contiguous(), x[:, 0].contiguous())):
             with pytest.raises(ValueError):
                 call()
+
+
+@gpu
+@pytest.mark.parametrize("n,V,D,kind,out,ids", [
+    (600, 50, 4100, "f32", "f32", 32), (1024, 40, 300, "bf16", "f32", 64), (1024, 9, 1025, "f16", "f16", 64), (1025, 700, 70, "f32", "f32", 32), (300, 20, 5000, "bf16", "bf16", 64),
+    (1984, 1, 65, "f32", "f32", 64), (4097, 100_000, 33, "bf16", "f32", 32), (8191, 2, 4, "f32", "bf16", 64), (7777, 7000, 3, "f16", "f32", 64)])
+def test_embed_gradient_between_few_and_many(n, V, D, kind, out, ids):
+    grad = normal((n, D), TYPES[kind], n + V)
+    tok = some_tokens(n, V, n + D, torch.int32 if ids == 32 else torch.int64)
+    total, size, count = gradient_reference(grad, tok, V, 0.5)
+    view, check = guarded(V, D, TYPES[out])
+    got = pqt.pqt_embed_gradient(grad, tok, V, 0.5, out=view, out_dtype=TYPES[out])
+    within(got, total, size * (count + 2) * U, "gradient")
+    check()
+    assert torch.equal(pqt.pqt_embed_gradient(grad, tok, V, 0.5, out_dtype=TYPES[out]), view)
+    start = normal((V, D), TYPES[out], 5)
+    view.copy_(start)
+    pqt.pqt_embed_gradient(grad, tok, V, 0.5, out=view, out_dtype=TYPES[out], accumulate=True)
+    within(view, total + start.double().cpu(), size * (count + 2) * U + (total.abs() + start.double().cpu().abs()) * U, "accumulated gradient")
+    check()
