@@ -41,7 +41,9 @@ struct NormArgs {
     void* out;                             // y or dx
     float* mean;
     float* rstd;
-    float* parts;                          // gradient: workgroups x 2 x D
+    float* parts;                          // gradient: workgroups x 2 x D, or null: the one workgroup's sums are ...
+    float* dweight;                        // ... these (either may be null)
+    float* dbias;
     int64_t rows, x_stride, grad_stride, out_stride;
     int D, param_type, want_parts;
     float eps;
@@ -217,7 +219,11 @@ __global__ __launch_bounds__(kGradThreads) void layer_norm_gradient_kernel(NormA
     }
     if (!g.want_parts) return;
     // The groups' sums, dweight's and then dbias's: over the groups of a wavefront by lanes, over its wavefronts in LDS.
-    float* out = g.parts + (size_t)blockIdx.x * 2 * g.D;
+    float* out[2] = {g.dweight, g.dbias};
+    if (g.parts) {
+        out[0] = g.parts + (size_t)blockIdx.x * 2 * g.D;
+        out[1] = out[0] + g.D;
+    }
     if constexpr (kRowsOfSums > 1) {
         const int row = threadIdx.x / (G < kWave ? kWave : G);
         for (int round = 0; round < 2; ++round) {
@@ -236,7 +242,7 @@ __global__ __launch_bounds__(kGradThreads) void layer_norm_gradient_kernel(NormA
                 float v = sums[0][c];
 #pragma unroll
                 for (int i = 1; i < kRowsOfSums; ++i) v += sums[i][c];
-                out[(size_t)round * g.D + c] = v;
+                if (out[round]) out[round][c] = v;
             }
             __syncthreads();
         }
@@ -244,10 +250,8 @@ __global__ __launch_bounds__(kGradThreads) void layer_norm_gradient_kernel(NormA
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int c = (p * G + l) * kNormE;
-            if (have[p]) {
-                store_piece<float, kNormE>(out + c, dw[p], have[p]);
-                store_piece<float, kNormE>(out + g.D + c, db[p], have[p]);
-            }
+            if (have[p] && out[0]) store_piece<float, kNormE>(out[0] + c, dw[p], have[p]);
+            if (have[p] && out[1]) store_piece<float, kNormE>(out[1] + c, db[p], have[p]);
         }
     }
 }
@@ -357,14 +361,23 @@ void with_gradient_shape(int64_t D, F&& f) {
     else f(Int<512>{}, Int<4>{});
 }
 
+// Workgroups of the backward kernel.  A single one for up to two rows a group: its sums are the result, without a second launch (8 x 1,000 bf16
+// 4.6 us in a graph, by two launches 6.3; 11.7 and 16.0 from Python.  Four rows a group: 32 x 1,000 7.9 and 6.5, 4 x 16,384 18.6 and 11.3).
+constexpr int kAloneRows = 2;
 unsigned gradient_blocks(int64_t rows, int groups) {
-    return (unsigned)std::min<int64_t>((rows + groups - 1) / groups, kGradBlocks);
+    return rows <= (int64_t)kAloneRows * groups ? 1u : (unsigned)std::min<int64_t>((rows + groups - 1) / groups, kGradBlocks);
 }
 unsigned gradient_blocks(int64_t rows, int64_t D, int type) {
     unsigned n = 0;
     if (D > one_pass_values(type)) return (unsigned)std::min<int64_t>(rows, kLongParts);
     with_gradient_shape(D, [&](auto G, auto) { n = gradient_blocks(rows, kGradThreads / G.value); });
     return n;
+}
+
+// rows of partial sums
+unsigned gradient_parts(int64_t rows, int64_t D, int type) {
+    const unsigned n = gradient_blocks(rows, D, type);
+    return n == 1 && D <= one_pass_values(type) ? 0 : n;
 }
 
 }  // namespace
@@ -420,7 +433,7 @@ int pqt_layer_norm(const void* x, int type, int64_t rows, int64_t D, int64_t x_s
 
 size_t pqt_layer_norm_gradient_workspace(int64_t rows, int64_t D) {
     if (rows < 1 || D < 1 || D > pqt::kMaxNormD) return 0;
-    return (size_t)std::max(pqt::gradient_blocks(rows, D, PQT_F32), pqt::gradient_blocks(rows, D, PQT_BF16)) * 2 * (size_t)D * sizeof(float);
+    return (size_t)std::max(pqt::gradient_parts(rows, D, PQT_F32), pqt::gradient_parts(rows, D, PQT_BF16)) * 2 * (size_t)D * sizeof(float);
 }
 
 int pqt_layer_norm_gradient(const void* grad, int64_t grad_stride, const void* x, int64_t x_stride, int type, int64_t rows,
@@ -454,7 +467,10 @@ int pqt_layer_norm_gradient(const void* grad, int64_t grad_stride, const void* x
     g.out = dx;
     g.mean = const_cast<float*>(mean);
     g.rstd = const_cast<float*>(rstd);
-    g.parts = static_cast<float*>(workspace);
+    const bool alone = rows > 0 && gradient_parts(rows, D, type) == 0;
+    g.parts = alone ? nullptr : static_cast<float*>(workspace);
+    g.dweight = dweight;
+    g.dbias = dbias;
     g.rows = rows;
     g.x_stride = x_stride;
     g.grad_stride = grad_stride;
@@ -479,7 +495,7 @@ int pqt_layer_norm_gradient(const void* grad, int64_t grad_stride, const void* x
         });
         HIP_TRY(hipGetLastError());
     }
-    if (sums) {
+    if (sums && !alone) {
         hipLaunchKernelGGL(columns_kernel, dim3((unsigned)((2 * D + kWave - 1) / kWave)), dim3(1024), 0, st, g.parts, (int)blocks, (int)D, dweight, dbias);
         HIP_TRY(hipGetLastError());
     }

@@ -748,3 +748,24 @@ def test_embed_gradient_between_few_and_many(n, V, D, kind, out, ids):
     pqt.pqt_embed_gradient(grad, tok, V, 0.5, out=view, out_dtype=TYPES[out], accumulate=True)
     within(view, total + start.double().cpu(), size * (count + 2) * U + (total.abs() + start.double().cpu().abs()) * U, "accumulated gradient")
     check()
+
+
+@gpu
+@pytest.mark.parametrize("rows,D,kind", [(1, 1, "f32"), (2, 1000, "bf16"), (16, 1000, "f16"), (17, 1000, "bf16"), (128, 60, "f32"), (129, 60, "f32"), (2, 8200, "f32"),
+                                         (2, 8200, "bf16"), (3, 8200, "bf16"), (2, 16384, "f16"), (1, 16385, "f16")])
+def test_layer_norm_gradient_of_few_rows(rows, D, kind):
+    x, grad = normal((rows, D), TYPES[kind], 1), normal((rows, D), TYPES[kind], 2)
+    weight = normal((1, D), torch.float32, 3)[0].contiguous()
+    _, mean, rstd = pqt.pqt_layer_norm(x, weight)
+    dx, dweight, dbias = pqt.pqt_layer_norm_gradient(grad, x, weight, mean, rstd)
+    X, G, W, M, R = (t.double().cpu() for t in (x, grad, weight, mean, rstd))
+    h = (X - M[:, None]) * R[:, None]
+    # a term of dweight is the product of grad and of a difference times rstd: 3 u, and u a sum
+    within(dweight, (G * h).sum(0), (G * h).abs().sum(0) * (rows + 4) * U + (G.abs() * (M.abs() * R)[:, None]).sum(0) * U, "dweight")
+    within(dbias, G.sum(0), G.abs().sum(0) * (rows + 1) * U, "dbias")
+    g = G * W
+    s1, s2 = g.mean(1, keepdim=True), (g * h).mean(1, keepdim=True)
+    size = g.abs() + g.abs().mean(1, keepdim=True) + h.abs() * (g * h).abs().mean(1, keepdim=True)
+    within(dx, R[:, None] * (g - s1 - h * s2), R[:, None] * size * (D + 16) * U, "dx")
+    again = pqt.pqt_layer_norm_gradient(grad, x, weight, mean, rstd)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dweight) and torch.equal(again[2], dbias)
