@@ -571,7 +571,7 @@ def _blocks(name, b):
     codes, scales, cols = b
     kb = -(-cols // PQT_BLOCK)
     rows = codes.shape[0]
-    if codes.dtype != torch.float8_e4m3fn or scales.dtype != torch.uint8 or not codes.is_cuda or scales.device != codes.device or \
+    if codes.dtype is not torch.float8_e4m3fn or scales.dtype is not torch.uint8 or not codes.is_cuda or scales.get_device() != codes.get_device() or \
             codes.shape != (rows, kb * PQT_BLOCK) or scales.shape != (rows, kb) or not codes.is_contiguous() or not scales.is_contiguous():
         raise ValueError(f"{name} must be Blocks: contiguous float8_e4m3fn codes (rows, {kb * PQT_BLOCK}) and uint8 scales (rows, {kb}) "
                          f"for {cols} columns")
@@ -601,17 +601,19 @@ def pqt_block_product(a, b, bias=None, out=None, out_dtype=torch.bfloat16, strea
         with torch.cuda.stream(stream):
             return pqt_block_product(a, b, bias, out, out_dtype)
     m, n = _blocks("a", a), _blocks("b", b)
-    device = a.codes.device
-    if a.cols != b.cols:
-        raise ValueError(f"a has {a.cols} columns, b {b.cols}")
-    if b.codes.device != device:
-        raise ValueError(f"b is on {b.codes.device}, expected {device}")
+    (codes, scales, k), (b_codes, b_scales, b_k) = a, b
+    device = codes.device
+    if k != b_k:
+        raise ValueError(f"a has {k} columns, b {b_k}")
+    if b_codes.get_device() != codes.get_device():
+        raise ValueError(f"b is on {b_codes.device}, expected {device}")
     bptr = _vector("bias", bias, n, _FLOATS, device)
     out, optr, okind, ostep = _result(out, (m, n), out_dtype, device, False)
-    nbytes = _lib.pqt_block_product_workspace(m, n, a.cols)
+    nbytes = _lib.pqt_block_product_workspace(m, n, k)
     ws = _workspace(nbytes, device)
-    _check(_lib.pqt_block_product(a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), m, n, a.cols, bptr,
-                                  optr, okind, ostep, ws.data_ptr() if nbytes else None, nbytes, device.index, _current(device.index)))
+    gpu = device.index
+    _check(_lib.pqt_block_product(codes.data_ptr(), scales.data_ptr(), b_codes.data_ptr(), b_scales.data_ptr(), m, n, k, bptr, optr, okind, ostep,
+                                  ws.data_ptr() if nbytes else None, nbytes, gpu, _current(gpu)))
     return out
 
 
