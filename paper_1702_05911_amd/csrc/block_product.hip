@@ -447,6 +447,7 @@ __global__ __launch_bounds__(256, 1) void product_wide_kernel(ProductArgs g) {
         }
     }
     __syncthreads();
+    const bool stream = (double)g.m * g.n * sizeof(TY) > kStreamBytes;
     const int unit = tid & 31, have = min(8, g.n - n0 - unit * 8);
     if (have <= 0) return;
 #pragma unroll 1
@@ -458,7 +459,7 @@ __global__ __launch_bounds__(256, 1) void product_wide_kernel(ProductArgs g) {
             if (row < g.m) {
                 const TY* from = reinterpret_cast<const TY*>(half + r * (2 * B) + ((unit ^ (r & 15)) << 4));
                 TY* dst = static_cast<TY*>(g.out) + (int64_t)row * g.out_stride + n0 + unit * 8;
-                if (have == 8) *reinterpret_cast<typename Piece_<TY, 8>::type*>(dst) = *reinterpret_cast<const typename Piece_<TY, 8>::type*>(from);
+                if (have == 8) store_vector(reinterpret_cast<typename Piece_<TY, 8>::type*>(dst), *reinterpret_cast<const typename Piece_<TY, 8>::type*>(from), stream);
                 else
                     for (int e = 0; e < have; ++e) dst[e] = from[e];
             }

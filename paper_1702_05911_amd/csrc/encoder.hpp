@@ -69,9 +69,11 @@ __device__ __forceinline__ typename Floats<N>::type load_piece(const T* p, int h
     return out;
 }
 
-// The embedding's results of more bytes than the eight XCDs' L2 hold are stored past it, so that they do not push out what is still to be read (a
-// lookup of 100,003 x 1,024 floats takes 82 us so and 122 otherwise); smaller ones stay for whoever reads them next.  (Layer norm, which
-// reads its input once, is slower that way: 49 us for 46.)
+// Results of more bytes than the eight XCDs' L2 hold are stored past it by lookups, layer norm and the wide products, so that they do not push out what is still
+// to be read, nor are written back in the next kernel's time (a lookup of 100,003 x 1,024 floats takes 82 us so and 122 otherwise; calls of
+// layer norm over 65,537 x 960 follow each other in 48.8 us and in 53.3, though one alone takes 49 and 46; cutting and product of
+// 16,384 x 4,096 x 4,096 in 263 and 266); smaller ones stay for
+// whoever reads them next.  (Not the layer norm's gradient, which reads twice what it writes: 92 us so, 90 otherwise.)
 constexpr double kStreamBytes = 32.0 * (1 << 20);
 template <typename V>
 __device__ __forceinline__ void store_vector(V* p, V v, bool stream) {
@@ -83,10 +85,10 @@ __device__ __forceinline__ void store_vector(V* p, V v, bool stream) {
 }
 
 template <typename T, int N>
-__device__ __forceinline__ void store_piece(T* p, typename Floats<N>::type v, int have) {
+__device__ __forceinline__ void store_piece(T* p, typename Floats<N>::type v, int have, bool stream = false) {
     typedef typename Piece_<T, N>::type V;
     if (have >= N) {
-        *reinterpret_cast<V*>(p) = __builtin_convertvector(v, V);
+        store_vector(reinterpret_cast<V*>(p), __builtin_convertvector(v, V), stream);
         return;
     }
 #pragma unroll

@@ -12,7 +12,7 @@
 // the input).  Longer rows than one_pass_values() take a kernel for dx and one for the sums.
 // In both the next row's values are on their way, as they are, while one is worked on.
 //
-// Measured (a large copy moves 5.1 TB/s): forward 65,537 x 960 bf16 46 us, 5.5 TB/s; 10,000 x 128 floats 4.8 us.  Backward 16,384 x 4,096 bf16
+// Measured (a large copy moves 5.1 TB/s): forward 65,537 x 960 bf16 49 us, 5.2 TB/s; 10,000 x 128 floats 4.5 us.  Backward 16,384 x 4,096 bf16
 // 90 us and 6 for the rows of sums, 4.2 TB/s; 4,097 x 1,000 10 and 6 us (1,024 threads a workgroup, registers that spill: 145).
 #include <algorithm>
 
@@ -45,7 +45,7 @@ struct NormArgs {
     float* dweight;                        // ... these (either may be null)
     float* dbias;
     int64_t rows, x_stride, grad_stride, out_stride;
-    int D, param_type, want_parts;
+    int D, param_type, want_parts, stream;
     float eps;
 };
 
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_kernel(NormArgs 
                 const int c = (p * G + l) * kNormE;
                 const f32x8 wp = kKeep ? w[kKeep ? p : 0] : param_piece(g.weight, g.param_type, c, have[p], 1.0f);
                 const f32x8 bp = kKeep ? b[kKeep ? p : 0] : param_piece(g.bias, g.param_type, c, have[p], 0.0f);
-                store_piece<TY, kNormE>(dst + c, x[p] * rstd * wp + bp, have[p]);
+                store_piece<TY, kNormE>(dst + c, x[p] * rstd * wp + bp, have[p], g.stream);
             }
         if (l == 0) {
             if (g.mean) g.mean[r] = mean;
@@ -414,6 +414,7 @@ int pqt_layer_norm(const void* x, int type, int64_t rows, int64_t D, int64_t x_s
     g.rows = rows;
     g.x_stride = x_stride;
     g.out_stride = y_stride;
+    g.stream = (double)rows * D * type_bytes(out_type) > kStreamBytes;
     g.D = (int)D;
     g.param_type = param_type;
     g.eps = eps;
