@@ -577,6 +577,9 @@ __global__ __launch_bounds__(NT) void few_places_kernel(FewArgs f) {
     finish_row<TY, E>(g, (uint32_t)v, own, sum);
 }
 
+// The workspace is asked for above kNoWorkspace places, whichever kernels these take: what a caller keeps room for hangs on sizes only, not on where
+// one way turns out faster than the other.
+constexpr int64_t kNoWorkspace = 512;
 bool few_places(int64_t n, int64_t D) { return n <= kFewPlaces && n * ((D + kWave * kSumE - 1) / (kWave * kSumE)) <= kFewBlocks; }
 
 // Places of a chunk: about 2,048 groups' worth, at least 16 so that few tokens are in parts, at most 256
@@ -656,7 +659,7 @@ int pqt_embed(const void* table, int type, int64_t V, int64_t D, int64_t table_s
 }
 
 size_t pqt_embed_gradient_workspace(int64_t n, int64_t V, int64_t D) {
-    if (n < 1 || V < 1 || D < 1 || pqt::few_places(n, D) || n > pqt::kMaxPlaces || V > pqt::kMaxRows || D > pqt::kMaxEmbedD) return 0;
+    if (n < 1 || V < 1 || D < 1 || (n <= pqt::kNoWorkspace && pqt::few_places(n, D)) || n > pqt::kMaxPlaces || V > pqt::kMaxRows || D > pqt::kMaxEmbedD) return 0;
     return pqt::gradient_space(n, D).total;
 }
 
@@ -674,7 +677,7 @@ int pqt_embed_gradient(const void* grad, int grad_type, int64_t grad_stride, con
     if (!out || (n > 0 && (!grad || !tokens))) return fail(PQT_EINVAL, "pqt_embed_gradient: null pointer");
     if (!aligned_to(grad, type_bytes(grad_type)) || !aligned_to(out, type_bytes(out_type)) || !aligned_to(tokens, (size_t)token_bytes))
         return fail(PQT_EINVAL, "pqt_embed_gradient: a pointer is not aligned to its element");
-    const GradientSpace s = n > 0 && !few_places(n, D) ? gradient_space(n, D) : GradientSpace{};
+    const GradientSpace s = n > 0 && (n > kNoWorkspace || !few_places(n, D)) ? gradient_space(n, D) : GradientSpace{};
     if (s.total && (!workspace || workspace_bytes < s.total || !aligned_to(workspace, 16)))
         return fail(PQT_EINVAL, "pqt_embed_gradient: workspace of %zu bytes, aligned to 16, needed (%zu given)", s.total, workspace_bytes);
     const int log_lanes = log_lanes_for((D + kSumE - 1) / kSumE);

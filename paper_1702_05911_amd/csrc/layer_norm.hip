@@ -362,7 +362,7 @@ void with_gradient_shape(int64_t D, F&& f) {
 }
 
 // Workgroups of the backward kernel.  A single one for up to two rows a group: its sums are the result, without a second launch (8 x 1,000 bf16
-// 4.6 us in a graph, by two launches 6.3; 11.7 and 16.0 from Python.  Four rows a group: 32 x 1,000 7.9 and 6.5, 4 x 16,384 18.6 and 11.3).
+// 4.7 us in a graph, by two launches 6.3; 13.3 and 16.0 from Python.  Four rows a group: 32 x 1,000 7.9 and 6.5, 4 x 16,384 18.6 and 11.3).
 constexpr int kAloneRows = 2;
 unsigned gradient_blocks(int64_t rows, int groups) {
     return rows <= (int64_t)kAloneRows * groups ? 1u : (unsigned)std::min<int64_t>((rows + groups - 1) / groups, kGradBlocks);
@@ -372,12 +372,6 @@ unsigned gradient_blocks(int64_t rows, int64_t D, int type) {
     if (D > one_pass_values(type)) return (unsigned)std::min<int64_t>(rows, kLongParts);
     with_gradient_shape(D, [&](auto G, auto) { n = gradient_blocks(rows, kGradThreads / G.value); });
     return n;
-}
-
-// rows of partial sums
-unsigned gradient_parts(int64_t rows, int64_t D, int type) {
-    const unsigned n = gradient_blocks(rows, D, type);
-    return n == 1 && D <= one_pass_values(type) ? 0 : n;
 }
 
 }  // namespace
@@ -434,7 +428,7 @@ int pqt_layer_norm(const void* x, int type, int64_t rows, int64_t D, int64_t x_s
 
 size_t pqt_layer_norm_gradient_workspace(int64_t rows, int64_t D) {
     if (rows < 1 || D < 1 || D > pqt::kMaxNormD) return 0;
-    return (size_t)std::max(pqt::gradient_parts(rows, D, PQT_F32), pqt::gradient_parts(rows, D, PQT_BF16)) * 2 * (size_t)D * sizeof(float);
+    return (size_t)std::max(pqt::gradient_blocks(rows, D, PQT_F32), pqt::gradient_blocks(rows, D, PQT_BF16)) * 2 * (size_t)D * sizeof(float);
 }
 
 int pqt_layer_norm_gradient(const void* grad, int64_t grad_stride, const void* x, int64_t x_stride, int type, int64_t rows,
@@ -468,7 +462,7 @@ int pqt_layer_norm_gradient(const void* grad, int64_t grad_stride, const void* x
     g.out = dx;
     g.mean = const_cast<float*>(mean);
     g.rstd = const_cast<float*>(rstd);
-    const bool alone = rows > 0 && gradient_parts(rows, D, type) == 0;
+    const bool alone = rows > 0 && D <= one_pass_values(type) && gradient_blocks(rows, D, type) == 1;      // (asked for room all the same: that hangs on sizes only)
     g.parts = alone ? nullptr : static_cast<float*>(workspace);
     g.dweight = dweight;
     g.dbias = dbias;
