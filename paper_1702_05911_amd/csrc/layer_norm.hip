@@ -61,6 +61,16 @@ __device__ __forceinline__ f32x8 param_piece(const void* p, int type, int c, int
     return load_piece<Half, kNormE>(static_cast<const Half*>(p) + c, have);
 }
 
+// Zeros past a row's end, whatever stands there: (0 - mean) * rstd may leave fp32, and its product with a gradient of zero is NaN then.
+__device__ __forceinline__ f32x8 up_to(f32x8 v, int have) {
+    if (have < kNormE) {
+        asm("" : "+v"(have));                  // (eight comparisons here, not their results kept in scalar registers over all rows)
+#pragma unroll
+        for (int j = 0; j < kNormE; ++j) v[j] = j < have ? v[j] : 0.0f;
+    }
+    return v;
+}
+
 __device__ __forceinline__ float sum8(f32x8 v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 
 // Sum over a group of G lanes; G > 64: over G / 64 wavefronts of a workgroup of whole groups, all of which call it (scratch: one value a
@@ -195,14 +205,14 @@ __global__ __launch_bounds__(kGradThreads) void layer_norm_gradient_kernel(NormA
         f32x8 h[NP], y[NP];
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            h[p] = (__builtin_convertvector(next_x[p], f32x8) - mean) * rstd;
+            h[p] = up_to((__builtin_convertvector(next_x[p], f32x8) - mean) * rstd, have[p]);
             y[p] = __builtin_convertvector(next_y[p], f32x8);
         }
         fetch(r + step);                                       // on its way while this row is worked on
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            dw[p] = dw[p] + y[p] * h[p];                       // (past the row's end grad is zero, and what h is there counts for nothing)
+            dw[p] = dw[p] + y[p] * h[p];
             db[p] = db[p] + y[p];
             y[p] = y[p] * w[p];
             s1 += sum8(y[p]);
@@ -273,7 +283,7 @@ __global__ __launch_bounds__(kGradThreads) void long_gradient_kernel(NormArgs g)
             const int have = min(kNormE, g.D - c);
             const f32x8 y = load_piece<T, kNormE>(gs + c, have) * param_piece(g.weight, g.param_type, c, have, 1.0f);
             s1 += sum8(y);
-            s2 += sum8(y * ((load_piece<T, kNormE>(xs + c, have) - mean) * rstd));
+            s2 += sum8(y * up_to((load_piece<T, kNormE>(xs + c, have) - mean) * rstd, have));
         }
         s1 = row_sum<kGradThreads>(s1, scratch, turn) / D;
         s2 = row_sum<kGradThreads>(s2, scratch, turn) / D;

@@ -769,3 +769,17 @@ def test_layer_norm_gradient_of_few_rows(rows, D, kind):
     within(dx, R[:, None] * (g - s1 - h * s2), R[:, None] * size * (D + 16) * U, "dx")
     again = pqt.pqt_layer_norm_gradient(grad, x, weight, mean, rstd)
     assert torch.equal(again[0], dx) and torch.equal(again[1], dweight) and torch.equal(again[2], dbias)
+
+
+@gpu
+@pytest.mark.parametrize("rows,D,kind", [(3, 1, "f32"), (2, 33, "f32"), (3, 100, "bf16"), (5, 1000, "f32"), (2, 2049, "bf16"), (3, 5000, "f32"), (2, 8201, "f32"), (2, 16385, "bf16")])
+def test_layer_norm_gradient_of_equal_large_values(rows, D, kind):
+    """Rows of one value, 2^121, with an rstd of 2^20: mean * rstd is beyond fp32, every h of the row is 0, and no value is anything but finite."""
+    x = torch.full((rows, D), 2.0 ** 121, device=dev()).to(TYPES[kind])
+    grad, w = normal((rows, D), TYPES[kind], 1), normal((1, D), torch.float32, 2)[0].contiguous()
+    mean, rstd = torch.full((rows,), 2.0 ** 121, device=dev()), torch.full((rows,), 2.0 ** 20, device=dev())
+    dx, dw, db = pqt.pqt_layer_norm_gradient(grad, x, w, mean, rstd)
+    wx, tx, ww, tw, wb, tb = norm_gradient_reference(grad, x, w, mean, rstd)
+    within(dx, wx, tx, "dx")
+    within(dw, ww, tw, "dweight")
+    within(db, wb, tb, "dbias")
