@@ -451,9 +451,10 @@ int pqt_layer_norm_gradient(const void* grad, int64_t grad_stride, const void* x
  * input's checkpoint in half the bytes.
  *
  * pqt_block_product -- out[i][j] = bias[j] + sum over k of A[i][k] * B[j][k], A an m x k matrix and B an n x k matrix in
- * 8-bit blocks, sums fp32; bias: n fp32 values or NULL; out m x n of `out_type`.  fp32 results are those of fp32 additions; for 16-bit ones
- * a product may lose what lies below 2^-13 of the largest of eight neighbouring products (2^-10 of the sum of |A B| at
- * most; 1.4e-5 of the result's size on normal data, far below its rounding).  Values below 2^-126 may count as zero.  With x (m x k) and weights w
+ * 8-bit blocks, sums fp32; bias: n fp32 values or NULL; out m x n of `out_type`.  fp32 and f16 results are those of fp32 additions; for bf16 ones
+ * a product may lose what lies below 2^-13 of the largest of eight neighbouring products: 2^-10 of the sum of |A B| at
+ * most, 1.4e-5 of the result's usual size on normal data, where rounding to bf16 takes 1.7e-3.  That is more than the rounding of a single result which is
+ * far smaller than the others because its terms cancel; a caller to whom those matter takes fp32 or f16 results, at about half the rate.  Values below 2^-126 may count as zero.  With x (m x k) and weights w
  * (n x k) in blocks: y = x w^T; dx = g w is the product of g's blocks with those of w's transpose; dw = g^T x that of the blocks
  * of g's transpose with those of x's.  m and n below 2^28, k from 1 to 2^22.
  */

@@ -1,16 +1,17 @@
 // Products of matrices in 8-bit blocks: out[i][j] = bias[j] + sum over k of A[i][k] B[j][k], where 128 consecutive k share a scale.
 //
-// Results of 16 bits: the scaled matrix instruction v_mfma_scale_f32_16x16x128_f8f6f4 contracts one block of 128 at a time and multiplies by both
+// bf16 results: the scaled matrix instruction v_mfma_scale_f32_16x16x128_f8f6f4 contracts one block of 128 at a time and multiplies by both
 // scales itself (a byte exponent for every row and 32 values: the four of a block are the same), so that the sums stay in its
 // accumulators from the first block to the last, in fp32.  B's rows are its first operand: a lane then holds four
 // consecutive columns of the result.
 //
-// fp32 results: that instruction keeps of each product only what reaches 2^-13 of the largest of eight neighbouring products (measured:
-// 1.4e-5 of the result's size on normal data; bf16 results lose 500 times as much when they are rounded).  So the codes become bf16
+// fp32 and f16 results: that instruction keeps of each product only what reaches 2^-13 of the largest of eight neighbouring products (measured,
+// of the result's size: 1.4e-5 on normal data, 5.5e-5 where a few inputs are twenty times as large as the others; rounding to bf16 takes 1.7e-3, to
+// f16 2.1e-4, so that f16 results came out up to 1.3 times as far off as their type makes them).  So the codes become bf16
 // numbers under their scale, which loses nothing, and the bf16 instruction multiplies them, at half the rate; its sums are fp32 ones (9e-9).
 //
 // Three kernels, by the size of the result (plan_of):
-//   wide   256 x 256 a workgroup of four wavefronts, one a SIMD, 128 x 128 each: half the bytes from LDS per multiplication of smaller ones
+//   wide   (bf16 results) 256 x 256 a workgroup of four wavefronts, one a SIMD, 128 x 128 each: half the bytes from LDS per multiplication of smaller ones
 //   tile   128 x 128 or 64 x 64 a workgroup, two or four workgroups a compute unit; where there are few tiles, the blocks of k are shared
 //          out over several workgroups, whose sums go to the workspace and are joined in order
 //   few    up to 16 rows of A: B goes straight to registers, a wavefront has 16 of its rows, the wavefronts of a workgroup share out k
@@ -170,11 +171,11 @@ __device__ __forceinline__ void store_result(const ProductArgs& g, int row, int 
 
 // ---- tile -----------------------------------------------------------------------------------------------------------
 // Four wavefronts, each a quarter of the tile.  A block of k is multiplied while the next is on its way; with two to four workgroups a
-// compute unit others multiply while this one waits.  fp32 results: half of the rate of the bf16 instructions (8192 x 8192 x 8192 1.2 PFLOP/s);
+// compute unit others multiply while this one waits.  fp32 and f16 results: half of the rate of the bf16 instructions (8192 x 8192 x 8192 1.2 PFLOP/s);
 // the conversions, two a multiplication, hide beside them, the waits of a step do not.
 template <typename TY, int B>
 __global__ __launch_bounds__(256, B == 128 ? 2 : 4) void product_tile_kernel(ProductArgs g) {
-    constexpr bool kExact = sizeof(TY) == 4;
+    constexpr bool kExact = !std::is_same_v<TY, Bf16>;
     constexpr int F = B / 32, kLoads = B / 32;                  // fragments of a wavefront and loads of a lane, either side
     __shared__ __align__(16) uint8_t even[2 * B * kBlock];
     __shared__ __align__(16) uint8_t odd[2 * B * kBlock];
@@ -284,8 +285,8 @@ __global__ __launch_bounds__(256, B == 128 ? 2 : 4) void product_tile_kernel(Pro
 // 4.0 on such data (its clock falls), with wavefronts of 64 x 128, two a SIMD, whose fragments take all of LDS's rate, 1.9.  A block of k
 // takes 1.26 us, the first loads and the result of a tile 14, in which nothing is multiplied: tiles in one long-lived workgroup with stores
 // straight from the registers were slower (249), as their sums did not stay in registers.
-template <typename TY>
 __global__ __launch_bounds__(256, 1) void product_wide_kernel(ProductArgs g) {
+    typedef Bf16 TY;
     constexpr int B = 256, F = 8, kHalf = B * kBlock;
     __shared__ __align__(16) uint8_t lo_even[kHalf];
     __shared__ __align__(16) uint8_t hi_even[kHalf];
@@ -489,7 +490,7 @@ constexpr int kFewRows = 16, kFewWaves = 8, kFewRun = 4;
 // round of loads, whose latency it is); 16 x 32768 x 4096 24.6, 5.5 TB/s (NF = 1: 35.1).
 template <typename TY, int NF>
 __global__ __launch_bounds__(kFewWaves * kWave) void product_few_kernel(ProductArgs g) {
-    constexpr bool kExact = sizeof(TY) == 4;
+    constexpr bool kExact = !std::is_same_v<TY, Bf16>;
     __shared__ f32x4 sums[kFewWaves][NF][kWave];
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), fr = lane & 15, q = lane >> 4;
     const int n0 = blockIdx.x * (16 * NF);
@@ -549,7 +550,7 @@ constexpr int64_t kManyColumns = 32768;    // of a result of few rows: two workg
 // more workgroup on it adds, how many fit, and what a call costs before and after (us).
 //   wide   2.9 PFLOP/s where there are many tiles; one tile alone takes 14 us before and after its steps
 //   bf16 results   128: 8191 x 960 x 2000 27.7 (64: 38.9, wide 31.2), 2048^3 18.2 (21.9, 28.9);  64: 1000^3 6.2 (128: 10.2), 10000 x 128 x 1000 7.8 (10.4)
-//   fp32 results   128: 8191 x 960 x 2000 39.6 (64: 50.9);  64: 1000^3 7.9 (13.4)
+//   fp32 results (and f16, by the same instructions)   128: 8191 x 960 x 2000 39.6 (64: 50.9);  64: 1000^3 7.9 (13.4)
 //   shared out     960 x 2000 x 8191 by four 35.4 (57.5 whole, 64: 40.8), fp32 48.0 (83.8, 59.2);  512 x 512 x 8192 on 64 by eight 14.3 (30.6)
 struct Cost { double step, more, fit, around; };
 double time_of(const Cost& c, double tiles, int steps, int splits, double results) {
@@ -617,7 +618,7 @@ int pqt_block_product(const uint8_t* a_codes, const uint8_t* a_scales, const uin
     if (need && (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)))
         return fail(PQT_EINVAL, "pqt_block_product: workspace of %zu bytes, aligned to 16, needed (%zu given)", need, workspace_bytes);
     const int kb = (int)((k + kBlock - 1) / kBlock);
-    const Plan p = plan_of(m, n, kb, out_type == PQT_F32);
+    const Plan p = plan_of(m, n, kb, out_type != PQT_BF16);
     if ((int64_t)p.tiles_m * p.tiles_n > kMaxTiles)
         return fail(PQT_EUNSUPPORTED, "pqt_block_product: %d x %d tiles", p.tiles_m, p.tiles_n);
     if (const int rc = check_device(device, "pqt_block_product")) return rc;
@@ -633,7 +634,7 @@ int pqt_block_product(const uint8_t* a_codes, const uint8_t* a_scales, const uin
         else if (p.tile == 16) hipLaunchKernelGGL((product_few_kernel<TY, 1>), dim3((unsigned)((n + 15) / 16)), dim3(kFewWaves * kWave), 0, st, g);
         else if (p.tile == 64) hipLaunchKernelGGL((product_tile_kernel<TY, 64>), grid, dim3(256), 0, st, g);
         else if (p.tile == 128) hipLaunchKernelGGL((product_tile_kernel<TY, 128>), grid, dim3(256), 0, st, g);
-        else if constexpr (sizeof(TY) == 2) hipLaunchKernelGGL((product_wide_kernel<TY>), grid, dim3(256), 0, st, g);
+        else if constexpr (std::is_same_v<TY, Bf16>) hipLaunchKernelGGL(product_wide_kernel, grid, dim3(256), 0, st, g);
     });
     HIP_TRY(hipGetLastError());
     if (p.splits > 1) {

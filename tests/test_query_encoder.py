@@ -783,3 +783,25 @@ def test_layer_norm_gradient_of_equal_large_values(rows, D, kind):
     within(dx, wx, tx, "dx")
     within(dw, ww, tw, "dweight")
     within(db, wb, tb, "dbias")
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k,bias", [(1, 900, 1000, True), (16, 33_000, 300, False), (40, 70, 513, True), (300, 1000, 4000, False), (700, 40, 8193, True),
+                                        (1301, 1270, 8190, False), (4500, 4001, 1100, True)])
+def test_block_product_f16_sums(m, n, k, bias):
+    """f16 results are fp32 sums, rounded once.  A few inputs are many times as large as their neighbours, as activations have them."""
+    x, w = normal((m, k), torch.float32, m + k), normal((n, k), torch.float32, n + k + 1, 0, 0.1 / k ** 0.5)
+    x[:, ::61] *= 20.0
+    w[:, ::97] *= 20.0
+    a, b = pqt.pqt_block_quantize(x), pqt.pqt_block_quantize(w)
+    v = normal((1, n), torch.float32, 5)[0].contiguous() if bias else None
+    got = pqt.pqt_block_product(a, b, bias=v, out_dtype=torch.float16)
+    A, B = stand_for(a), stand_for(b)
+    want = torch.from_numpy(A @ B.T)
+    # an instruction adds up 32 products, a wavefront's instructions follow each other, and up to 16 such sums are joined: additions that are each
+    # off by at most 2^-23 of a partial sum
+    tol = torch.from_numpy(np.abs(A) @ np.abs(B).T) * ((k / 32 + 48) * 2.0 ** -23)
+    if bias:
+        want = want + v.double().cpu()
+        tol = tol + U * (want.abs() + v.double().cpu().abs())
+    within(got, want, tol, "f16 product")
