@@ -449,6 +449,14 @@ def _same_device(device, **tensors):
             raise ValueError(f"{name} is on {t.device}, expected {device}")
 
 
+def _running_on(stream, *tensors):
+    """Makes `stream` the current one for a call on these tensors (None among them counts for nothing), which have to be on its GPU."""
+    for t in tensors:
+        if t is not None and t.device != stream.device:
+            raise ValueError(f"the stream is on {stream.device}, a tensor on {t.device}")
+    return torch.cuda.stream(stream)
+
+
 # The handle of the current stream of a GPU (torch.cuda.current_stream(device).cuda_stream, which makes an object first).  Every call below
 # runs on it; one that is given another stream makes that the current one, so that what it allocates belongs to it.
 _current = torch._C._cuda_getCurrentRawStream
@@ -484,7 +492,7 @@ def pqt_embed(table, tokens, scale=1.0, out=None, out_dtype=None, stream=None):
     """pqt_embed.  table: (V, D); tokens: (n,) int32 or int64.  Returns (n, D): scale * table[tokens], rows of zeros for
     tokens outside the table."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _running_on(stream, table, tokens, out):
             return pqt_embed(table, tokens, scale, out, out_dtype)
     ptr, kind, step = _matrix("table", table)
     V, D = table.shape
@@ -498,7 +506,7 @@ def pqt_embed(table, tokens, scale=1.0, out=None, out_dtype=None, stream=None):
 def pqt_embed_gradient(grad, tokens, V, scale=1.0, out=None, out_dtype=torch.float32, accumulate=False, stream=None):
     """pqt_embed_gradient.  grad: (n, D).  Returns (V, D): scale times the sum of every token's rows; accumulate adds it to `out`."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _running_on(stream, grad, tokens, out):
             return pqt_embed_gradient(grad, tokens, V, scale, out, out_dtype, accumulate)
     ptr, kind, step = _matrix("grad", grad)
     n, D = grad.shape
@@ -519,7 +527,7 @@ def pqt_embed_gradient(grad, tokens, V, scale=1.0, out=None, out_dtype=torch.flo
 def pqt_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, out_dtype=None, stream=None):
     """pqt_layer_norm.  x: (rows, D); weight, bias: (D,) of one type, or None.  Returns (y, mean, rstd)."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _running_on(stream, x, weight, bias, out):
             return pqt_layer_norm(x, weight, bias, eps, out, out_dtype)
     ptr, kind, step = _matrix("x", x)
     rows, D = x.shape
@@ -538,7 +546,7 @@ def pqt_layer_norm_gradient(grad, x, weight, mean, rstd, out=None, stream=None):
     """pqt_layer_norm_gradient.  grad, x: (rows, D) of one type; mean, rstd: what pqt_layer_norm returned.  Returns (dx, dweight,
     dbias), the last two float32."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _running_on(stream, grad, x, weight, mean, rstd, out):
             return pqt_layer_norm_gradient(grad, x, weight, mean, rstd, out)
     ptr, kind, step = _matrix("x", x)
     rows, D = x.shape
@@ -581,7 +589,7 @@ def _blocks(name, b):
 def pqt_block_quantize(x, rows=True, columns=False, stream=None):
     """pqt_block_quantize.  x: (r, c).  Returns the Blocks of x (rows), of its transpose (columns), or both as a pair."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _running_on(stream, x):
             return pqt_block_quantize(x, rows, columns)
     ptr, kind, step = _matrix("x", x)
     r, c = x.shape
@@ -600,7 +608,7 @@ def pqt_block_product(a, b, bias=None, out=None, out_dtype=torch.bfloat16, strea
     of out_dtype: float32 and float16 results are those of fp32 additions; bfloat16 ones take about half the time and lose products below
     2^-13 of the largest of eight neighbours."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _running_on(stream, *a[:2], *b[:2], bias, out):
             return pqt_block_product(a, b, bias, out, out_dtype)
     m, n = _blocks("a", a), _blocks("b", b)
     (codes, scales, k), (b_codes, b_scales, b_k) = a, b

@@ -5,6 +5,7 @@ Tolerances follow from the arithmetic, u = 2^-24 the unit of fp32: a sum of c te
 of their magnitudes, a product or a stored result by its type's unit.  What is exact (codes, scales, integer-valued products) is
 compared bit for bit."""
 import os
+import types
 
 import numpy as np
 import pytest
@@ -805,3 +806,14 @@ def test_block_product_f16_sums(m, n, k, bias):
         want = want + v.double().cpu()
         tol = tol + U * (want.abs() + v.double().cpu().abs())
     within(got, want, tol, "f16 product")
+
+
+def test_refusals_of_a_stream_of_another_gpu():
+    """A call on a stream of another GPU than the tensors' is refused, not run on some other stream."""
+    x, tok, blocks = torch.zeros((4, 8)), torch.zeros(4, dtype=torch.int64), pqt.Blocks(torch.zeros((4, 128)), torch.zeros((4, 1)), 8)
+    other = types.SimpleNamespace(device=torch.device("cuda", 7))
+    for call in (lambda **kw: pqt.pqt_embed(x, tok, **kw), lambda **kw: pqt.pqt_embed_gradient(x, tok, 5, **kw), lambda **kw: pqt.pqt_layer_norm(x, x[0], **kw),
+                 lambda **kw: pqt.pqt_layer_norm_gradient(x, x, None, x[:, 0], x[:, 0], **kw), lambda **kw: pqt.pqt_block_quantize(x, **kw),
+                 lambda **kw: pqt.pqt_block_product(blocks, blocks, **kw)):
+        with pytest.raises(ValueError, match="the stream is on cuda:7"):
+            call(stream=other)
