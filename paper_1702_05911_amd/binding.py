@@ -450,15 +450,20 @@ def _same_device(device, **tensors):
 
 
 def _running_on(stream, *tensors):
-    """Makes `stream` the current one for a call on these tensors (None among them counts for nothing), which have to be on its GPU."""
+    """Makes `stream` the current one for a call on these tensors (None among them counts for nothing), which have to be on its GPU.  Their
+    memory is not handed out again before the stream is done with it, also where the caller drops one at once."""
+    tensors = [t for t in tensors if t is not None]
     for t in tensors:
-        if t is not None and t.device != stream.device:
+        if t.device != stream.device:
             raise ValueError(f"the stream is on {stream.device}, a tensor on {t.device}")
+    for t in tensors:
+        t.record_stream(stream)
     return torch.cuda.stream(stream)
 
 
 # The handle of the current stream of a GPU (torch.cuda.current_stream(device).cuda_stream, which makes an object first).  Every call below
-# runs on it; one that is given another stream makes that the current one, so that what it allocates belongs to it.
+# runs on it; one that is given another stream makes that the current one, so that what it allocates belongs to it (who uses a result on a
+# third stream waits for it there, and tells the allocator by record_stream, as with any tensor).
 _current = torch._C._cuda_getCurrentRawStream
 
 

@@ -817,3 +817,48 @@ def test_refusals_of_a_stream_of_another_gpu():
                  lambda **kw: pqt.pqt_block_product(blocks, blocks, **kw)):
         with pytest.raises(ValueError, match="the stream is on cuda:7"):
             call(stream=other)
+
+
+def test_inputs_of_a_call_on_another_stream_are_recorded():
+    recorded = []
+
+    class Tensor:
+        device = torch.device("cuda", 7)
+
+        def record_stream(self, stream):
+            recorded.append((self, stream))
+    stream, a, b = types.SimpleNamespace(device=torch.device("cuda", 7)), Tensor(), Tensor()
+    pqt._running_on(stream, a, None, b)
+    assert recorded == [(a, stream), (b, stream)]
+
+
+@gpu
+def test_inputs_dropped_after_a_call_on_another_stream_are_kept():
+    """Inputs that the caller drops at once are not handed out again while the other stream still has to read them."""
+    side, n, D = torch.cuda.Stream(), 3001, 640
+    grad, w = normal((n, D), torch.bfloat16, 1), torch.ones(D, device=dev())
+    _, mean, rstd = pqt.pqt_layer_norm(grad, w)
+    blocks = pqt.pqt_block_quantize(grad)
+    tok = some_tokens(n, 500, 1)
+    calls = [(tok, lambda t: pqt.pqt_embed(grad, t, stream=side)), (tok, lambda t: pqt.pqt_embed_gradient(grad, t, 500, stream=side)),
+             (grad, lambda t: pqt.pqt_embed(t, tok, stream=side)), (grad, lambda t: pqt.pqt_embed_gradient(t, tok, 500, stream=side)),
+             (grad, lambda t: pqt.pqt_layer_norm(t, w, stream=side)), (w, lambda t: pqt.pqt_layer_norm(grad, t, stream=side)),
+             (grad, lambda t: pqt.pqt_layer_norm_gradient(t, grad, w, mean, rstd, stream=side)), (rstd, lambda t: pqt.pqt_layer_norm_gradient(grad, grad, w, mean, t, stream=side)),
+             (grad, lambda t: pqt.pqt_block_quantize(t, columns=True, stream=side)),
+             (blocks.codes, lambda t: pqt.pqt_block_product(blocks._replace(codes=t), blocks, stream=side)),
+             (blocks.scales, lambda t: pqt.pqt_block_product(blocks, blocks._replace(scales=t), stream=side))]
+    busy = torch.zeros(4096, 4096, device=dev())
+    torch.cuda.synchronize()
+    for like, call in calls:
+        temporary = like.clone()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for _ in range(60):
+                busy = busy @ busy                                 # tens of milliseconds
+        call(temporary)
+        at = temporary.data_ptr()
+        del temporary
+        others = [torch.empty_like(like) for _ in range(3)]
+        assert not side.query()
+        assert at not in [t.data_ptr() for t in others]
+        side.synchronize()
