@@ -508,8 +508,9 @@ def pqt_embed(table, tokens, scale=1.0, out=None, out_dtype=None, stream=None):
     return out
 
 
-def pqt_embed_gradient(grad, tokens, V, scale=1.0, out=None, out_dtype=torch.float32, accumulate=False, stream=None):
-    """pqt_embed_gradient.  grad: (n, D).  Returns (V, D): scale times the sum of every token's rows; accumulate adds it to `out`."""
+def pqt_embed_gradient(grad, tokens, V, scale=1.0, out=None, out_dtype=None, accumulate=False, stream=None):
+    """pqt_embed_gradient.  grad: (n, D).  Returns (V, D), of `out`'s type or out_dtype (float32): scale times the sum of every token's rows;
+    accumulate adds it to `out`."""
     if stream is not None:
         with _running_on(stream, grad, tokens, out):
             return pqt_embed_gradient(grad, tokens, V, scale, out, out_dtype, accumulate)
@@ -521,7 +522,7 @@ def pqt_embed_gradient(grad, tokens, V, scale=1.0, out=None, out_dtype=torch.flo
         raise ValueError(f"{nt} tokens for {n} rows")
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
-    out, optr, okind, ostep = _result(out, (V, D), out_dtype, device, False)
+    out, optr, okind, ostep = _result(out, (V, D), out_dtype or torch.float32, device, out_dtype is not None)
     nbytes = _lib.pqt_embed_gradient_workspace(n, V, D)
     ws = _workspace(nbytes, device)
     _check(_lib.pqt_embed_gradient(ptr, kind, step, tok, size, n, V, D, scale, 1 if accumulate else 0, optr, okind, ostep,
@@ -608,9 +609,9 @@ def pqt_block_quantize(x, rows=True, columns=False, stream=None):
     return (a, t) if rows and columns else a if rows else t
 
 
-def pqt_block_product(a, b, bias=None, out=None, out_dtype=torch.bfloat16, stream=None):
+def pqt_block_product(a, b, bias=None, out=None, out_dtype=None, stream=None):
     """pqt_block_product.  a, b: Blocks of m x k and n x k values; bias: (n,) float32 or None.  Returns (m, n): a b^T + bias,
-    of out_dtype: float32 and float16 results are those of fp32 additions; bfloat16 ones take about half the time and lose products below
+    of `out`'s type or out_dtype (bfloat16): float32 and float16 results are those of fp32 additions; bfloat16 ones take about half the time and lose products below
     2^-13 of the largest of eight neighbours."""
     if stream is not None:
         with _running_on(stream, *a[:2], *b[:2], bias, out):
@@ -623,7 +624,7 @@ def pqt_block_product(a, b, bias=None, out=None, out_dtype=torch.bfloat16, strea
     if b_codes.get_device() != codes.get_device():
         raise ValueError(f"b is on {b_codes.device}, expected {device}")
     bptr = _vector("bias", bias, n, _FLOATS, device)
-    out, optr, okind, ostep = _result(out, (m, n), out_dtype, device, False)
+    out, optr, okind, ostep = _result(out, (m, n), out_dtype or torch.bfloat16, device, out_dtype is not None)
     nbytes = _lib.pqt_block_product_workspace(m, n, k)
     ws = _workspace(nbytes, device)
     gpu = device.index

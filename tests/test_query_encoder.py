@@ -862,3 +862,19 @@ def test_inputs_dropped_after_a_call_on_another_stream_are_kept():
         assert not side.query()
         assert at not in [t.data_ptr() for t in others]
         side.synchronize()
+
+
+@gpu
+def test_refusals_of_an_out_of_another_type_than_out_dtype():
+    x, tok = torch.ones((4, 8), device=dev()), torch.zeros(4, dtype=torch.int64, device=dev())
+    blocks = pqt.pqt_block_quantize(x)
+    for shape, call in (((4, 8), lambda **kw: pqt.pqt_embed(x, tok, **kw)), ((5, 8), lambda **kw: pqt.pqt_embed_gradient(x, tok, 5, **kw)),
+                        ((4, 8), lambda **kw: pqt.pqt_layer_norm(x, **kw)[0]), ((4, 4), lambda **kw: pqt.pqt_block_product(blocks, blocks, **kw))):
+        for t in TYPES.values():
+            out = torch.zeros(shape, dtype=t, device=dev())
+            assert call(out=out) is out and call(out=out, out_dtype=t) is out
+            for other in TYPES.values():
+                if other != t:
+                    with pytest.raises(ValueError, match="out must be"):
+                        call(out=out, out_dtype=other)
+    assert pqt.pqt_embed_gradient(x, tok, 5).dtype == torch.float32 and pqt.pqt_block_product(blocks, blocks).dtype == torch.bfloat16
