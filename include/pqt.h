@@ -392,7 +392,7 @@ int pqt_measure_peaks(int device, double* hbm_read_gb_per_s, double* mfma_f32_tf
  *   - outputs must not overlap inputs; the same inputs give the same bytes;
  *   - errors: PQT_EINVAL (null or misaligned pointer, size or stride out of range, unknown type, workspace too small),
  *     PQT_EUNSUPPORTED (limits named below), PQT_EHIP.  Calls with no rows do nothing, except that sums over no rows are
- *     zero.
+ *     zero (products of no k are refused: an empty batch's weight gradient is the caller's to clear).
  */
 #define PQT_F32  0
 #define PQT_BF16 1

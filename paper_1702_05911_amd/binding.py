@@ -624,6 +624,10 @@ def pqt_block_product(a, b, bias=None, out=None, out_dtype=None, stream=None):
     if b_codes.get_device() != codes.get_device():
         raise ValueError(f"b is on {b_codes.device}, expected {device}")
     bptr = _vector("bias", bias, n, _FLOATS, device)
+    if k == 0:                                                     # a sum of nothing (the gradient of an empty batch): that of a block of zeros
+        codes, b_codes = (torch.zeros(rows, PQT_BLOCK, dtype=torch.uint8, device=device) for rows in (m, n))
+        scales, b_scales = (torch.ones(rows, 1, dtype=torch.uint8, device=device) for rows in (m, n))
+        k = 1
     out, optr, okind, ostep = _result(out, (m, n), out_dtype or torch.bfloat16, device, out_dtype is not None)
     nbytes = _lib.pqt_block_product_workspace(m, n, k)
     ws = _workspace(nbytes, device)

@@ -878,3 +878,35 @@ def test_refusals_of_an_out_of_another_type_than_out_dtype():
                     with pytest.raises(ValueError, match="out must be"):
                         call(out=out, out_dtype=other)
     assert pqt.pqt_embed_gradient(x, tok, 5).dtype == torch.float32 and pqt.pqt_block_product(blocks, blocks).dtype == torch.bfloat16
+
+
+@gpu
+@pytest.mark.parametrize("m,n", [(40, 70), (1, 9), (200, 130), (0, 5), (3, 0)])
+def test_block_product_over_no_positions(m, n):
+    """The weight's gradient of an empty batch is zero; with a bias, a product over nothing is the bias."""
+    g, gt = pqt.pqt_block_quantize(torch.zeros((0, m), device=dev()), columns=True) if m else (None, None)
+    if not m:
+        gt = pqt.Blocks(torch.zeros((0, 0), dtype=torch.float8_e4m3fn, device=dev()), torch.zeros((0, 0), dtype=torch.uint8, device=dev()), 0)
+    xt = pqt.pqt_block_quantize(torch.zeros((0, n), device=dev()), rows=False, columns=True) if n else gt._replace(codes=gt.codes[:0], scales=gt.scales[:0])
+    for kind in TYPES.values():
+        view, check = guarded(m, n, kind)
+        assert pqt.pqt_block_product(gt, xt, out=view) is view
+        assert not bool(view.any())
+        check()
+        bias = normal((1, max(n, 1)), torch.float32, 3)[0][:n].contiguous()
+        assert torch.equal(pqt.pqt_block_product(gt, xt, bias=bias, out_dtype=kind), bias.to(kind).expand(m, n))
+
+
+@gpu
+def test_a_training_step_of_an_empty_batch():
+    """Every call of a step takes no rows: results without rows, and gradients of zeros."""
+    table, tok = normal((20, 48), torch.bfloat16, 1), torch.zeros(0, dtype=torch.int64, device=dev())
+    w, wt = pqt.pqt_block_quantize(normal((30, 48), torch.float32, 2), columns=True)
+    y, mean, rstd = pqt.pqt_layer_norm(pqt.pqt_embed(table, tok, 3.0))
+    a, at = pqt.pqt_block_quantize(y, columns=True)
+    out = pqt.pqt_block_product(a, w, bias=torch.ones(30, device=dev()), out_dtype=torch.float32)
+    g, gt = pqt.pqt_block_quantize(out, columns=True)
+    dx, dweight, dbias = pqt.pqt_layer_norm_gradient(pqt.pqt_block_product(g, wt), y, None, mean, rstd)
+    assert out.shape == (0, 30) and dx.shape == (0, 48)
+    for t, shape in ((pqt.pqt_block_product(gt, at, out_dtype=torch.float32), (30, 48)), (dweight, (48,)), (dbias, (48,)), (pqt.pqt_embed_gradient(dx, tok, 20), (20, 48))):
+        assert t.shape == shape and not bool(t.any())
