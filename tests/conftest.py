@@ -20,6 +20,32 @@ def pytest_terminal_summary(terminalreporter):
         terminalreporter.write_line("parity tolerance (1e-4 relative + floor): " + pu.STATS.summary())
 
 
+class LibraryWithoutGpu:
+    """The compiled library with GPU -1 in every call (the last argument but one): arguments are checked as ever, and a call that passes the
+    checks ends there, before anything could be launched on the addresses that it was given."""
+
+    def __init__(self, lib):
+        self._lib = lib
+
+    def __getattr__(self, name):
+        fn = getattr(self._lib, name)
+        return fn if name.endswith("_workspace") or name == "pqt_last_error" else lambda *args: fn(*args[:-2], -1, args[-1])
+
+
+@pytest.fixture
+def library_without_gpu(monkeypatch):
+    import paper_1702_05911_amd.binding as binding
+    monkeypatch.setattr(binding, "_lib", LibraryWithoutGpu(binding._lib))
+    return binding._lib
+
+
+@pytest.fixture(autouse=True)
+def made_up_addresses_stay_off_the_gpu(request):
+    """Refusals are tested with addresses that nobody may read.  Where a GPU is there, a check that is missing must not run a kernel on them."""
+    if request.node.name == "test_refusals_of_the_library":
+        request.getfixturevalue("library_without_gpu")
+
+
 @pytest.fixture(scope="session")
 def tiny():
     """Tiny workload: vectors, queries and an oracle-built index."""

@@ -910,3 +910,14 @@ def test_a_training_step_of_an_empty_batch():
     assert out.shape == (0, 30) and dx.shape == (0, 48)
     for t, shape in ((pqt.pqt_block_product(gt, at, out_dtype=torch.float32), (30, 48)), (dweight, (48,)), (dbias, (48,)), (pqt.pqt_embed_gradient(dx, tok, 20), (20, 48))):
         assert t.shape == shape and not bool(t.any())
+
+
+def test_refusals_launch_nothing(library_without_gpu):
+    """Calls whose arguments are all right (addresses made up), through the library that the refusals are tested with: each ends at its GPU."""
+    lib, p, far = library_without_gpu, 1 << 20, 1 << 40
+    assert pqt._lib is lib
+    for fn, args in ((lib.pqt_embed, (p, 0, 10, 8, 8, p, 8, 4, 1.0, p, 0, 8)), (lib.pqt_embed_gradient, (p, 1, 8, p, 4, 1000, 10, 8, 1.0, 0, p, 0, 8, p, far)),
+                     (lib.pqt_layer_norm, (p, 0, 4, 8, 8, p, p, 0, 1e-5, p, 0, 8, p, p)), (lib.pqt_layer_norm_gradient, (p, 8, p, 8, 0, 4, 8, p, 0, p, p, p, 8, p, p, p, far)),
+                     (lib.pqt_block_quantize, (p, 0, 4, 8, 8, p, p, p, p)), (lib.pqt_block_product, (p, p, p, p, 4, 8, 100, p, p, 0, 8, p, far))):
+        refused(fn, *args, 0, None, code=pqt.PQT_EHIP)
+        assert "GPU -1" in pqt.last_error()
