@@ -410,6 +410,8 @@ def pqt_measure_peaks(device=0):
 
 
 # ---- the query encoder's operators ---------------------------------------------------------------
+# None of them takes part in autograd: a result carries no graph, also where an input requires a gradient.  The backward pass is made of the
+# gradients' own calls (pqt_embed_gradient, pqt_layer_norm_gradient, pqt_block_product of transposed blocks), as examples/query_encoder.py does.
 PQT_F32, PQT_BF16, PQT_F16 = 0, 1, 2
 PQT_BLOCK = 128
 _TYPES = {torch.float32: PQT_F32, torch.bfloat16: PQT_BF16, torch.float16: PQT_F16}

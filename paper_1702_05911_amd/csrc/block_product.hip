@@ -281,7 +281,7 @@ __global__ __launch_bounds__(256, B == 128 ? 2 : 4) void product_tile_kernel(Pro
 //   first half   barrier; loads lo of k + 2; reads hi of k; multiplies A lo with B lo, then with B hi
 //   second half  barrier; loads hi of k + 2; reads lo of k + 1; multiplies A hi with B lo, then with B hi
 // so that a load has one and a half blocks of time, and 16 loads (of the two halves after it) may still be out when it is waited for.
-// 8192 x 8192 x 8192 2.9 PFLOP/s, 16384 x 4096 x 4096 2.5 (216 us by itself, 220 to 260 in a row of them); this card's instruction by itself
+// 8192 x 8192 x 8192 2.9 PFLOP/s, 16384 x 4096 x 4096 2.5 (216 us by itself, 220 behind the cutting of A, 263 at the median under a profiler); this card's instruction by itself
 // 4.0 on such data (its clock falls), with wavefronts of 64 x 128, two a SIMD, whose fragments take all of LDS's rate, 1.9.  A block of k
 // takes 1.26 us, the first loads and the result of a tile 14, in which nothing is multiplied: tiles in one long-lived workgroup with stores
 // straight from the registers were slower (249), as their sums did not stay in registers.
@@ -486,8 +486,9 @@ __global__ __launch_bounds__(256) void join_splits_kernel(ProductArgs g) {
 constexpr int kFewWaves = 8, kFewRun = 4;
 
 // A wavefront multiplies 16 NF rows of B with all of A's over every kFewWaves-th run of four blocks, all of whose loads are sent first; the sums
-// of the wavefronts are added in order.  Bound by the reading of B: 1 x 4096 x 4096 4.8 us with B in the caches, 6.8 from memory (2.5 TB/s: one
-// round of loads, whose latency it is); 16 x 32768 x 4096 24.6, 5.5 TB/s (NF = 1: 35.1).
+// of the wavefronts are added in order.  Bound by the reading of B: 1 x 4096 x 4096 4.8 us with B in the caches, 6.2 from memory (2.7 TB/s: one
+// round of loads, whose latency it is); 16 x 32768 x 4096 24.6 from the caches, 5.5 TB/s (NF = 1: 35.1), 37 from memory.  bf16 results by the
+// instructions of the others: 6.4, 38, and 4 x 40000 x 1000 16.7 for 14.5.
 template <typename TY, int NF>
 __global__ __launch_bounds__(kFewWaves * kWave) void product_few_kernel(ProductArgs g) {
     constexpr bool kExact = !std::is_same_v<TY, Bf16>;

@@ -577,8 +577,8 @@ __global__ __launch_bounds__(NT) void few_places_kernel(FewArgs f) {
     finish_row<TY, E>(g, (uint32_t)v, own, sum);
 }
 
-// The workspace is asked for above kNoWorkspace places, whichever kernels these take: what a caller keeps room for hangs on sizes only, not on where
-// one way turns out faster than the other.
+// Places that few_places() takes use no workspace.  Above kNoWorkspace of them one is asked for all the same: how much room a number of
+// places needs is part of the interface, and does not move with where one way turns out faster than the other.
 constexpr int64_t kNoWorkspace = 512;
 bool few_places(int64_t n, int64_t D) { return n <= kFewPlaces && n * ((D + kWave * kSumE - 1) / (kWave * kSumE)) <= kFewBlocks; }
 

@@ -73,7 +73,7 @@ __device__ __forceinline__ typename Floats<N>::type load_piece(const T* p, int h
 // to be read, nor are written back in the next kernel's time (a lookup of 100,003 x 1,024 floats takes 82 us so and 122 otherwise; calls of
 // layer norm over 65,537 x 960 follow each other in 48.8 us and in 53.3, though one alone takes 49 and 46; cutting and product of
 // 16,384 x 4,096 x 4,096 in 263 and 266); smaller ones stay for
-// whoever reads them next.  (Not the layer norm's gradient, which reads twice what it writes: 92 us so, 90 otherwise.)
+// whoever reads them next.  (Not the layer norm's gradient, which reads twice what it writes: 16,384 x 4,096 80 us a call either way.)
 constexpr double kStreamBytes = 32.0 * (1 << 20);
 template <typename V>
 __device__ __forceinline__ void store_vector(V* p, V v, bool stream) {

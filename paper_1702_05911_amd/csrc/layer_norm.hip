@@ -13,7 +13,8 @@
 // In both the next row's values are on their way, as they are, while one is worked on.
 //
 // Measured (a large copy moves 5.1 TB/s): forward 65,537 x 960 bf16 49 us, 5.2 TB/s; 10,000 x 128 floats 4.5 us.  Backward 16,384 x 4,096 bf16
-// 90 us and 6 for the rows of sums, 4.2 TB/s; 4,097 x 1,000 10 and 6 us (1,024 threads a workgroup, registers that spill: 145).
+// 76 us and 5 for the rows of sums, 5.0 TB/s; 4,097 x 1,000 10.8 and 3.9 us, two rows a wavefront: too little on its way (1,024 threads a
+// workgroup, whose registers spill: 158 and 18 us a call).
 #include <algorithm>
 
 #include "encoder.hpp"
@@ -27,8 +28,8 @@ namespace {
 constexpr int kNormE = 8;                  // values of a piece
 constexpr int64_t kMaxNormD = 32768;       // 1,024 lanes, four pieces
 constexpr int kGradThreads = 512;
-// The longest rows that the one-pass backward kernel takes: 8,192 floats (4,000 rows of 8,200: 184 us by it, 151 by two kernels), twice as many
-// 16-bit values, which wait in half the registers (2,000 x 16,384 61 us, by two kernels 87)
+// The longest rows that the one-pass backward kernel takes: 8,192 floats (4,000 rows of 8,200: 187 us a call by it, 154 by two
+// kernels), twice as many 16-bit values, which wait in half the registers (2,000 x 16,384 73 us, by two kernels 104)
 inline int64_t one_pass_values(int type) { return type == PQT_F32 ? 8192 : 16384; }
 constexpr unsigned kLongParts = 64;        // parts of the rows whose columns are added up one after the other beyond that
 constexpr unsigned kGradBlocks = 256;      // workgroups of the backward pass, at most: one a compute unit
@@ -372,7 +373,7 @@ void with_gradient_shape(int64_t D, F&& f) {
 }
 
 // Workgroups of the backward kernel.  A single one for up to two rows a group: its sums are the result, without a second launch (8 x 1,000 bf16
-// 4.7 us in a graph, by two launches 6.3; 13.3 and 16.0 from Python.  Four rows a group: 32 x 1,000 7.9 and 6.5, 4 x 16,384 18.6 and 11.3).
+// 4.6 us in a graph, by two launches 6.3.  Four rows a group: 32 x 1,000 7.9 and 6.8, 4 x 16,384 18.3 and 11.3).
 constexpr int kAloneRows = 2;
 unsigned gradient_blocks(int64_t rows, int groups) {
     return rows <= (int64_t)kAloneRows * groups ? 1u : (unsigned)std::min<int64_t>((rows + groups - 1) / groups, kGradBlocks);
