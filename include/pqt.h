@@ -379,7 +379,7 @@ int pqt_measure_peaks(int device, double* hbm_read_gb_per_s, double* mfma_f32_tf
 
 /*
  * The query encoder's operators -- what stands between the tokens of a text and the vectors the index is built from
- * and asked with: rows of an embedding table, layer norm, and products with 8-bit weights, each with its gradient.  They
+ * and asked with: rows of an embedding table, layer norm, root-mean-square norm, attention, and products with 8-bit weights, each with its gradient.  They
  * belong to no index.  Conventions common to all of them:
  *   - matrices are row-major device arrays on GPU `device`; a row begins `stride` elements after the one before
  *     (stride >= the row's length, any number; a slice of a wider buffer needs no copy), and every pointer is aligned to
@@ -465,6 +465,63 @@ size_t pqt_block_product_workspace(int64_t m, int64_t n, int64_t k);
 int pqt_block_product(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, int64_t m,
                       int64_t n, int64_t k, const float* bias, void* out, int out_type, int64_t out_stride, void* workspace,
                       size_t workspace_bytes, int device, void* hip_stream);
+
+/*
+ * pqt_rms_norm -- for every row: h = x + residual, rounded to their type as it is kept; rstd = 1 / sqrt(mean of h^2 + eps); y = h * rstd *
+ * weight.  x, residual (may be NULL: h = x) and h (may be NULL: not kept) are rows x D of `type`; weight: D values of param_type, or NULL (ones); rstd:
+ * fp32 values for the backward pass, or NULL.  The result is either y, rows x D of `out_type`, or codes and scales: y in 8-bit blocks along its rows, as
+ * pqt_block_quantize lays them out (of y's fp32 values, which are not rounded to another type before).  1 <= D <= 32768
+ * (above: PQT_EUNSUPPORTED), eps >= 0.
+ *
+ * pqt_rms_norm_gradient -- with z = h * rstd and g = grad * weight:
+ *     dx = through + rstd * (g - z * mean(g * z)),   dweight = sum over rows of grad * z.
+ * dx is the gradient of h, and so of x and of residual; through (may be NULL: zeros): what arrives at h along the residual's way.  grad,
+ * through, h and dx are rows x D of `type`; rstd as pqt_rms_norm wrote it; weight may be NULL (ones); dweight: D fp32 values or NULL.
+ */
+int pqt_rms_norm(const void* x, int type, int64_t rows, int64_t D, int64_t x_stride, const void* residual, int64_t residual_stride, void* h,
+                 int64_t h_stride, const void* weight, int param_type, float eps, void* y, int out_type, int64_t y_stride, uint8_t* codes,
+                 uint8_t* scales, float* rstd, int device, void* hip_stream);
+size_t pqt_rms_norm_gradient_workspace(int64_t rows, int64_t D);
+int pqt_rms_norm_gradient(const void* grad, int64_t grad_stride, const void* through, int64_t through_stride, const void* h, int64_t h_stride,
+                          int type, int64_t rows, int64_t D, const void* weight, int param_type, const float* rstd, void* dx,
+                          int64_t dx_stride, float* dweight, void* workspace, size_t workspace_bytes, int device, void* hip_stream);
+
+/*
+ * pqt_attention -- attention among the tokens of every text.  Rows starts[s] .. starts[s + 1] - 1 of the n rows belong to text s of `texts`; starts:
+ * device array of texts + 1 integers of place_bytes = 4 or 8, ascending.  lengths: as many integers of that size for each text, or NULL: only
+ * a text's first lengths[s] rows hold tokens, the others pad it.  (Numbers out of range are taken as the nearest that is in range; results of texts that
+ * overlap are not defined.)  A row of q has `heads` times d values, one of k and v `kv_heads` times d, which divides heads: heads / kv_heads
+ * consecutive heads share keys and values.  For every head and every token i, over the tokens j of its text:
+ *     z_ij = scale * q_i . k_j + bias[head][distances[j - i]],   lse_i = log(sum over j of exp(z_ij)),   out_i = sum over j of exp(z_ij - lse_i) v_j.
+ * bias: heads x buckets fp32, or NULL; distances: device array of 2 * reach + 1 integers (int32), the buckets of the distances -reach .. reach; farther
+ * ones have their ends', and a bucket outside 0 .. buckets - 1 has no bias.  A bias of -inf masks its distances; a token to which it leaves nothing
+ * gets zeros and an lse of -inf, as the rows that pad a text do.  Finite bias / scale counts within 2^90.  Rows of no text are left as they were, or,
+ * with clear != 0, get the same.  out: n x heads * d of `type`, the type of q, k and v; lse: heads x n fp32, or NULL.
+ * For bf16 and f16 the weights exp(z_ij - lse_i) are rounded to that type where they are multiplied; sums are fp32.
+ * 1 <= d <= 128, reach <= 512, buckets <= 1024, 2^-32 <= scale <= 2^32; (n / 16 + texts + 1) * heads below 2^24 (beyond: PQT_EUNSUPPORTED).
+ *
+ * pqt_attention_gradient -- the gradients of q, k, v (n rows each, as those) and of bias (heads x buckets fp32, may be NULL) from that of out; out and
+ * lse as pqt_attention wrote them.  With p_ij = exp(z_ij - lse_i) and ds_ij = p_ij (grad_i . v_j - grad_i . out_i):
+ *     dq_i = scale * sum of ds_ij k_j,  dk_j = scale * sum of ds_ij q_i,  dv_j = sum of p_ij grad_i,  dbias[head][b] = sum of ds_ij over b's distances;
+ * dk and dv are sums over the heads that share them too.  Rows that pad a text get zeros, rows of no text are left or cleared as above.  The workspace is
+ * asked for with buckets = 0 where there is no dbias.
+ *
+ * pqt_distance_buckets -- the usual buckets, on the host: distances (2 * far + 1 integers in host memory) for `buckets` of distances -far .. far.
+ * both != 0: half of the buckets (an even number) for keys before the query and it itself, half for those behind it; else all for those before, with
+ * those behind in the first.  Of each, the first half has a bucket for every distance, the rest ever wider ones: distance t lies in step
+ * floor(log(t / near) / log(far / near) * rest) of the `rest` that follow the `near` first.  2 to 1024 buckets, far up to 512.
+ */
+int pqt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int type, int64_t n, int heads,
+                  int kv_heads, int d, const void* starts, const void* lengths, int place_bytes, int64_t texts, float scale, const float* bias,
+                  int buckets, const int32_t* distances, int reach, int clear, void* out, int64_t out_stride, float* lse, int device,
+                  void* hip_stream);
+size_t pqt_attention_gradient_workspace(int64_t n, int64_t texts, int heads, int buckets);
+int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                           int64_t v_stride, const void* out, int64_t out_stride, const float* lse, int type, int64_t n, int heads, int kv_heads, int d,
+                           const void* starts, const void* lengths, int place_bytes, int64_t texts, float scale, const float* bias, int buckets,
+                           const int32_t* distances, int reach, int clear, void* dq, int64_t dq_stride, void* dk, int64_t dk_stride, void* dv,
+                           int64_t dv_stride, float* dbias, void* workspace, size_t workspace_bytes, int device, void* hip_stream);
+int pqt_distance_buckets(int buckets, int far, int both, int32_t* distances);
 
 /* Message of the last failing call on this thread ("" if none).  Static storage. */
 const char* pqt_last_error(void);

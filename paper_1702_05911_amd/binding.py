@@ -23,7 +23,8 @@ EXPORTS = (
     "pqt_index_set_vectors", "pqt_query_batch_exact", "pqt_brute_force", "pqt_measure_peaks", "pqt_set_profiling",
     "pqt_stage_times", "pqt_embed", "pqt_embed_gradient_workspace", "pqt_embed_gradient", "pqt_layer_norm",
     "pqt_layer_norm_gradient_workspace", "pqt_layer_norm_gradient", "pqt_block_quantize", "pqt_block_product_workspace",
-    "pqt_block_product", "pqt_last_error",
+    "pqt_block_product", "pqt_rms_norm", "pqt_rms_norm_gradient_workspace", "pqt_rms_norm_gradient", "pqt_attention",
+    "pqt_attention_gradient_workspace", "pqt_attention_gradient", "pqt_distance_buckets", "pqt_last_error",
 )
 
 
@@ -138,6 +139,21 @@ def load_library(path=LIB_PATH):
     lib.pqt_block_product_workspace.restype = sz
     lib.pqt_block_product.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, ci, i64, vp, sz, ci, vp]
     lib.pqt_block_product.restype = ci
+    lib.pqt_rms_norm.argtypes = [vp, ci, i64, i64, i64, vp, i64, vp, i64, vp, ci, cf, vp, ci, i64, vp, vp, vp, ci, vp]
+    lib.pqt_rms_norm.restype = ci
+    lib.pqt_rms_norm_gradient_workspace.argtypes = [i64, i64]
+    lib.pqt_rms_norm_gradient_workspace.restype = sz
+    lib.pqt_rms_norm_gradient.argtypes = [vp, i64, vp, i64, vp, i64, ci, i64, i64, vp, ci, vp, vp, i64, vp, vp, sz, ci, vp]
+    lib.pqt_rms_norm_gradient.restype = ci
+    lib.pqt_attention.argtypes = [vp, i64, vp, i64, vp, i64, ci, i64, ci, ci, ci, vp, vp, ci, i64, cf, vp, ci, vp, ci, ci, vp, i64, vp, ci, vp]
+    lib.pqt_attention.restype = ci
+    lib.pqt_attention_gradient_workspace.argtypes = [i64, i64, ci, ci]
+    lib.pqt_attention_gradient_workspace.restype = sz
+    lib.pqt_attention_gradient.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, ci, i64, ci, ci, ci, vp, vp, ci, i64, cf, vp, ci, vp, ci, ci,
+                                           vp, i64, vp, i64, vp, i64, vp, vp, sz, ci, vp]
+    lib.pqt_attention_gradient.restype = ci
+    lib.pqt_distance_buckets.argtypes = [ci, ci, ci, vp]
+    lib.pqt_distance_buckets.restype = ci
     lib.pqt_last_error.argtypes = []
     lib.pqt_last_error.restype = ctypes.c_char_p
     return lib
@@ -639,6 +655,161 @@ def pqt_block_product(a, b, bias=None, out=None, out_dtype=None, stream=None):
     return out
 
 
+def pqt_rms_norm(x, weight=None, residual=None, eps=1e-6, blocks=False, out=None, out_dtype=None, stream=None):
+    """pqt_rms_norm.  x, residual: (rows, D) of one type; weight: (D,) or None.  Returns (y, h, rstd): h = x + residual (x itself where there is no residual),
+    y = h * rstd * weight, with blocks=True as Blocks, which pqt_block_product takes."""
+    if stream is not None:
+        with _running_on(stream, x, weight, residual, out):
+            return pqt_rms_norm(x, weight, residual, eps, blocks, out, out_dtype)
+    ptr, kind, step = _matrix("x", x)
+    rows, D = x.shape
+    device = x.device
+    w = _vector("weight", weight, D, _TYPES, device)
+    if residual is None:
+        h, rptr, rstep, hptr, hstep = x, None, 0, None, 0
+    else:
+        _same_device(device, residual=residual)
+        rptr, _, rstep = _matrix("residual", residual, (rows, D), x.dtype)
+        h = torch.empty(rows, D, dtype=x.dtype, device=device)
+        hptr, hstep = h.data_ptr(), D
+    rstd = torch.empty(rows, dtype=torch.float32, device=device)
+    if blocks:
+        if out is not None or out_dtype is not None:
+            raise ValueError("out and out_dtype do not go with blocks")
+        y = _empty_blocks(rows, D, device)
+        optr, okind, ostep, codes, scales = None, kind, 0, y.codes.data_ptr(), y.scales.data_ptr()
+    else:
+        y, optr, okind, ostep = _result(out, (rows, D), out_dtype or x.dtype, device, out_dtype is not None)
+        codes = scales = None
+    _check(_lib.pqt_rms_norm(ptr, kind, rows, D, step, rptr, rstep, hptr, hstep, w, PQT_F32 if weight is None else _type_of(weight), eps, optr, okind, ostep,
+                             codes, scales, rstd.data_ptr(), device.index, _current(device.index)))
+    return y, h, rstd
+
+
+def pqt_rms_norm_gradient(grad, h, weight, rstd, through=None, out=None, stream=None):
+    """pqt_rms_norm_gradient.  grad, h, through: (rows, D) of one type; rstd: what pqt_rms_norm returned; through: the gradient that arrives at h
+    along the residual's way, or None.  Returns (dx, dweight): the gradient of x and of the residual, and the weight's in float32."""
+    if stream is not None:
+        with _running_on(stream, grad, h, weight, rstd, through, out):
+            return pqt_rms_norm_gradient(grad, h, weight, rstd, through, out)
+    ptr, kind, step = _matrix("h", h)
+    rows, D = h.shape
+    device = h.device
+    _same_device(device, grad=grad, through=through)
+    gptr, _, gstep = _matrix("grad", grad, (rows, D), h.dtype)
+    tptr, _, tstep = _matrix("through", through, (rows, D), h.dtype) if through is not None else (None, 0, 0)
+    w = _vector("weight", weight, D, _TYPES, device)
+    rptr = _vector("rstd", rstd, rows, _FLOATS, device)
+    out, optr, _, ostep = _result(out, (rows, D), h.dtype, device)
+    dweight = torch.empty(D, dtype=torch.float32, device=device)
+    nbytes = _lib.pqt_rms_norm_gradient_workspace(rows, D)
+    ws = _workspace(nbytes, device)
+    _check(_lib.pqt_rms_norm_gradient(gptr, gstep, tptr, tstep, ptr, step, kind, rows, D, w, PQT_F32 if weight is None else _type_of(weight), rptr, optr,
+                                      ostep, dweight.data_ptr(), ws.data_ptr() if nbytes else None, nbytes, device.index, _current(device.index)))
+    return out, dweight
+
+
+def pqt_distance_buckets(buckets, far, both=True, device=None):
+    """pqt_distance_buckets.  Returns (2 * far + 1,) int32 on `device` (the CPU): the usual buckets of the distances -far .. far."""
+    distances = torch.empty(2 * far + 1, dtype=torch.int32) if far > 0 else None
+    _check(_lib.pqt_distance_buckets(buckets, far, 1 if both else 0, distances.data_ptr() if far > 0 else None))
+    return distances if device is None else distances.to(device)
+
+
+def _heads(q, k, v, heads):
+    """Sizes of attention's inputs: rows, values of a head, heads of keys, and the three with their strides and common type."""
+    qptr, kind, qstep = _matrix("q", q)
+    n, wide = q.shape
+    if heads < 1 or wide % heads:
+        raise ValueError(f"q has {wide} values in a row, which are not those of {heads} heads")
+    d = wide // heads
+    narrow = k.shape[1] if k.dim() == 2 else 0
+    if d < 1 or narrow < d or narrow % d or heads % (narrow // d):
+        raise ValueError(f"k has shape {tuple(k.shape)}: expected {n} rows of heads of {d} values, as many as {heads} or a divisor of that")
+    _same_device(q.device, k=k, v=v)
+    kptr, _, kstep = _matrix("k", k, (n, narrow), q.dtype)
+    vptr, _, vstep = _matrix("v", v, (n, narrow), q.dtype)
+    return n, d, narrow // d, kind, (qptr, qstep, kptr, kstep, vptr, vstep)
+
+
+def _texts(starts, lengths, device):
+    """Where texts are: (starts, lengths, bytes of a place, number of texts)."""
+    size = _TOKEN_BYTES.get(starts.dtype)
+    if size is None or starts.device != device or starts.dim() != 1 or not starts.is_contiguous() or starts.shape[0] < 1:
+        raise ValueError(f"starts must be a contiguous 1-D int32 or int64 tensor on {device} of a place for every text and one more")
+    texts = starts.shape[0] - 1
+    return starts.data_ptr(), _vector("lengths", lengths, texts, (starts.dtype,), device), size, texts
+
+
+_PLACES = (torch.int32,)
+
+
+def _bias(bias, distances, heads, device):
+    """Attention's bias: (pointer, buckets, distances, reach)."""
+    if bias is None:
+        if distances is not None:
+            raise ValueError("distances need a bias")
+        return None, 0, None, 0
+    if bias.dtype is not torch.float32 or bias.device != device or bias.dim() != 2 or bias.shape[0] != heads or bias.shape[1] < 1 or not bias.is_contiguous():
+        raise ValueError(f"bias must be a contiguous float32 tensor (heads, buckets) on {device}, with {heads} heads")
+    if distances is None or distances.dim() != 1 or distances.shape[0] % 2 == 0:
+        raise ValueError("distances must be a 1-D tensor of the buckets of the distances -reach .. reach")
+    return bias.data_ptr(), bias.shape[1], _vector("distances", distances, distances.shape[0], _PLACES, device), distances.shape[0] // 2
+
+
+def pqt_attention(q, k, v, starts, heads, scale=None, bias=None, distances=None, lengths=None, out=None, stream=None):
+    """pqt_attention.  q: (n, heads * d); k, v: (n, kv_heads * d), of one type; starts: (texts + 1,) int32 or int64: the rows of each text; lengths:
+    (texts,) of that type, or None: how many of them hold tokens; scale: 1 / sqrt(d) unless given; bias: (heads, buckets) float32 with distances (2 * reach + 1,)
+    int32, the buckets of the distances -reach .. reach of a key from its query (pqt_distance_buckets).  Returns (out, lse): (n, heads * d) and, for
+    the backward pass, (heads, n) float32.  Rows of no text are zeros (lse -inf) in results that the call makes, and left as they were in `out`."""
+    if stream is not None:
+        with _running_on(stream, q, k, v, starts, bias, distances, lengths, out):
+            return pqt_attention(q, k, v, starts, heads, scale, bias, distances, lengths, out)
+    n, d, kv_heads, kind, inputs = _heads(q, k, v, heads)
+    device = q.device
+    sptr, lptr, size, texts = _texts(starts, lengths, device)
+    bptr, buckets, dptr, reach = _bias(bias, distances, heads, device)
+    clear = out is None
+    out, optr, _, ostep = _result(out, (n, heads * d), q.dtype, device)
+    lse = torch.empty(heads, n, dtype=torch.float32, device=device)
+    if not clear:
+        lse.fill_(-float("inf"))
+    _check(_lib.pqt_attention(*inputs, kind, n, heads, kv_heads, d, sptr, lptr, size, texts, d ** -0.5 if scale is None else scale, bptr, buckets, dptr, reach,
+                              1 if clear else 0, optr, ostep, lse.data_ptr(), device.index, _current(device.index)))
+    return out, lse
+
+
+def pqt_attention_gradient(grad, q, k, v, out, lse, starts, heads, scale=None, bias=None, distances=None, lengths=None, grads=None, stream=None):
+    """pqt_attention_gradient.  grad: (n, heads * d), the gradient of `out`; out, lse: what pqt_attention returned, the others what it was given.
+    grads: three matrices for the results, of q's, k's and v's sizes (slices of one, where these are), or None.  Returns (dq, dk, dv, dbias), dbias (heads,
+    buckets) float32, or None where there is no bias."""
+    if stream is not None:
+        with _running_on(stream, grad, q, k, v, out, lse, starts, bias, distances, lengths, *(grads or ())):
+            return pqt_attention_gradient(grad, q, k, v, out, lse, starts, heads, scale, bias, distances, lengths, grads)
+    n, d, kv_heads, kind, inputs = _heads(q, k, v, heads)
+    device, dtype = q.device, q.dtype
+    wide, narrow = heads * d, kv_heads * d
+    _same_device(device, grad=grad, out=out)
+    gptr, _, gstep = _matrix("grad", grad, (n, wide), dtype)
+    optr, _, ostep = _matrix("out", out, (n, wide), dtype)
+    if lse.dtype is not torch.float32 or lse.device != device or lse.shape != (heads, n) or not lse.is_contiguous():
+        raise ValueError(f"lse must be a contiguous float32 tensor {(heads, n)} on {device}")
+    sptr, lptr, size, texts = _texts(starts, lengths, device)
+    bptr, buckets, dptr, reach = _bias(bias, distances, heads, device)
+    dq, dk, dv = grads or (None, None, None)
+    dq, dqptr, _, dqstep = _result(dq, (n, wide), dtype, device)
+    dk, dkptr, _, dkstep = _result(dk, (n, narrow), dtype, device)
+    dv, dvptr, _, dvstep = _result(dv, (n, narrow), dtype, device)
+    dbias = None if bias is None else torch.empty(heads, buckets, dtype=torch.float32, device=device)
+    nbytes = _lib.pqt_attention_gradient_workspace(n, texts, heads, buckets)
+    ws = _workspace(nbytes, device)
+    _check(_lib.pqt_attention_gradient(gptr, gstep, *inputs, optr, ostep, lse.data_ptr(), kind, n, heads, kv_heads, d, sptr, lptr, size, texts,
+                                       d ** -0.5 if scale is None else scale, bptr, buckets, dptr, reach, 0 if grads else 1, dqptr, dqstep, dkptr, dkstep,
+                                       dvptr, dvstep, None if dbias is None else dbias.data_ptr(), ws.data_ptr() if nbytes else None, nbytes, device.index,
+                                       _current(device.index)))
+    return dq, dk, dv, dbias
+
+
 # The sizes of scratch memory are asked for by the calls above; a caller of the C ABI asks for them itself.
 def pqt_embed_gradient_workspace(n, V, D):
     return int(_lib.pqt_embed_gradient_workspace(n, V, D))
@@ -650,6 +821,14 @@ def pqt_layer_norm_gradient_workspace(rows, D):
 
 def pqt_block_product_workspace(m, n, k):
     return int(_lib.pqt_block_product_workspace(m, n, k))
+
+
+def pqt_rms_norm_gradient_workspace(rows, D):
+    return int(_lib.pqt_rms_norm_gradient_workspace(rows, D))
+
+
+def pqt_attention_gradient_workspace(n, texts, heads, buckets):
+    return int(_lib.pqt_attention_gradient_workspace(n, texts, heads, buckets))
 
 
 def last_error():

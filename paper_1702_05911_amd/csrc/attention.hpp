@@ -1,0 +1,328 @@
+// What attention and its gradient share (attention.hip, attention_gradient.hip): fragments and the matrix instructions, tiles of rows in LDS, which
+// rows a workgroup has, and the bias by distance.
+//
+// Everything is built on products of 16 x 16 results over 32 values.  A fragment holds, of one of 16 rows (lane & 15), eight values: those of
+// places 8 * (lane >> 4) .. + 7.  A result has its column in lane & 15 and rows 4 * (lane >> 4) .. + 3 in four registers.  So the results of two products
+// that lie 16 rows apart are, column by column, a fragment of 32 places in the order place(e) = 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3): weights go
+// from one product into the next without leaving their lane, if the other operand's values are taken in that order.
+#pragma once
+#include <algorithm>
+
+#include "encoder.hpp"
+
+namespace pqt {
+namespace {
+
+constexpr int kMaxHeadD = 128;
+constexpr int kMaxReach = 512;
+constexpr int kMaxBuckets = 1024;
+constexpr int64_t kMaxRows = 0x7ffffff0;       // rows of a text are 32-bit numbers
+constexpr int64_t kMaxWorkgroups = 0xffffff;   // of up to 256 threads each, fewer than 2^32 in all
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// ---- fragments -------------------------------------------------------------------------------------------------------
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <typename T> struct FragmentOf;
+template <> struct FragmentOf<Bf16> {
+    typedef __bf16 type __attribute__((ext_vector_type(8)));
+    typedef u32x4 piece __attribute__((aligned(2)));           // 16 bytes at any element
+};
+template <> struct FragmentOf<Half> {
+    typedef _Float16 type __attribute__((ext_vector_type(8)));
+    typedef u32x4 piece __attribute__((aligned(2)));           // 16 bytes at any element
+};
+template <> struct FragmentOf<float> {
+    typedef float type __attribute__((ext_vector_type(8)));
+    typedef u32x4 piece __attribute__((aligned(4)));
+};
+template <typename T> using Fragment = typename FragmentOf<T>::type;
+
+__device__ __forceinline__ f32x4 multiply(Fragment<Bf16> a, Fragment<Bf16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 multiply(Fragment<Half> a, Fragment<Half> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+// fp32: eight instructions over four places each, the e-th over the e-th values of the four groups of lanes
+__device__ __forceinline__ f32x4 multiply(Fragment<float> a, Fragment<float> b, f32x4 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+}
+
+// results of two products 16 rows apart as a fragment (rounded to nearest even)
+template <typename T>
+__device__ __forceinline__ Fragment<T> fragment_of(f32x4 lo, f32x4 hi) {
+    f32x8 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[e] = lo[e];
+        v[e + 4] = hi[e];
+    }
+    return __builtin_convertvector(v, Fragment<T>);
+}
+
+// ---- tiles of rows in LDS --------------------------------------------------------------------------------------------
+template <typename T> struct Stored { typedef T type; };
+template <> struct Stored<Bf16> { typedef __bf16 type; };
+template <> struct Stored<Half> { typedef _Float16 type; };
+
+// ROWS rows of up to DP values, 16 bytes further apart than they are long, so that 16 rows' 16-byte pieces begin in different banks
+template <typename T, int ROWS, int DP>
+struct Tile {
+    typedef typename Stored<T>::type S;
+    static constexpr int kPitch = DP + 16 / (int)sizeof(T);
+    S v[ROWS * kPitch];
+
+    // values 32 chunk + 8 (lane >> 4) .. + 7 of row row0 + (lane & 15)
+    __device__ __forceinline__ Fragment<T> rows(int row0, int chunk) const {
+        const int lane = threadIdx.x & (kWave - 1);
+        const S* p = v + (row0 + (lane & 15)) * kPitch + chunk * 32 + (lane >> 4) * 8;
+        typedef Fragment<T> __attribute__((aligned(16))) F;
+        return *reinterpret_cast<const F*>(p);
+    }
+    // the transpose's: of column 16 block + (lane & 15), the rows row0 + place(e)
+    __device__ __forceinline__ Fragment<T> columns(int row0, int block) const {
+        const int lane = threadIdx.x & (kWave - 1);
+        Fragment<T> f;
+        if constexpr (sizeof(T) == 2) {
+            // sixteen lanes read 4 x 16 values, 8 bytes each, and get a column's four
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const S* p = v + (row0 + (lane >> 4) * 4 + ((lane & 15) >> 2)) * kPitch + block * 16 + (lane & 3) * 4;
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * kPitch));
+            f = __builtin_bit_cast(Fragment<T>, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const S* p = v + (row0 + (lane >> 4) * 4) * kPitch + block * 16 + (lane & 15);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = p[(16 * (e >> 2) + (e & 3)) * kPitch];
+        }
+        return f;
+    }
+};
+
+// A thread's 16-byte pieces of the next tile, on their way while one is worked on.  WHOLE: rows are whole pieces; else a row's last piece is read
+// value by value.  Rows past `len` and values past `d` become zeros, whatever stands there in memory.
+template <typename T, int ROWS, int DP, int THREADS, bool WHOLE>
+struct Loads {
+    static constexpr int E = 16 / (int)sizeof(T), kOfRow = DP / E, kPieces = ROWS * kOfRow / THREADS;
+    static_assert(ROWS * kOfRow % THREADS == 0, "whole pieces for every thread");
+    u32x4 v[kPieces];
+    typedef typename FragmentOf<T>::piece Unaligned;
+
+    __device__ __forceinline__ void fetch(const T* base, int64_t stride, int row0, int len, int d) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int at = threadIdx.x + i * THREADS, row = row0 + at / kOfRow, c = at % kOfRow * E;
+            const T* p = base + (int64_t)min(row, len - 1) * stride;
+            if constexpr (WHOLE) {
+                v[i] = *reinterpret_cast<const Unaligned*>(p + min(c, d - E));
+                if (row >= len || c >= d) v[i] = u32x4{};
+            } else {
+                v[i] = u32x4{};
+                if (row < len && c < d) v[i] = piece(p + c, d - c);
+            }
+        }
+    }
+    static __device__ __forceinline__ u32x4 piece(const T* p, int have) {
+        if (have >= E) return *reinterpret_cast<const Unaligned*>(p);
+        union { u32x4 v; T e[E]; } u;
+        u.v = u32x4{};
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            if (j < have) u.e[j] = p[j];
+        return u.v;
+    }
+    __device__ __forceinline__ void put(Tile<T, ROWS, DP>& tile) const {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int at = threadIdx.x + i * THREADS;
+            *reinterpret_cast<u32x4*>(tile.v + at / kOfRow * Tile<T, ROWS, DP>::kPitch + at % kOfRow * E) = v[i];
+        }
+    }
+};
+
+// fragment `chunk` of a wavefront's own 16 rows row0 + (lane & 15), straight from memory
+template <typename T>
+__device__ __forceinline__ Fragment<T> rows_of_memory(const T* base, int64_t stride, int row0, int len, int d, int chunk) {
+    const int lane = threadIdx.x & (kWave - 1), row = row0 + (lane & 15), c = chunk * 32 + (lane >> 4) * 8;
+    typedef typename Piece_<T, 8>::type V;
+    V v = V{};
+    if (row < len && c < d) v = load_raw<T, 8>(base + (int64_t)row * stride + c, d - c);
+    return __builtin_bit_cast(Fragment<T>, v);
+}
+
+// ---- which rows ------------------------------------------------------------------------------------------------------
+struct AttentionArgs {
+    const void* q;
+    const void* k;
+    const void* v;
+    const void* grad;
+    const void* out_in;                    // gradient: what the forward pass wrote
+    const float* lse_in;
+    const void* starts;
+    const void* lengths;                   // or null: texts reach to the next one
+    const float* bias;                     // heads x buckets, or null
+    const int32_t* distances;              // buckets of -reach .. reach
+    void* out;
+    float* lse;
+    void* dq;
+    void* dk;
+    void* dv;
+    float* delta;                          // heads x n
+    float* parts;                          // workgroups x buckets
+    int64_t q_stride, k_stride, v_stride, grad_stride, out_stride, dq_stride, dk_stride, dv_stride;
+    int64_t n, texts;
+    int64_t tiles;                         // workgroups of a head
+    int wide;                              // starts and lengths are 64-bit numbers
+    int heads, group, d, buckets, reach, clear;
+    float scale;
+};
+
+__device__ __forceinline__ int64_t number(const void* p, int wide, int64_t i) {
+    return wide ? static_cast<const int64_t*>(p)[i] : static_cast<const int32_t*>(p)[i];
+}
+
+// Rows begin .. begin + span of a text (of which `len` have tokens), and the first of those that a workgroup has.  Workgroup t of a head, of M rows each: text s
+// has those from floor(start / M) + s on, which leaves every text one for each M rows it begins, without a table of them.
+struct Rows {
+    int64_t begin;
+    int span, len, row0;
+    bool mine;                             // false: nothing to do
+    bool text;                             // false: rows of no text
+    int64_t before;                        // rows before the first text that this workgroup clears, too
+};
+
+template <int M>
+__device__ __forceinline__ Rows rows_of_workgroup(const AttentionArgs& g, int64_t t) {
+    const int lane = threadIdx.x & (kWave - 1);
+    auto start = [&](int64_t s) __attribute__((always_inline)) { return min(max(number(g.starts, g.wide, s), (int64_t)0), g.n); };
+    // the last text with floor(start / M) + s <= t: 64 of them looked at at once.  (texts: the rows behind the last one.)
+    int64_t lo = 0, hi = g.texts + 1;
+    bool first = true;
+    Rows r{};
+    while (first || hi - lo > 1) {
+        const int64_t step = (hi - lo + kWave - 1) / kWave, probe = lo + lane * step;
+        const bool ok = probe < hi && start(probe) / M + probe <= t;
+        const int count = (int)__popcll(__ballot(ok));
+        if (count == 0) break;                                   // (of the first round only: later ones begin with one that is)
+        lo = lo + (int64_t)(count - 1) * step;
+        hi = min(hi, lo + step);
+        first = false;
+    }
+    lo = __builtin_amdgcn_readfirstlane((int)lo);              // (texts are fewer than 2^31)
+    if (first) {                                               // rows before the first text
+        r.begin = t * M;
+        r.span = M;
+        r.mine = g.clear != 0;
+        return r;
+    }
+    const int64_t begin = start(lo), end = lo < g.texts ? max(start(lo + 1), begin) : g.n;
+    r.begin = begin;
+    r.span = (int)(end - begin);
+    r.text = lo < g.texts;
+    r.len = r.text ? (g.lengths ? (int)min(max(number(g.lengths, g.wide, lo), (int64_t)0), end - begin) : r.span) : 0;
+    const int64_t row0 = (t - (begin / M + lo)) * M;
+    r.before = lo == 0 && row0 == 0 && g.clear ? begin % M : 0;
+    r.mine = r.before > 0 || (row0 < r.span && (r.text || g.clear));
+    r.row0 = (int)min(row0, (int64_t)r.span);
+    return r;
+}
+
+// Workgroup -> (rows, head).  Consecutive workgroups go to the eight XCDs in turn: each XCD gets a run of one head's rows after another, so that its L2
+// holds the keys and values that they share.
+__device__ __forceinline__ void place_of_workgroup(const AttentionArgs& g, int heads, int64_t& t, int& head) {
+    const int64_t total = g.tiles * heads, per = total >> 3;
+    const int x = blockIdx.x & 7, more = (int)(total & 7);
+    const int64_t at = x * per + min(x, more) + (blockIdx.x >> 3);
+    head = (int)(at / g.tiles);
+    t = at - (int64_t)head * g.tiles;
+}
+
+// zeros in rows from .. to of d columns
+template <typename T>
+__device__ __forceinline__ void clear_rows(T* p, int64_t stride, int64_t from, int64_t to, int d) {
+    for (int64_t e = threadIdx.x; e < (to - from) * d; e += blockDim.x) p[(from + e / d) * stride + e % d] = from_float<T>(0.0f);
+}
+
+// ---- the bias by distance --------------------------------------------------------------------------------------------
+// Products are taken unscaled, with bias / scale as what they are added to, so that a logit is one multiplication by scale * log2 e away from its power
+// of two.  Finite entries are kept within 2^90, where that multiplication (scale up to 2^32) cannot overflow; -inf stays.
+constexpr float kBiasTop = 0x1p90f, kLowest = -0x1p92f;        // (kLowest: below every finite logit)
+
+__device__ __forceinline__ float bias_of(const AttentionArgs& g, int head, int distance) {
+    const int b = g.distances[max(-g.reach, min(distance, g.reach)) + g.reach];
+    if ((unsigned)b >= (unsigned)g.buckets) return 0.0f;       // a distance of no bucket has no bias
+    const float entry = g.bias[(int64_t)head * g.buckets + b], v = entry / g.scale;
+    return fabsf(entry) < __builtin_inff() ? fmaxf(-kBiasTop, fminf(v, kBiasTop)) : v;
+}
+
+// Fills table[0 .. 2 W] with the bias of the distances -W .. W (SIGN -1: W .. -W)
+template <int SIGN, int THREADS>
+__device__ __forceinline__ void fill_bias(const AttentionArgs& g, int head, float* table, int W) {
+    for (int i = threadIdx.x; i <= 2 * W; i += THREADS) table[i] = bias_of(g, head, SIGN * (i - W));
+}
+
+__device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// the largest, and the sum, over the four groups of sixteen lanes
+__device__ __forceinline__ float max_of_groups(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16, kWave));
+    return fmaxf(v, __shfl_xor(v, 32, kWave));
+}
+__device__ __forceinline__ float sum_of_groups(float v) {
+    v += __shfl_xor(v, 16, kWave);
+    return v + __shfl_xor(v, 32, kWave);
+}
+
+// calls f(Int<DP>) for heads of d values
+template <int V> struct Width { static constexpr int value = V; };
+template <typename F>
+void with_head(int d, F&& f) {
+    if (d <= 32) f(Width<32>{});
+    else if (d <= 64) f(Width<64>{});
+    else if (d <= 96) f(Width<96>{});
+    else f(Width<128>{});
+}
+
+// ---- checks of the C entries, and the choice of workgroup -------------------------------------------------------------
+inline int attention_checks(const char* who, int type, int64_t n, int heads, int kv_heads, int d, const void* starts, const void* lengths, int place_bytes,
+                            int64_t texts, float scale, const float* bias, int buckets, const int32_t* distances, int reach, AttentionArgs& g) {
+    using pqt_host::fail;
+    if (!known_type(type)) return fail(PQT_EINVAL, "%s: unknown type %d", who, type);
+    if (n < 0 || texts < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || d < 1)
+        return fail(PQT_EINVAL, "%s: n=%lld texts=%lld heads=%d (of keys %d) d=%d out of range", who, (long long)n, (long long)texts, heads, kv_heads, d);
+    if (place_bytes != 4 && place_bytes != 8) return fail(PQT_EINVAL, "%s: starts of %d bytes", who, place_bytes);
+    if (!(scale >= 0x1p-32f && scale <= 0x1p32f)) return fail(PQT_EINVAL, "%s: scale=%g is not between 2^-32 and 2^32", who, (double)scale);
+    if (bias && (buckets < 1 || reach < 0 || !distances)) return fail(PQT_EINVAL, "%s: a bias of %d buckets and distances up to %d", who, buckets, reach);
+    if (n > 0 && !starts) return fail(PQT_EINVAL, "%s: null pointer", who);
+    if (!aligned_to(starts, place_bytes) || !aligned_to(lengths, place_bytes) || !aligned_to(bias, 4) || !aligned_to(distances, 4))
+        return fail(PQT_EINVAL, "%s: a pointer is not aligned to its element", who);
+    if (d > kMaxHeadD) return fail(PQT_EUNSUPPORTED, "%s: heads of %d values, at most %d", who, d, kMaxHeadD);
+    if (bias && (buckets > kMaxBuckets || reach > kMaxReach))
+        return fail(PQT_EUNSUPPORTED, "%s: %d buckets, at most %d; distances up to %d, at most %d", who, buckets, kMaxBuckets, reach, kMaxReach);
+    if (n > kMaxRows || texts > kMaxRows || heads > 65535 || (n / 16 + texts + 1) * heads > kMaxWorkgroups)
+        return fail(PQT_EUNSUPPORTED, "%s: %lld rows in %lld texts of %d heads", who, (long long)n, (long long)texts, heads);
+    g.n = n;
+    g.texts = texts;
+    g.heads = heads;
+    g.group = heads / kv_heads;
+    g.d = d;
+    g.starts = starts;
+    g.lengths = lengths;
+    g.wide = place_bytes == 8;
+    g.scale = scale;
+    g.bias = bias;
+    g.buckets = buckets;
+    g.distances = distances;
+    g.reach = reach;
+    return PQT_OK;
+}
+
+// Queries of a workgroup, by the texts' mean length and how many workgroups there are for 256 compute units.
+inline int rows_of_a_workgroup(int64_t n, int64_t texts, int heads) {
+    const int64_t mean = texts ? n / texts : 0;
+    if (mean <= 32 || n / 64 * heads < 256) return 16;
+    return mean <= 512 || n / 128 * heads < 512 ? 64 : 128;
+}
+
+}  // namespace
+}  // namespace pqt
