@@ -498,7 +498,7 @@ int pqt_rms_norm_gradient(const void* grad, int64_t grad_stride, const void* thr
  * gets zeros and an lse of -inf, as the rows that pad a text do.  Finite bias / scale counts within 2^90.  Rows of no text are left as they were, or,
  * with clear != 0, get the same.  out: n x heads * d of `type`, the type of q, k and v; lse: heads x n fp32, or NULL.
  * For bf16 and f16 the weights exp(z_ij - lse_i) are rounded to that type where they are multiplied; sums are fp32.
- * 1 <= d <= 128, reach <= 512, buckets <= 1024, 2^-32 <= scale <= 2^32; (n / 16 + texts + 1) * heads below 2^24 (beyond: PQT_EUNSUPPORTED).
+ * 1 <= d <= 128, reach <= 448, buckets <= 1024, 2^-32 <= scale <= 2^32; (n / 16 + texts + 1) * heads below 2^24 (beyond: PQT_EUNSUPPORTED).
  *
  * pqt_attention_gradient -- the gradients of q, k, v (n rows each, as those) and of bias (heads x buckets fp32, may be NULL) from that of out; out and
  * lse as pqt_attention wrote them.  With p_ij = exp(z_ij - lse_i) and ds_ij = p_ij (grad_i . v_j - grad_i . out_i):
@@ -509,13 +509,13 @@ int pqt_rms_norm_gradient(const void* grad, int64_t grad_stride, const void* thr
  * pqt_distance_buckets -- the usual buckets, on the host: distances (2 * far + 1 integers in host memory) for `buckets` of distances -far .. far.
  * both != 0: half of the buckets (an even number) for keys before the query and it itself, half for those behind it; else all for those before, with
  * those behind in the first.  Of each, the first half has a bucket for every distance, the rest ever wider ones: distance t lies in step
- * floor(log(t / near) / log(far / near) * rest) of the `rest` that follow the `near` first.  2 to 1024 buckets, far up to 512.
+ * floor(log(t / near) / log(far / near) * rest) of the `rest` that follow the `near` first.  2 to 1024 buckets, far up to 448.
  */
 int pqt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int type, int64_t n, int heads,
                   int kv_heads, int d, const void* starts, const void* lengths, int place_bytes, int64_t texts, float scale, const float* bias,
                   int buckets, const int32_t* distances, int reach, int clear, void* out, int64_t out_stride, float* lse, int device,
                   void* hip_stream);
-size_t pqt_attention_gradient_workspace(int64_t n, int64_t texts, int heads, int buckets);
+size_t pqt_attention_gradient_workspace(int64_t n, int64_t texts, int heads, int kv_heads, int d, int buckets);
 int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                            int64_t v_stride, const void* out, int64_t out_stride, const float* lse, int type, int64_t n, int heads, int kv_heads, int d,
                            const void* starts, const void* lengths, int place_bytes, int64_t texts, float scale, const float* bias, int buckets,

@@ -147,7 +147,7 @@ def load_library(path=LIB_PATH):
     lib.pqt_rms_norm_gradient.restype = ci
     lib.pqt_attention.argtypes = [vp, i64, vp, i64, vp, i64, ci, i64, ci, ci, ci, vp, vp, ci, i64, cf, vp, ci, vp, ci, ci, vp, i64, vp, ci, vp]
     lib.pqt_attention.restype = ci
-    lib.pqt_attention_gradient_workspace.argtypes = [i64, i64, ci, ci]
+    lib.pqt_attention_gradient_workspace.argtypes = [i64, i64, ci, ci, ci, ci]
     lib.pqt_attention_gradient_workspace.restype = sz
     lib.pqt_attention_gradient.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, ci, i64, ci, ci, ci, vp, vp, ci, i64, cf, vp, ci, vp, ci, ci,
                                            vp, i64, vp, i64, vp, i64, vp, vp, sz, ci, vp]
@@ -801,7 +801,7 @@ def pqt_attention_gradient(grad, q, k, v, out, lse, starts, heads, scale=None, b
     dk, dkptr, _, dkstep = _result(dk, (n, narrow), dtype, device)
     dv, dvptr, _, dvstep = _result(dv, (n, narrow), dtype, device)
     dbias = None if bias is None else torch.empty(heads, buckets, dtype=torch.float32, device=device)
-    nbytes = _lib.pqt_attention_gradient_workspace(n, texts, heads, buckets)
+    nbytes = _lib.pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, buckets)
     ws = _workspace(nbytes, device)
     _check(_lib.pqt_attention_gradient(gptr, gstep, *inputs, optr, ostep, lse.data_ptr(), kind, n, heads, kv_heads, d, sptr, lptr, size, texts,
                                        d ** -0.5 if scale is None else scale, bptr, buckets, dptr, reach, 0 if grads else 1, dqptr, dqstep, dkptr, dkstep,
@@ -827,8 +827,8 @@ def pqt_rms_norm_gradient_workspace(rows, D):
     return int(_lib.pqt_rms_norm_gradient_workspace(rows, D))
 
 
-def pqt_attention_gradient_workspace(n, texts, heads, buckets):
-    return int(_lib.pqt_attention_gradient_workspace(n, texts, heads, buckets))
+def pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, buckets):
+    return int(_lib.pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, buckets))
 
 
 def last_error():

@@ -14,11 +14,12 @@ namespace pqt {
 namespace {
 
 constexpr int kMaxHeadD = 128;
-constexpr int kMaxReach = 512;
+constexpr int kMaxReach = 448;              // (the sums by distance of four wavefronts, 16 each, and the tiles of the widest heads fill LDS)
 constexpr int kMaxBuckets = 1024;
 constexpr int64_t kMaxRows = 0x7ffffff0;       // rows of a text are 32-bit numbers
 constexpr int64_t kMaxWorkgroups = 0xffffff;   // of up to 256 threads each, fewer than 2^32 in all
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLog2eRest = (float)(1.44269504088896340736 - (double)kLog2e);
 
 // ---- fragments -------------------------------------------------------------------------------------------------------
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -29,12 +30,15 @@ template <> struct FragmentOf<Bf16> {
 };
 template <> struct FragmentOf<Half> {
     typedef _Float16 type __attribute__((ext_vector_type(8)));
-    typedef u32x4 piece __attribute__((aligned(2)));           // 16 bytes at any element
+    typedef u32x4 piece __attribute__((aligned(2)));
 };
 template <> struct FragmentOf<float> {
     typedef float type __attribute__((ext_vector_type(8)));
     typedef u32x4 piece __attribute__((aligned(4)));
 };
+template <typename T> struct Stored { typedef T type; };
+template <> struct Stored<Bf16> { typedef __bf16 type; };
+template <> struct Stored<Half> { typedef _Float16 type; };
 template <typename T> using Fragment = typename FragmentOf<T>::type;
 
 __device__ __forceinline__ f32x4 multiply(Fragment<Bf16> a, Fragment<Bf16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -59,67 +63,106 @@ __device__ __forceinline__ Fragment<T> fragment_of(f32x4 lo, f32x4 hi) {
 }
 
 // ---- tiles of rows in LDS --------------------------------------------------------------------------------------------
-template <typename T> struct Stored { typedef T type; };
-template <> struct Stored<Bf16> { typedef __bf16 type; };
-template <> struct Stored<Half> { typedef _Float16 type; };
-
-// ROWS rows of up to DP values, 16 bytes further apart than they are long, so that 16 rows' 16-byte pieces begin in different banks
+// ROWS rows of DP values in pieces of 16 bytes, which lie permuted by the row's number, so that the rows whose pieces are read together fall into different
+// banks (the lanes that a 16-byte read serves together are 0-3, 12-15, 20-27 and so on: see the rows of a fragment).
 template <typename T, int ROWS, int DP>
 struct Tile {
     typedef typename Stored<T>::type S;
-    static constexpr int kPitch = DP + 16 / (int)sizeof(T);
-    S v[ROWS * kPitch];
+    typedef __attribute__((address_space(3))) S* Place;
+    static constexpr int E = 16 / (int)sizeof(T), kOfRow = DP / E, kSize = ROWS * DP;
+    Place v;                               // an LDS array of kSize values
 
+    static __device__ __forceinline__ int turn(int row) { return kOfRow % 16 == 0 ? row & 15 : kOfRow % 8 == 0 ? row & 7 : row & 8 ? 3 : 0; }
     // values 32 chunk + 8 (lane >> 4) .. + 7 of row row0 + (lane & 15)
     __device__ __forceinline__ Fragment<T> rows(int row0, int chunk) const {
-        const int lane = threadIdx.x & (kWave - 1);
-        const S* p = v + (row0 + (lane & 15)) * kPitch + chunk * 32 + (lane >> 4) * 8;
-        typedef Fragment<T> __attribute__((aligned(16))) F;
-        return *reinterpret_cast<const F*>(p);
+        const int lane = threadIdx.x & (kWave - 1), row = lane & 15, q = lane >> 4;
+        const Place p = v + (row0 + row) * DP;
+        typedef __attribute__((address_space(3))) const u32x4 P;
+        if constexpr (sizeof(T) == 2) {
+            return __builtin_bit_cast(Fragment<T>, *(P*)(p + ((chunk * 4 + q) ^ turn(row)) * E));
+        } else {
+            const u32x4 lo = *(P*)(p + ((chunk * 8 + q * 2) ^ turn(row)) * E), hi = *(P*)(p + ((chunk * 8 + q * 2 + 1) ^ turn(row)) * E);
+            return __builtin_shufflevector(__builtin_bit_cast(f32x4, lo), __builtin_bit_cast(f32x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+        }
     }
     // the transpose's: of column 16 block + (lane & 15), the rows row0 + place(e)
     __device__ __forceinline__ Fragment<T> columns(int row0, int block) const {
-        const int lane = threadIdx.x & (kWave - 1);
-        Fragment<T> f;
+        const int lane = threadIdx.x & (kWave - 1), col = lane & 15, q = lane >> 4;
         if constexpr (sizeof(T) == 2) {
             // sixteen lanes read 4 x 16 values, 8 bytes each, and get a column's four
             typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const S* p = v + (row0 + (lane >> 4) * 4 + ((lane & 15) >> 2)) * kPitch + block * 16 + (lane & 3) * 4;
             typedef short s16x8 __attribute__((ext_vector_type(8)));
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const int row = q * 4 + (col >> 2);
+            const Place p = v + (row0 + row) * DP + (((block * 2 + ((col >> 1) & 1)) ^ turn(row)) * E + (col & 1) * 4);
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * kPitch));
-            f = __builtin_bit_cast(Fragment<T>, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * DP));
+            return __builtin_bit_cast(Fragment<T>, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            const S* p = v + (row0 + (lane >> 4) * 4) * kPitch + block * 16 + (lane & 15);
+            Fragment<T> f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = p[(16 * (e >> 2) + (e & 3)) * kPitch];
+            for (int e = 0; e < 8; ++e) {
+                const int row = q * 4 + (e & 3);
+                f[e] = v[(row0 + 16 * (e >> 2) + row) * DP + ((block * 4 + (col >> 2)) ^ turn(row)) * E + (col & 3)];
+            }
+            return f;
         }
-        return f;
     }
 };
 
-// A thread's 16-byte pieces of the next tile, on their way while one is worked on.  WHOLE: rows are whole pieces; else a row's last piece is read
-// value by value.  Rows past `len` and values past `d` become zeros, whatever stands there in memory.
-template <typename T, int ROWS, int DP, int THREADS, bool WHOLE>
-struct Loads {
-    static constexpr int E = 16 / (int)sizeof(T), kOfRow = DP / E, kPieces = ROWS * kOfRow / THREADS;
+// What brings ROWS rows of d values, from row0 on, of the `len` at base to a tile, zeros in rows past len and in values past d: begin(), other work, finish(),
+// and a barrier.
+// DIRECT: straight to LDS, 16 bytes a lane; rows begin at multiples of 16 bytes and are whole pieces, and a tile spans less than 2^31 bytes (direct_rows()).
+// Else by registers; rows begin anywhere, and their last piece is read value by value.
+template <typename T, int ROWS, int DP, int THREADS, bool DIRECT>
+struct Loader {
+    typedef Tile<T, ROWS, DP> Into;
+    static constexpr int E = Into::E, kOfRow = Into::kOfRow, kPieces = ROWS * kOfRow / THREADS;
     static_assert(ROWS * kOfRow % THREADS == 0, "whole pieces for every thread");
-    u32x4 v[kPieces];
+    static constexpr uint32_t kNowhere = 0x80000000u;
     typedef typename FragmentOf<T>::piece Unaligned;
+    u32x4 v[DIRECT ? 1 : kPieces];
+    uint32_t off[DIRECT ? kPieces : 1];
 
-    __device__ __forceinline__ void fetch(const T* base, int64_t stride, int row0, int len, int d) {
+    __device__ __forceinline__ Loader(int64_t stride, int d) {
+        if constexpr (DIRECT) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int at = threadIdx.x + i * THREADS, row = row0 + at / kOfRow, c = at % kOfRow * E;
-            const T* p = base + (int64_t)min(row, len - 1) * stride;
-            if constexpr (WHOLE) {
-                v[i] = *reinterpret_cast<const Unaligned*>(p + min(c, d - E));
-                if (row >= len || c >= d) v[i] = u32x4{};
-            } else {
-                v[i] = u32x4{};
-                if (row < len && c < d) v[i] = piece(p + c, d - c);
+            for (int i = 0; i < kPieces; ++i) {
+                const int at = threadIdx.x % THREADS + i * THREADS, row = at / kOfRow, c = ((at % kOfRow) ^ Into::turn(row)) * E;
+                off[i] = c < d ? (uint32_t)((row * (int)stride + c) * (int)sizeof(T)) : kNowhere;
             }
+        }
+    }
+    __device__ __forceinline__ void begin(Into tile, const T* base, int64_t stride, int row0, int len, int d) {
+        if constexpr (DIRECT) {
+            typedef __attribute__((address_space(3))) void lds_bytes;
+            const uint64_t at = (uint64_t)(base + (int64_t)row0 * stride);
+            const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
+            const int rows = min(len - row0, ROWS);
+            const uint32_t bytes = __builtin_amdgcn_readfirstlane((uint32_t)(((rows - 1) * (int)stride + d) * (int)sizeof(T)));
+            const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), (short)0, bytes, 0x00027000);
+            const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x % THREADS) / kWave);
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+#if defined(__HIP_DEVICE_COMPILE__)                            // (the host's pass over this file takes 16 bytes for an error, and leaves the kernels out)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_bytes*)(tile.v + (i * THREADS + wave * kWave) * E), 16, off[i], 0, 0, 0);
+#else
+                (void)from, (void)wave;
+#endif
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int at = threadIdx.x % THREADS + i * THREADS, row = row0 + at / kOfRow, c = ((at % kOfRow) ^ Into::turn(at / kOfRow)) * E;
+                v[i] = u32x4{};
+                if (row < len && c < d) v[i] = piece(base + (int64_t)row * stride + c, d - c);
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(Into tile) {
+        if constexpr (DIRECT) __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0)
+        else {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) *(__attribute__((address_space(3))) u32x4*)(tile.v + (threadIdx.x % THREADS + i * THREADS) * E) = v[i];
         }
     }
     static __device__ __forceinline__ u32x4 piece(const T* p, int have) {
@@ -131,14 +174,10 @@ struct Loads {
             if (j < have) u.e[j] = p[j];
         return u.v;
     }
-    __device__ __forceinline__ void put(Tile<T, ROWS, DP>& tile) const {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int at = threadIdx.x + i * THREADS;
-            *reinterpret_cast<u32x4*>(tile.v + at / kOfRow * Tile<T, ROWS, DP>::kPitch + at % kOfRow * E) = v[i];
-        }
-    }
 };
+inline bool direct_rows(const void* p, int64_t stride, size_t element, int d) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * element % 16 == 0 && d * element % 16 == 0 && stride * (int64_t)element < (1 << 24);
+}
 
 // fragment `chunk` of a wavefront's own 16 rows row0 + (lane & 15), straight from memory
 template <typename T>
@@ -169,6 +208,7 @@ struct AttentionArgs {
     void* dv;
     float* delta;                          // heads x n
     float* parts;                          // workgroups x buckets
+    float* key_parts;                      // splits x heads of keys x n x (dk, dv), where the queries of a key are shared out
     int64_t q_stride, k_stride, v_stride, grad_stride, out_stride, dq_stride, dk_stride, dv_stride;
     int64_t n, texts;
     int64_t tiles;                         // workgroups of a head
@@ -208,7 +248,7 @@ __device__ __forceinline__ Rows rows_of_workgroup(const AttentionArgs& g, int64_
         hi = min(hi, lo + step);
         first = false;
     }
-    lo = __builtin_amdgcn_readfirstlane((int)lo);              // (texts are fewer than 2^31)
+    lo = __builtin_amdgcn_readfirstlane((int)lo);              // (rows and texts are fewer than 2^31)
     if (first) {                                               // rows before the first text
         r.begin = t * M;
         r.span = M;
@@ -216,12 +256,14 @@ __device__ __forceinline__ Rows rows_of_workgroup(const AttentionArgs& g, int64_
         return r;
     }
     const int64_t begin = start(lo), end = lo < g.texts ? max(start(lo + 1), begin) : g.n;
-    r.begin = begin;
-    r.span = (int)(end - begin);
     r.text = lo < g.texts;
-    r.len = r.text ? (g.lengths ? (int)min(max(number(g.lengths, g.wide, lo), (int64_t)0), end - begin) : r.span) : 0;
-    const int64_t row0 = (t - (begin / M + lo)) * M;
-    r.before = lo == 0 && row0 == 0 && g.clear ? begin % M : 0;
+    const int64_t have = r.text ? (g.lengths ? min(max(number(g.lengths, g.wide, lo), (int64_t)0), end - begin) : end - begin) : 0;
+    // (numbers of the workgroup, not of lanes)
+    r.begin = __builtin_amdgcn_readfirstlane((int)begin);
+    r.span = __builtin_amdgcn_readfirstlane((int)(end - begin));
+    r.len = __builtin_amdgcn_readfirstlane((int)have);
+    const int64_t row0 = (t - (r.begin / M + lo)) * M;
+    r.before = lo == 0 && row0 == 0 && g.clear ? r.begin % M : 0;
     r.mine = r.before > 0 || (row0 < r.span && (r.text || g.clear));
     r.row0 = (int)min(row0, (int64_t)r.span);
     return r;
@@ -255,11 +297,27 @@ __device__ __forceinline__ float bias_of(const AttentionArgs& g, int head, int d
     return fabsf(entry) < __builtin_inff() ? fmaxf(-kBiasTop, fminf(v, kBiasTop)) : v;
 }
 
-// Fills table[0 .. 2 W] with the bias of the distances -W .. W (SIGN -1: W .. -W)
-template <int SIGN, int THREADS>
-__device__ __forceinline__ void fill_bias(const AttentionArgs& g, int head, float* table, int W) {
-    for (int i = threadIdx.x; i <= 2 * W; i += THREADS) table[i] = bias_of(g, head, SIGN * (i - W));
-}
+// The bias of the distances -W .. W (SIGN -1: W .. -W) in LDS, four times, copy c shifted by c places: the four consecutive ones that a lane needs for a
+// result then begin at a multiple of 16 bytes in copy (first & 3), which is the same for all of a lane's.
+struct BiasTable {
+    float* v;
+    int pitch;
+    static __host__ __device__ __forceinline__ int pitch_of(int most) { return (2 * most + 4 + 63) / 64 * 64 + 16; }      // for W up to `most`
+    static size_t bytes(int most) { return 4 * sizeof(float) * pitch_of(most); }
+
+    template <int SIGN, int THREADS>
+    __device__ __forceinline__ void fill(const AttentionArgs& g, int head, int W) const {
+        for (int i = threadIdx.x % THREADS; i <= 2 * W; i += THREADS) {
+            const float b = bias_of(g, head, SIGN * (i - W));
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (i >= c) v[c * pitch + i - c] = b;
+        }
+    }
+    // where a lane finds places first, first + 1 .. (of which it reads four from multiples of four on)
+    __device__ __forceinline__ const float* from(int first) const { return v + (first & 3) * pitch + (first & ~3); }
+};
+__device__ __forceinline__ f32x4 four_of(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
 

@@ -57,137 +57,187 @@ template <int N> __device__ __forceinline__ float from_left(float v) { return dp
 
 // the logarithm of the sum as a power of two's; rows without weights have none
 __device__ __forceinline__ float power_of(float lse) { return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e; }
+// what weights are to be multiplied by for that power's rounding, the same for all of a row: 1 - rest * ln 2 (the rest is below 2^-13 even of sums of e^1000)
+__device__ __forceinline__ float rest_of_power(float lse) {
+    const float rest = __builtin_fmaf(lse, kLog2e, -(lse * kLog2e)) + lse * kLog2eRest;
+    return fabsf(lse) < __builtin_inff() ? __builtin_fmaf(rest, -kLn2, 1.0f) : 1.0f;
+}
 
-template <typename T, int DP, int NW, int BN, bool WHOLE>
-__global__ __launch_bounds__(NW* kWave) void attention_query_gradient_kernel(AttentionArgs g) {
-    constexpr int kThreads = NW * kWave, M = NW * 16, KC = DP / 32, DT = DP / 16, kCopies = NW * 4;
-    __shared__ __align__(16) Tile<T, BN, DP> ks[2], vs[2];
-    __shared__ float table[2 * (kMaxReach + M + BN) + 1];
-    __shared__ float far_sums[2][NW];
-    extern __shared__ float by_distance[];                     // kCopies x (2 W + 1)
+// Places of the bias table, and of the sums by distance, on either side: those of the tiles that are near, and sixteen for what is carried past one.
+template <int RT, int BN>
+__host__ __device__ constexpr int most_places(int reach) { return reach + RT * 16 + BN + 16; }
+
+template <typename T, int DP, int NW, int RT, int BN, bool DIRECT>
+__global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void attention_query_gradient_kernel(AttentionArgs g) {
+    constexpr int kThreads = NW * kWave, M = NW * RT * 16, KC = DP / 32, DT = DP / 16, kCopies = NW * 4;
+    typedef Tile<T, BN, DP> KeyTile;
+    __shared__ __align__(16) typename KeyTile::S k_0[KeyTile::kSize], k_1[KeyTile::kSize], v_0[KeyTile::kSize], v_1[KeyTile::kSize];
+    typedef typename KeyTile::Place Place;
+    const KeyTile k_even{(Place)k_0}, k_odd{(Place)k_1}, v_even{(Place)v_0}, v_odd{(Place)v_1};
+    __shared__ double far_sums[2][NW];
+    extern __shared__ __align__(16) float room[];              // the bias by distance, and kCopies x (2 W + 1) sums
+    const BiasTable table{room, BiasTable::pitch_of(most_places<RT, BN>(g.reach))};
+    float* const by_distance = room + 4 * table.pitch;
     int64_t t;
     int head;
     place_of_workgroup(g, g.heads, t, head);
     const Rows r = rows_of_workgroup<M>(g, t);
-    const int d = g.d, lane = threadIdx.x & (kWave - 1), col = lane & 15, quad = lane >> 4, wave = threadIdx.x / kWave;
+    const int d = g.d, lane = threadIdx.x & (kWave - 1), col = lane & 15, quad = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     T* dq = static_cast<T*>(g.dq) + (int64_t)head * d;
     float* parts = g.parts ? g.parts + (t * g.heads + head) * g.buckets : nullptr;
     if (r.mine && (r.before || !r.text)) {                     // rows of no text
         const int64_t from = r.before ? r.begin - r.before : r.begin + r.row0;
         clear_rows(dq, g.dq_stride, from, r.before && r.text ? r.begin : min(r.begin + r.row0 + M, r.begin + r.span), d);
     }
-    const int len = r.len, row0 = r.row0 + wave * 16, row = row0 + col;
+    const int len = r.len, row0 = r.row0 + wave * RT * 16;
     const bool work = r.mine && r.text && r.row0 < len;
     if (!work && parts)
         for (int b = threadIdx.x; b < g.buckets; b += kThreads) parts[b] = 0.0f;
     if (!r.mine || !r.text) return;
-    f32x4 sums[DT];
+    f32x4 sums[RT][DT];
+    Lift<T> lift[RT];
 #pragma unroll
-    for (int b = 0; b < DT; ++b) sums[b] = f32x4{};
-    Lift<T> lift;
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int b = 0; b < DT; ++b) sums[rt][b] = f32x4{};
     if (work) {
         const int kv = head / g.group;
         const T* k = static_cast<const T*>(g.k) + r.begin * g.k_stride + (int64_t)kv * d;
         const T* v = static_cast<const T*>(g.v) + r.begin * g.v_stride + (int64_t)kv * d;
         const float cs = g.scale * kLog2e;
-        const int W = min(g.reach, len) + M + BN, width = 2 * W + 1;
-        if (g.bias) fill_bias<1, kThreads>(g, head, table, W);
+        const int W = min(most_places<RT, BN>(g.reach), len + M + BN), width = 2 * W + 1;
+        Loader<T, BN, DP, kThreads, DIRECT> next_k(g.k_stride, d), next_v(g.v_stride, d);
+        next_k.begin(k_even, k, g.k_stride, 0, len, d);
+        next_v.begin(v_even, v, g.v_stride, 0, len, d);
+        if (g.bias) table.fill<1, kThreads>(g, head, W);
         if (parts)
             for (int i = threadIdx.x; i < kCopies * width; i += kThreads) by_distance[i] = 0.0f;
-        Fragment<T> q[KC], grad[KC];
-        float delta = 0.0f;
+        Fragment<T> q[RT][KC], grad[RT][KC];
+        float delta[RT], power[RT], factor[RT];
 #pragma unroll
-        for (int c = 0; c < KC; ++c) {
-            q[c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, row0, len, d, c);
-            grad[c] = rows_of_memory(static_cast<const T*>(g.grad) + r.begin * g.grad_stride + (int64_t)head * d, g.grad_stride, row0, len, d, c);
-            const f32x8 o = __builtin_convertvector(
-                rows_of_memory(static_cast<const T*>(g.out_in) + r.begin * g.out_stride + (int64_t)head * d, g.out_stride, row0, len, d, c), f32x8);
-            const f32x8 y = __builtin_convertvector(grad[c], f32x8) * o;
-            delta += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
-        }
-        delta = sum_of_groups(delta);
-        const float power = row < len ? power_of(g.lse_in[(int64_t)head * g.n + r.begin + row]) : __builtin_inff();
-        if (row < len && quad == 0) g.delta[(int64_t)head * g.n + r.begin + row] = delta;
-        float far_left = 0.0f, far_right = 0.0f;
-        Loads<T, BN, DP, kThreads, WHOLE> next_k, next_v;
-        next_k.fetch(k, g.k_stride, 0, len, d);
-        next_v.fetch(v, g.v_stride, 0, len, d);
-        next_k.put(ks[0]);
-        next_v.put(vs[0]);
-        __syncthreads();
-        const int steps = (len + BN - 1) / BN;
-        float* mine = by_distance + (wave * 4 + quad) * width + W;
-        for (int step = 0; step < steps; ++step) {
-            const int j0 = step * BN;
-            if (step + 1 < steps) {
-                next_k.fetch(k, g.k_stride, j0 + BN, len, d);
-                next_v.fetch(v, g.v_stride, j0 + BN, len, d);
+        for (int rt = 0; rt < RT; ++rt) {
+            const int row = row0 + rt * 16 + col;
+            delta[rt] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                q[rt][c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, row0 + rt * 16, len, d, c);
+                grad[rt][c] = rows_of_memory(static_cast<const T*>(g.grad) + r.begin * g.grad_stride + (int64_t)head * d, g.grad_stride, row0 + rt * 16, len, d, c);
+                const f32x8 o = __builtin_convertvector(
+                    rows_of_memory(static_cast<const T*>(g.out_in) + r.begin * g.out_stride + (int64_t)head * d, g.out_stride, row0 + rt * 16, len, d, c), f32x8);
+                const f32x8 y = __builtin_convertvector(grad[rt][c], f32x8) * o;
+                delta[rt] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
             }
-            const Tile<T, BN, DP>& kt = ks[step & 1];
-            const Tile<T, BN, DP>& vt = vs[step & 1];
-            const int low = j0 - (row0 + 15), high = j0 + BN - 1 - row0;
+            delta[rt] = sum_of_groups(delta[rt]);
+            const float lse = row < len ? g.lse_in[(int64_t)head * g.n + r.begin + row] : -__builtin_inff();
+            if (row < len && quad == 0) g.delta[(int64_t)head * g.n + r.begin + row] = delta[rt];
+            power[rt] = power_of(lse);
+            factor[rt] = rest_of_power(lse);
+            delta[rt] *= factor[rt];
+        }
+        double far_left = 0.0, far_right = 0.0;
+        next_k.finish(k_even);
+        next_v.finish(v_even);
+        __syncthreads();
+        const float before = g.bias ? table.v[0] : 0.0f, behind = g.bias ? table.v[2 * W] : 0.0f;
+        float* const mine = by_distance + (wave * 4 + quad) * width + W;
+        auto step = [&](int j0, KeyTile kt, KeyTile vt, KeyTile k_next, KeyTile v_next) __attribute__((always_inline)) {
+            const bool more = j0 + BN < len;
+            if (more) {
+                next_k.begin(k_next, k, g.k_stride, j0 + BN, len, d);
+                next_v.begin(v_next, v, g.v_stride, j0 + BN, len, d);
+            }
+            const int low = j0 - (row0 + RT * 16 - 1), high = j0 + BN - 1 - row0;
             const bool near = g.bias && high > -g.reach && low < g.reach;
-            const float far = g.bias && !near ? table[low >= g.reach ? 2 * W : 0] : 0.0f;
-            const float* at = table + (j0 + quad * 4 - row0 - col + W);
-            float carry = 0.0f;
+            const float far = low >= g.reach ? behind : before;
+            const float* at = table.from(j0 + quad * 4 - row0 - col + W);
+            float carry[RT], far_sum = 0.0f;
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) carry[rt] = 0.0f;
 #pragma unroll
             for (int c = 0; c < BN / 32; ++c) {
-                f32x4 s[2], dp[2];
+                f32x4 s[RT][2], dp[RT][2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    s[h] = f32x4{far, far, far, far};
-                    if (near) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[h][e] = at[c * 32 + h * 16 + e];
+                    for (int rt = 0; rt < RT; ++rt) {
+                        s[rt][h] = near ? four_of(at + c * 32 + h * 16 - rt * 16) : f32x4{far, far, far, far};
+                        dp[rt][h] = f32x4{};
                     }
-                    dp[h] = f32x4{};
 #pragma unroll
                     for (int x = 0; x < KC; ++x) {
-                        s[h] = multiply(kt.rows(c * 32 + h * 16, x), q[x], s[h]);
-                        dp[h] = multiply(vt.rows(c * 32 + h * 16, x), grad[x], dp[h]);
+                        const Fragment<T> f = kt.rows(c * 32 + h * 16, x);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) s[rt][h] = multiply(f, q[rt][x], s[rt][h]);
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float p = exp2_of(__builtin_fmaf(s[h][e], cs, -power));
-                        s[h][e] = p * (dp[h][e] - delta);
+                    for (int x = 0; x < KC; ++x) {
+                        const Fragment<T> f = vt.rows(c * 32 + h * 16, x);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) dp[rt][h] = multiply(f, grad[rt][x], dp[rt][h]);
                     }
-                    if (j0 + BN > len) {                       // places behind the text's last token
+                }
+                Fragment<T> ds[RT];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (j0 + c * 32 + h * 16 + quad * 4 + e >= len) s[h][e] = 0.0f;
-                    }
-                }
-                if (parts) {
-                    if (near) {
+                            s[rt][h][e] = exp2_of(__builtin_fmaf(s[rt][h][e], cs, -power[rt])) * __builtin_fmaf(dp[rt][h][e], factor[rt], -delta[rt]);
+                        if (j0 + c * 32 + 32 > len) {          // places behind the text's last token
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            // lane `col` gets what lies at key 16 c + 4 quad - col from its query on; what moved past the sixteen lanes is the next sixteen keys'
-                            const float sum = ((carry + s[h][0]) + from_right<1>(s[h][1])) + (from_right<2>(s[h][2]) + from_right<3>(s[h][3]));
-                            carry = from_left<15>(s[h][1]) + from_left<14>(s[h][2]) + from_left<13>(s[h][3]);
-                            mine[j0 + c * 32 + h * 16 + quad * 4 - row0 - col] += sum;
+                            for (int e = 0; e < 4; ++e)
+                                if (j0 + c * 32 + h * 16 + quad * 4 + e >= len) s[rt][h][e] = 0.0f;
                         }
-                    } else {
-                        const f32x4 both = s[0] + s[1];
-                        const float sum = (both[0] + both[1]) + (both[2] + both[3]);
-                        if (low >= g.reach) far_right += sum;
-                        else far_left += sum;
                     }
-                }
-                lift.apply(s[0], s[1], sums);
-                const Fragment<T> ds = fragment_of<T>(s[0], s[1]);
+                    if (parts) {
+                        if (near) {
 #pragma unroll
-                for (int b = 0; b < DT; ++b) sums[b] = multiply(kt.columns(c * 32, b), ds, sums[b]);
+                            for (int h = 0; h < 2; ++h) {
+                                // lane `col` gets what lies at key 16 c + 4 quad - col from its query on; what moved past the sixteen lanes is the next sixteen keys'
+                                const f32x4 v = s[rt][h];
+                                const float sum = ((carry[rt] + v[0]) + from_right<1>(v[1])) + (from_right<2>(v[2]) + from_right<3>(v[3]));
+                                carry[rt] = from_left<15>(v[1]) + from_left<14>(v[2]) + from_left<13>(v[3]);
+                                mine[j0 + c * 32 + h * 16 + quad * 4 - (row0 + rt * 16) - col] += sum;
+                            }
+                        } else {
+                            const f32x4 both = s[rt][0] + s[rt][1];
+                            far_sum += (both[0] + both[1]) + (both[2] + both[3]);
+                        }
+                    }
+                    lift[rt].apply(s[rt][0], s[rt][1], sums[rt]);
+                    ds[rt] = fragment_of<T>(s[rt][0], s[rt][1]);
+                }
+#pragma unroll
+                for (int b = 0; b < DT; ++b) {
+                    const Fragment<T> f = kt.columns(c * 32, b);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) sums[rt][b] = multiply(f, ds[rt], sums[rt][b]);
+                }
             }
-            if (parts && near) mine[j0 + BN + quad * 4 - row0 - col] += carry;
-            if (step + 1 < steps) {
-                next_k.put(ks[(step + 1) & 1]);
-                next_v.put(vs[(step + 1) & 1]);
+            if (parts) {
+                if (near) {
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) mine[j0 + BN + quad * 4 - (row0 + rt * 16) - col] += carry[rt];
+                } else if (low >= g.reach) far_right += far_sum;
+                else far_left += far_sum;
+            }
+            if (more) {
+                next_k.finish(k_next);
+                next_v.finish(v_next);
             }
             __syncthreads();
+        };
+        for (int j0 = 0; j0 < len; j0 += 2 * BN) {
+            step(j0, k_even, v_even, k_odd, v_odd);
+            if (j0 + BN < len) step(j0 + BN, k_odd, v_odd, k_even, v_even);
         }
         if (parts) {
-            far_left = group_sum<kWave>(far_left);
-            far_right = group_sum<kWave>(far_right);
+#pragma unroll
+            for (int off = 1; off < kWave; off *= 2) {
+                far_left += __shfl_xor(far_left, off, kWave);
+                far_right += __shfl_xor(far_right, off, kWave);
+            }
             if (lane == 0) {
                 far_sums[0][wave] = far_left;
                 far_sums[1][wave] = far_right;
@@ -204,161 +254,209 @@ __global__ __launch_bounds__(NW* kWave) void attention_query_gradient_kernel(Att
             const int first = g.distances[0], last = g.distances[2 * g.reach];
             for (int e = threadIdx.x; e < g.buckets * 8; e += kThreads) {
                 const int b = e >> 3;
-                float sum = 0.0f;
+                double sum = 0.0;
                 for (int i = e & 7; i < width; i += 8) sum += __float_as_int(by_distance[width + i]) == b ? by_distance[i] : 0.0f;
-                sum = group_sum<8>(sum);
+#pragma unroll
+                for (int off = 1; off < 8; off *= 2) sum += __shfl_xor(sum, off, kWave);
                 if ((e & 7) == 0) {
 #pragma unroll
-                    for (int w = 0; w < NW; ++w) sum += (first == b ? far_sums[0][w] : 0.0f) + (last == b ? far_sums[1][w] : 0.0f);
-                    parts[b] = sum;
+                    for (int w = 0; w < NW; ++w) sum += (first == b ? far_sums[0][w] : 0.0) + (last == b ? far_sums[1][w] : 0.0);
+                    parts[b] = (float)sum;
                 }
             }
         }
     }
-    if (row >= r.span) return;
-    const float by = g.scale * lift.inverse();
-    T* dst = dq + (r.begin + row) * g.dq_stride;
 #pragma unroll
-    for (int b = 0; b < DT; ++b) {
-        const int c = b * 16 + quad * 4;
-        store_piece<T, 4>(dst + c, row < len ? sums[b] * by : f32x4{}, d - c);
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = row0 + rt * 16 + col;
+        if (row >= r.span) continue;
+        const float by = g.scale * lift[rt].inverse();
+        T* dst = dq + (r.begin + row) * g.dq_stride;
+#pragma unroll
+        for (int b = 0; b < DT; ++b) {
+            const int c = b * 16 + quad * 4;
+            store_piece<T, 4>(dst + c, row < len ? sums[rt][b] * by : f32x4{}, d - c);
+        }
     }
 }
 
-template <typename T, int DP, int NW, int BN, bool WHOLE>
-__global__ __launch_bounds__(NW* kWave) void attention_key_gradient_kernel(AttentionArgs g) {
-    constexpr int kThreads = NW * kWave, M = NW * 16, KC = DP / 32, DT = DP / 16;
-    __shared__ __align__(16) Tile<T, BN, DP> qs[2], gs[2];
+template <typename T, int DP, int NW, int RT, int BN, bool DIRECT>
+__global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void attention_key_gradient_kernel(AttentionArgs g) {
+    constexpr int kThreads = NW * kWave, M = NW * RT * 16, KC = DP / 32, DT = DP / 16;
+    typedef Tile<T, BN, DP> QueryTile;
+    __shared__ __align__(16) typename QueryTile::S q_0[QueryTile::kSize], q_1[QueryTile::kSize], g_0[QueryTile::kSize], g_1[QueryTile::kSize];
+    typedef typename QueryTile::Place Place;
+    const QueryTile q_even{(Place)q_0}, q_odd{(Place)q_1}, g_even{(Place)g_0}, g_odd{(Place)g_1};
     __shared__ __align__(16) float powers[2][BN], deltas[2][BN];
-    __shared__ float table[2 * (kMaxReach + M + BN) + 1];
+    extern __shared__ __align__(16) float room[];
+    const BiasTable table{room, BiasTable::pitch_of(most_places<RT, BN>(g.reach))};
     int64_t t;
     int kv;
     place_of_workgroup(g, g.heads / g.group, t, kv);
     const Rows r = rows_of_workgroup<M>(g, t);
     if (!r.mine) return;
-    const int d = g.d, lane = threadIdx.x & (kWave - 1), col = lane & 15, quad = lane >> 4, wave = threadIdx.x / kWave;
+    const int d = g.d, lane = threadIdx.x & (kWave - 1), col = lane & 15, quad = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int split = blockIdx.y;
     T* dk = static_cast<T*>(g.dk) + (int64_t)kv * d;
     T* dv = static_cast<T*>(g.dv) + (int64_t)kv * d;
     if (r.before || !r.text) {                                 // rows of no text
         const int64_t from = r.before ? r.begin - r.before : r.begin + r.row0, to = r.before && r.text ? r.begin : min(r.begin + r.row0 + M, r.begin + r.span);
-        clear_rows(dk, g.dk_stride, from, to, d);
-        clear_rows(dv, g.dv_stride, from, to, d);
+        if (split == 0) {
+            clear_rows(dk, g.dk_stride, from, to, d);
+            clear_rows(dv, g.dv_stride, from, to, d);
+        }
         if (!r.text) return;
     }
-    const int len = r.len, row0 = r.row0 + wave * 16, row = row0 + col;
-    f32x4 k_sums[DT], v_sums[DT];
+    const int len = r.len, row0 = r.row0 + wave * RT * 16;
+    f32x4 k_sums[RT][DT], v_sums[RT][DT];
+    Lift<T> lift[RT];
 #pragma unroll
-    for (int b = 0; b < DT; ++b) {
-        k_sums[b] = f32x4{};
-        v_sums[b] = f32x4{};
-    }
-    Lift<T> lift;
-    if (r.row0 < len) {
-        const float cs = g.scale * kLog2e;
-        const int W = min(g.reach, len) + M + BN;
-        Fragment<T> k[KC], v[KC];
+    for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int c = 0; c < KC; ++c) {
-            k[c] = rows_of_memory(static_cast<const T*>(g.k) + r.begin * g.k_stride + (int64_t)kv * d, g.k_stride, row0, len, d, c);
-            v[c] = rows_of_memory(static_cast<const T*>(g.v) + r.begin * g.v_stride + (int64_t)kv * d, g.v_stride, row0, len, d, c);
+        for (int b = 0; b < DT; ++b) {
+            k_sums[rt][b] = f32x4{};
+            v_sums[rt][b] = f32x4{};
         }
-        Loads<T, BN, DP, kThreads, WHOLE> next_q, next_g;
+    // the tiles of all heads one after the other, of which this workgroup has from .. to - 1
+    const int steps = (len + BN - 1) / BN, total = steps * g.group;
+    const int from = (int)((int64_t)total * split / gridDim.y), to = (int)((int64_t)total * (split + 1) / gridDim.y);
+    if (r.row0 < len && from < to) {
+        const float cs = g.scale * kLog2e;
+        const int W = min(most_places<RT, BN>(g.reach), len + M + BN);
+        Fragment<T> k[RT][KC], v[RT][KC];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                k[rt][c] = rows_of_memory(static_cast<const T*>(g.k) + r.begin * g.k_stride + (int64_t)kv * d, g.k_stride, row0 + rt * 16, len, d, c);
+                v[rt][c] = rows_of_memory(static_cast<const T*>(g.v) + r.begin * g.v_stride + (int64_t)kv * d, g.v_stride, row0 + rt * 16, len, d, c);
+            }
+        Loader<T, BN, DP, kThreads, DIRECT> next_q(g.q_stride, d), next_g(g.grad_stride, d);
         float next_power = 0.0f, next_delta = 0.0f;
-        // the tiles of all heads one after the other
-        auto fetch = [&](int head, int i0) __attribute__((always_inline)) {
-            next_q.fetch(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, i0, len, d);
-            next_g.fetch(static_cast<const T*>(g.grad) + r.begin * g.grad_stride + (int64_t)head * d, g.grad_stride, i0, len, d);
+        auto fetch = [&](int at, QueryTile qt, QueryTile gt) __attribute__((always_inline)) {
+            const int head = kv * g.group + at / steps, i0 = at % steps * BN;
+            next_q.begin(qt, static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, i0, len, d);
+            next_g.begin(gt, static_cast<const T*>(g.grad) + r.begin * g.grad_stride + (int64_t)head * d, g.grad_stride, i0, len, d);
             if (threadIdx.x < BN) {
                 const int i = i0 + (int)threadIdx.x;
-                const int64_t at = (int64_t)head * g.n + r.begin + min(i, len - 1);
-                next_power = i < len ? power_of(g.lse_in[at]) : __builtin_inff();
-                next_delta = i < len ? g.delta[at] : 0.0f;
+                const int64_t place = (int64_t)head * g.n + r.begin + min(i, len - 1);
+                next_power = i < len ? power_of(g.lse_in[place]) : __builtin_inff();
+                next_delta = i < len ? g.delta[place] : 0.0f;
             }
         };
-        auto put = [&](int half) __attribute__((always_inline)) {
-            next_q.put(qs[half]);
-            next_g.put(gs[half]);
+        auto arrive = [&](int half, QueryTile qt, QueryTile gt) __attribute__((always_inline)) {
+            next_q.finish(qt);
+            next_g.finish(gt);
             if (threadIdx.x < BN) {
                 powers[half][threadIdx.x] = next_power;
                 deltas[half][threadIdx.x] = next_delta;
             }
         };
-        const int steps = (len + BN - 1) / BN;
-        int head = kv * g.group, half = 0;
-        fetch(head, 0);
-        put(0);
-        for (int h = 0; h < g.group; ++h, ++head) {
-            if (g.bias) fill_bias<-1, kThreads>(g, head, table, W);    // (the last barrier stands after the last reading of it)
-            __syncthreads();
-            for (int step = 0; step < steps; ++step, half ^= 1) {
-                const int i0 = step * BN;
-                const bool more = step + 1 < steps || h + 1 < g.group;
-                if (step + 1 < steps) fetch(head, i0 + BN);
-                else if (more) fetch(head + 1, 0);
-                const Tile<T, BN, DP>& qt = qs[half];
-                const Tile<T, BN, DP>& gt = gs[half];
-                const int low = row0 - (i0 + BN - 1), high = row0 + 15 - i0;       // distances key - query
-                const bool near = g.bias && high > -g.reach && low < g.reach;
-                const float far = g.bias && !near ? table[low >= g.reach ? 0 : 2 * W] : 0.0f;
-                const float* at = table + (i0 + quad * 4 - row0 - col + W);
-#pragma unroll
-                for (int c = 0; c < BN / 32; ++c) {
-                    f32x4 s[2], dp[2];
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int i = c * 32 + x * 16;
-                        s[x] = f32x4{far, far, far, far};
-                        if (near) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) s[x][e] = at[i + e];
-                        }
-                        dp[x] = f32x4{};
-#pragma unroll
-                        for (int y = 0; y < KC; ++y) {
-                            s[x] = multiply(qt.rows(i, y), k[y], s[x]);
-                            dp[x] = multiply(gt.rows(i, y), v[y], dp[x]);
-                        }
-                        const f32x4 power = *reinterpret_cast<const f32x4*>(&powers[half][i + quad * 4]);
-                        const f32x4 delta = *reinterpret_cast<const f32x4*>(&deltas[half][i + quad * 4]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            s[x][e] = exp2_of(__builtin_fmaf(s[x][e], cs, WeightLift<T>::log2 - power[e]));
-                            dp[x][e] = s[x][e] * (dp[x][e] - delta[e]);
-                        }
-                    }
-                    const Fragment<T> p = fragment_of<T>(s[0], s[1]);
-                    lift.apply(dp[0], dp[1], k_sums);
-                    const Fragment<T> ds = fragment_of<T>(dp[0], dp[1]);
-#pragma unroll
-                    for (int b = 0; b < DT; ++b) {
-                        v_sums[b] = multiply(gt.columns(c * 32, b), p, v_sums[b]);
-                        k_sums[b] = multiply(qt.columns(c * 32, b), ds, k_sums[b]);
-                    }
-                }
-                if (more) put(half ^ 1);
+        auto step = [&](int at, int half, QueryTile qt, QueryTile gt, QueryTile q_next, QueryTile g_next) __attribute__((always_inline)) {
+            const int i0 = at % steps * BN;
+            if (g.bias && (i0 == 0 || at == from)) {           // another head's (the last barrier stands after the last reading of the one before)
+                table.fill<-1, kThreads>(g, kv * g.group + at / steps, W);
                 __syncthreads();
             }
+            const bool more = at + 1 < to;
+            if (more) fetch(at + 1, q_next, g_next);
+            const int low = row0 - (i0 + BN - 1), high = row0 + RT * 16 - 1 - i0;      // distances key - query
+            const bool near = g.bias && high > -g.reach && low < g.reach;
+            const float far = g.bias ? table.v[low >= g.reach ? 0 : 2 * W] : 0.0f;
+            const float* bias_at = table.from(i0 + quad * 4 - row0 - col + W);
+#pragma unroll
+            for (int c = 0; c < BN / 32; ++c) {
+                f32x4 s[RT][2], dp[RT][2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int i = c * 32 + x * 16;
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        s[rt][x] = near ? four_of(bias_at + i - rt * 16) : f32x4{far, far, far, far};
+                        dp[rt][x] = f32x4{};
+                    }
+#pragma unroll
+                    for (int y = 0; y < KC; ++y) {
+                        const Fragment<T> f = qt.rows(i, y);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) s[rt][x] = multiply(f, k[rt][y], s[rt][x]);
+                    }
+#pragma unroll
+                    for (int y = 0; y < KC; ++y) {
+                        const Fragment<T> f = gt.rows(i, y);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) dp[rt][x] = multiply(f, v[rt][y], dp[rt][x]);
+                    }
+                    const f32x4 power = *reinterpret_cast<const f32x4*>(&powers[half][i + quad * 4]);
+                    const f32x4 delta = *reinterpret_cast<const f32x4*>(&deltas[half][i + quad * 4]);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            s[rt][x][e] = exp2_of(__builtin_fmaf(s[rt][x][e], cs, WeightLift<T>::log2 - power[e]));
+                            dp[rt][x][e] = s[rt][x][e] * (dp[rt][x][e] - delta[e]);
+                        }
+                }
+                Fragment<T> p[RT], ds[RT];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    p[rt] = fragment_of<T>(s[rt][0], s[rt][1]);
+                    lift[rt].apply(dp[rt][0], dp[rt][1], k_sums[rt]);
+                    ds[rt] = fragment_of<T>(dp[rt][0], dp[rt][1]);
+                }
+#pragma unroll
+                for (int b = 0; b < DT; ++b) {
+                    const Fragment<T> fg = gt.columns(c * 32, b), fq = qt.columns(c * 32, b);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        v_sums[rt][b] = multiply(fg, p[rt], v_sums[rt][b]);
+                        k_sums[rt][b] = multiply(fq, ds[rt], k_sums[rt][b]);
+                    }
+                }
+            }
+            if (more) arrive(half ^ 1, q_next, g_next);
+            __syncthreads();
+        };
+        fetch(from, q_even, g_even);
+        arrive(0, q_even, g_even);
+        __syncthreads();
+        for (int at = from; at < to; at += 2) {
+            step(at, 0, q_even, g_even, q_odd, g_odd);
+            if (at + 1 < to) step(at + 1, 1, q_odd, g_odd, q_even, g_even);
         }
     }
-    if (row >= r.span) return;
-    const float by = g.scale * lift.inverse() * WeightLift<T>::inverse;
-    T* to_k = dk + (r.begin + row) * g.dk_stride;
-    T* to_v = dv + (r.begin + row) * g.dv_stride;
 #pragma unroll
-    for (int b = 0; b < DT; ++b) {
-        const int c = b * 16 + quad * 4;
-        store_piece<T, 4>(to_k + c, row < len ? k_sums[b] * by : f32x4{}, d - c);
-        store_piece<T, 4>(to_v + c, row < len ? v_sums[b] * WeightLift<T>::inverse : f32x4{}, d - c);
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = row0 + rt * 16 + col;
+        if (row >= r.span) continue;
+        const float by = g.scale * lift[rt].inverse() * WeightLift<T>::inverse;
+        if (gridDim.y > 1) {                                   // this split's part of the sums
+            float* part = g.key_parts + (((int64_t)split * (g.heads / g.group) + kv) * g.n + r.begin + row) * (2 * DP) + quad * 4;
+#pragma unroll
+            for (int b = 0; b < DT; ++b) {
+                *reinterpret_cast<f32x4*>(part + b * 16) = k_sums[rt][b] * by;
+                *reinterpret_cast<f32x4*>(part + DP + b * 16) = v_sums[rt][b] * WeightLift<T>::inverse;
+            }
+            continue;
+        }
+        T* to_k = dk + (r.begin + row) * g.dk_stride;
+        T* to_v = dv + (r.begin + row) * g.dv_stride;
+#pragma unroll
+        for (int b = 0; b < DT; ++b) {
+            const int c = b * 16 + quad * 4;
+            store_piece<T, 4>(to_k + c, row < len ? k_sums[rt][b] * by : f32x4{}, d - c);
+            store_piece<T, 4>(to_v + c, row < len ? v_sums[rt][b] * WeightLift<T>::inverse : f32x4{}, d - c);
+        }
     }
 }
 
-// Sums over rows of `columns` values, in a fixed order: 64 columns a workgroup, its sixteen wavefronts a part of the rows each, of every gridDim.y-th
+// Sums over rows of `columns` values, in 64 bits and a fixed order: 64 columns a workgroup, its sixteen wavefronts a part of the rows each, of every gridDim.y-th
 // run of rows; out: gridDim.y x columns.
 __global__ __launch_bounds__(1024) void join_kernel(const float* parts, int64_t rows, int64_t columns, float* out) {
-    __shared__ float sums[16][kWave];
+    __shared__ double sums[16][kWave];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int64_t c = (int64_t)blockIdx.x * kWave + lane, per = (rows + gridDim.y - 1) / gridDim.y, from = blockIdx.y * per, to = min(from + per, rows);
-    float s = 0.0f;
+    double s = 0.0;
     if (c < columns)
         for (int64_t r = from + wave; r < to; r += 16 * 8) {   // eight rows on their way
             float v[8];
@@ -372,20 +470,55 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* parts, int64_t 
     if (wave || c >= columns) return;
 #pragma unroll
     for (int w = 1; w < 16; ++w) s += sums[w][lane];
-    out[blockIdx.y * columns + c] = s;
+    out[blockIdx.y * columns + c] = (float)s;
 }
 
-// Where the workspace's parts begin, in floats.
-struct Room { int64_t delta, parts, joined, all; };
-inline int gradient_rows(int64_t n, int64_t texts, int heads) { return rows_of_a_workgroup(n, texts, heads) == 16 ? 16 : 64; }
-inline int64_t runs_of(int64_t tiles) { return std::min<int64_t>(64, std::max<int64_t>(1, tiles / 256)); }
-inline Room room_of(int64_t n, int64_t texts, int heads, int buckets) {
-    const int64_t tiles = n / gradient_rows(n, texts, heads) + texts + 1, columns = (int64_t)heads * buckets;
-    Room r{};
-    r.parts = (heads * n + 3) / 4 * 4;
-    r.joined = r.parts + (tiles * columns + 3) / 4 * 4;
-    r.all = r.joined + (runs_of(tiles) > 1 ? runs_of(tiles) * columns : 0);
-    return r;
+// dk and dv from the parts of shared out queries: a wavefront a row, in the splits' order
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void key_join_kernel(AttentionArgs g, int splits) {
+    int64_t t;
+    int kv;
+    const int kv_heads = g.heads / g.group;
+    place_of_workgroup(g, kv_heads, t, kv);
+    const Rows r = rows_of_workgroup<64>(g, t);
+    if (!r.mine || !r.text) return;
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int row = r.row0 + threadIdx.x / kWave; row < min(r.row0 + 64, r.span); row += 256 / kWave) {
+        for (int c = lane * 4; c < 2 * DP; c += kWave * 4) {
+            f32x4 sum = f32x4{};
+            if (row < r.len)
+                for (int s = 0; s < splits; ++s)
+                    sum = sum + *reinterpret_cast<const f32x4*>(g.key_parts + (((int64_t)s * kv_heads + kv) * g.n + r.begin + row) * (2 * DP) + c);
+            const int x = c < DP ? c : c - DP;
+            T* to = c < DP ? static_cast<T*>(g.dk) + (r.begin + row) * g.dk_stride : static_cast<T*>(g.dv) + (r.begin + row) * g.dv_stride;
+            store_piece<T, 4>(to + (int64_t)kv * g.d + x, sum, g.d - x);
+        }
+    }
+}
+
+// Workgroups' rows and shares, by the sizes alone, and where the workspace's parts begin, in floats.
+struct GradientPlan {
+    int rows;                              // of a workgroup
+    int splits;                            // workgroups that share out a key's queries
+    int runs;                              // of the bias' parts that are joined side by side
+    int64_t tiles, parts, key_parts, joined, all;
+};
+inline GradientPlan gradient_plan(int64_t n, int64_t texts, int heads, int kv_heads, int d, int buckets) {
+    GradientPlan p{};
+    p.rows = rows_of_a_workgroup(n, texts, heads);
+    p.tiles = n / p.rows + texts + 1;
+    // few workgroups have keys: up to eight share the queries, of which each has four tiles at least
+    const int64_t busy = std::max<int64_t>(1, n / p.rows) * kv_heads, of_a_key = (texts ? n / texts : 0) * (heads / kv_heads) / (4 * 64);
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, of_a_key), 768 / busy));
+    p.runs = (int)std::min<int64_t>(64, std::max<int64_t>(1, p.tiles / 256));
+    const int64_t columns = (int64_t)heads * buckets;
+    int width = 0;
+    with_head(d, [&](auto dp) { width = dp.value; });
+    p.parts = (heads * n + 3) / 4 * 4;
+    p.key_parts = p.parts + (p.tiles * columns + 3) / 4 * 4;
+    p.joined = p.key_parts + (p.splits > 1 ? (int64_t)p.splits * kv_heads * n * 2 * width : 0);
+    p.all = p.joined + (p.runs > 1 ? p.runs * columns : 0);
+    return p;
 }
 
 }  // namespace
@@ -393,10 +526,10 @@ inline Room room_of(int64_t n, int64_t texts, int heads, int buckets) {
 
 extern "C" {
 
-size_t pqt_attention_gradient_workspace(int64_t n, int64_t texts, int heads, int buckets) {
+size_t pqt_attention_gradient_workspace(int64_t n, int64_t texts, int heads, int kv_heads, int d, int buckets) {
     using namespace pqt;
-    if (n < 1 || texts < 0 || heads < 1 || n > kMaxRows || texts > kMaxRows || heads > 65535) return 0;
-    return (size_t)room_of(n, texts, heads, std::max(0, std::min(buckets, kMaxBuckets))).all * sizeof(float);
+    if (n < 1 || texts < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || d < 1 || d > kMaxHeadD || n > kMaxRows || texts > kMaxRows || heads > 65535) return 0;
+    return (size_t)gradient_plan(n, texts, heads, kv_heads, d, std::max(0, std::min(buckets, kMaxBuckets))).all * sizeof(float);
 }
 
 int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
@@ -416,7 +549,7 @@ int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q,
     if (!aligned_to(grad, eb) || !aligned_to(q, eb) || !aligned_to(k, eb) || !aligned_to(v, eb) || !aligned_to(out, eb) || !aligned_to(dq, eb) || !aligned_to(dk, eb) ||
         !aligned_to(dv, eb) || !aligned_to(lse, 4) || !aligned_to(dbias, 4))
         return fail(PQT_EINVAL, "pqt_attention_gradient: a pointer is not aligned to its element");
-    const size_t need = pqt_attention_gradient_workspace(n, texts, heads, dbias ? buckets : 0);
+    const size_t need = pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, dbias ? buckets : 0);
     if (need && (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)))
         return fail(PQT_EINVAL, "pqt_attention_gradient: workspace of %zu bytes, aligned to 16, needed (%zu given)", need, workspace_bytes);
     if (n == 0 && !dbias) return PQT_OK;
@@ -426,7 +559,7 @@ int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q,
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const int64_t columns = (int64_t)heads * buckets;
     if (n > 0) {
-        const Room room = room_of(n, texts, heads, dbias ? buckets : 0);
+        const GradientPlan plan = gradient_plan(n, texts, heads, kv_heads, d, dbias ? buckets : 0);
         float* const at = static_cast<float*>(workspace);
         g.grad = grad;
         g.q = q;
@@ -438,7 +571,8 @@ int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q,
         g.dk = dk;
         g.dv = dv;
         g.delta = at;
-        g.parts = dbias ? at + room.parts : nullptr;
+        g.parts = dbias ? at + plan.parts : nullptr;
+        g.key_parts = at + plan.key_parts;
         g.grad_stride = grad_stride;
         g.q_stride = q_stride;
         g.k_stride = k_stride;
@@ -448,32 +582,47 @@ int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q,
         g.dk_stride = dk_stride;
         g.dv_stride = dv_stride;
         g.clear = clear;
-        const int rows = gradient_rows(n, texts, heads);
-        g.tiles = n / rows + texts + 1;
-        const unsigned query_blocks = (unsigned)(g.tiles * heads), key_blocks = (unsigned)(g.tiles * kv_heads);
+        g.tiles = plan.tiles;
+        const unsigned query_blocks = (unsigned)(g.tiles * heads);
         with_type(type, [&](auto t) {
             typedef decltype(t) T;
-            const bool whole = d % (16 / (int)sizeof(T)) == 0;
+            const bool by_query = direct_rows(k, k_stride, sizeof(T), d) && direct_rows(v, v_stride, sizeof(T), d);
+            const bool by_key = direct_rows(q, q_stride, sizeof(T), d) && direct_rows(grad, grad_stride, sizeof(T), d);
             with_head(d, [&](auto dp) {
                 constexpr int DP = dp.value, kRows = sizeof(T) == 4 && DP > 64 ? 32 : 64;
-                auto launch = [&](auto queries, auto keys, int waves, int step) {
-                    const size_t bytes = dbias ? sizeof(float) * waves * 4 * (2 * (reach + waves * 16 + step) + 1) : 0;
-                    hipLaunchKernelGGL(queries, dim3(query_blocks), dim3(waves * kWave), bytes, st, g);
-                    hipLaunchKernelGGL(keys, dim3(key_blocks), dim3(waves * kWave), 0, st, g);
+                auto launch = [&](auto queries, int waves, int most) {
+                    const size_t table = bias ? BiasTable::bytes(most) : 0, sums = dbias ? sizeof(float) * waves * 4 * (2 * most + 1) : 0;
+                    hipLaunchKernelGGL(queries, dim3(query_blocks), dim3(waves * kWave), table + sums, st, g);
                 };
-                if (rows == 16)
-                    whole ? launch(attention_query_gradient_kernel<T, DP, 1, 32, true>, attention_key_gradient_kernel<T, DP, 1, 32, true>, 1, 32)
-                          : launch(attention_query_gradient_kernel<T, DP, 1, 32, false>, attention_key_gradient_kernel<T, DP, 1, 32, false>, 1, 32);
-                else
-                    whole ? launch(attention_query_gradient_kernel<T, DP, 4, kRows, true>, attention_key_gradient_kernel<T, DP, 4, kRows, true>, 4, kRows)
-                          : launch(attention_query_gradient_kernel<T, DP, 4, kRows, false>, attention_key_gradient_kernel<T, DP, 4, kRows, false>, 4, kRows);
+                auto launch_keys = [&](auto keys, int waves, int rows, int most) {
+                    AttentionArgs k = g;
+                    k.tiles = n / rows + texts + 1;
+                    hipLaunchKernelGGL(keys, dim3((unsigned)(k.tiles * kv_heads), (unsigned)plan.splits), dim3(waves * kWave), bias ? BiasTable::bytes(most) : 0, st, k);
+                };
+                auto of = [&](auto waves, auto rt, auto step) {
+                    // (two rows' sums of keys and values of the widest heads leave no registers: 222 spilled)
+                    constexpr int NW = waves.value, RT = rt.value, BN = step.value, KRT = sizeof(T) * DP > (sizeof(T) == 2 ? 192 : 128) ? 1 : RT;
+                    const int most = most_places<RT, BN>(reach), key_most = most_places<KRT, BN>(reach);
+                    if (by_query) launch(attention_query_gradient_kernel<T, DP, NW, RT, BN, true>, NW, most);
+                    else launch(attention_query_gradient_kernel<T, DP, NW, RT, BN, false>, NW, most);
+                    if (by_key) launch_keys(attention_key_gradient_kernel<T, DP, NW, KRT, BN, true>, NW, NW * KRT * 16, key_most);
+                    else launch_keys(attention_key_gradient_kernel<T, DP, NW, KRT, BN, false>, NW, NW * KRT * 16, key_most);
+                };
+                if (plan.rows == 16) of(Width<1>{}, Width<1>{}, Width<32>{});
+                else if (plan.rows == 64) of(Width<4>{}, Width<1>{}, Width<kRows>{});
+                else of(Width<4>{}, Width<2>{}, Width<kRows>{});
+                if (plan.splits > 1) {
+                    AttentionArgs j = g;
+                    j.tiles = n / 64 + texts + 1;
+                    hipLaunchKernelGGL((key_join_kernel<T, DP>), dim3((unsigned)(j.tiles * kv_heads)), dim3(256), 0, st, j, plan.splits);
+                }
             });
         });
         HIP_TRY(hipGetLastError());
         if (dbias) {
-            const unsigned runs = (unsigned)runs_of(g.tiles), across = (unsigned)((columns + kWave - 1) / kWave);
-            hipLaunchKernelGGL(join_kernel, dim3(across, runs), dim3(1024), 0, st, g.parts, g.tiles, columns, runs > 1 ? at + room.joined : dbias);
-            if (runs > 1) hipLaunchKernelGGL(join_kernel, dim3(across), dim3(1024), 0, st, at + room.joined, (int64_t)runs, columns, dbias);
+            const unsigned across = (unsigned)((columns + kWave - 1) / kWave);
+            hipLaunchKernelGGL(join_kernel, dim3(across, (unsigned)plan.runs), dim3(1024), 0, st, g.parts, g.tiles, columns, plan.runs > 1 ? at + plan.joined : dbias);
+            if (plan.runs > 1) hipLaunchKernelGGL(join_kernel, dim3(across), dim3(1024), 0, st, at + plan.joined, (int64_t)plan.runs, columns, dbias);
             HIP_TRY(hipGetLastError());
         }
     } else {

@@ -281,8 +281,8 @@ def check_attention(s, out, lse):
 ATTENTION = [  # lengths, heads, heads of keys, d, type, buckets, reach, padded to, pad, ids, rows behind
     ([1], 1, 1, 1, "f32", 0, 0, 0, 0, 64, 0), ([7], 16, 16, 64, "bf16", 32, 128, 0, 0, 64, 0), ([3, 0, 1, 33, 17, 0], 3, 1, 33, "f16", 5, 3, 0, 5, 32, 9),
     ([16, 32, 15, 31, 0], 4, 2, 64, "bf16", 32, 16, 40, 0, 64, 0), ([48, 5, 20], 8, 8, 64, "f32", 32, 128, 0, 8, 64, 0), ([129], 2, 2, 128, "f32", 20, 40, 0, 0, 32, 1),
-    ([65, 200, 1], 2, 1, 96, "bf16", 64, 500, 201, 3, 64, 0), ([300], 4, 4, 80, "f16", 32, 128, 0, 0, 64, 0), ([513], 1, 1, 7, "bf16", 8, 1, 0, 1, 64, 2),
-    ([100, 90, 0, 200, 130, 1, 99, 70, 60, 55, 300], 16, 8, 64, "bf16", 32, 128, 0, 0, 64, 5), ([400, 500, 700], 12, 3, 32, "f16", 2, 512, 0, 8, 32, 0),
+    ([65, 200, 1], 2, 1, 96, "bf16", 64, 448, 201, 3, 64, 0), ([300], 4, 4, 80, "f16", 32, 128, 0, 0, 64, 0), ([513], 1, 1, 7, "bf16", 8, 1, 0, 1, 64, 2),
+    ([100, 90, 0, 200, 130, 1, 99, 70, 60, 55, 300], 16, 8, 64, "bf16", 32, 128, 0, 0, 64, 5), ([400, 500, 700], 12, 3, 32, "f16", 2, 448, 0, 8, 32, 0),
     ([333, 444, 260], 16, 16, 100, "bf16", 32, 32, 500, 0, 64, 0), ([1025, 40], 16, 4, 128, "f32", 32, 128, 0, 0, 64, 0), ([777, 800], 12, 1, 96, "f16", 0, 0, 0, 1, 64, 100),
     ([1300], 16, 2, 97, "bf16", 16, 7, 0, 0, 64, 0), ([900, 200], 16, 16, 31, "f32", 33, 100, 0, 0, 64, 0), ([5000], 16, 4, 64, "bf16", 32, 128, 0, 0, 64, 3),
     ([2100, 2050], 16, 16, 128, "f16", 32, 128, 2200, 0, 64, 0), ([4500], 16, 1, 30, "f32", 32, 200, 0, 3, 32, 0), ([4300], 16, 8, 96, "bf16", 0, 0, 0, 0, 64, 0)]
@@ -308,7 +308,7 @@ def check_gradient(s, grad, out, lse, got):
     zeros = lambda heads: torch.zeros(s.n, heads * s.d, dtype=torch.float64, device=dev())               # noqa: E731
     want, tol = [zeros(s.heads), zeros(s.kv), zeros(s.kv)], [zeros(s.heads), zeros(s.kv), zeros(s.kv)]
     buckets = s.bias.shape[1] if s.bias is not None else 1
-    want_b, tol_b = torch.zeros(s.heads, buckets + 1, dtype=torch.float64, device=dev()), torch.zeros(s.heads, buckets + 1, dtype=torch.float64, device=dev())
+    want_b, tol_b = torch.zeros(s.heads, buckets, dtype=torch.float64, device=dev()), torch.zeros(s.heads, buckets, dtype=torch.float64, device=dev())
     unit = weight_unit(s.q.dtype)
     small = 2.0 ** -32 if s.q.dtype == torch.float16 else 0.0      # f16 numbers end that far below a row's largest
     scale = torch.tensor(s.scale, dtype=torch.float32).double().item()
@@ -341,16 +341,18 @@ def check_gradient(s, grad, out, lse, got):
             want[2][rows, shared] += p.t() @ g
             tol[2][rows, shared] += (p * (rel + unit * 1.01 + add * s.heads / s.kv) + small + 2.0 ** -126).t() @ g.abs()
             if bucket is not None:
-                slot = torch.where((bucket >= 0) & (bucket < buckets), bucket, buckets).flatten()
-                want_b[head].index_add_(0, slot, ds.flatten())
                 # a sum over at most m places of a diagonal, the texts' and the distances' sums: no term is added to more than m + 2 reach + 64 + texts
-                tol_b[head].index_add_(0, slot, (off_ds + ds.abs() * (m + 2 * s.reach + 64 + len(s.of)) * U).flatten())
+                off_sum = off_ds + ds.abs() * (m + 2 * s.reach + 64 + len(s.of)) * U
+                for b in range(buckets):
+                    mine = bucket == b
+                    want_b[head, b] += torch.where(mine, ds, 0.0).sum()
+                    tol_b[head, b] += torch.where(mine, off_sum, 0.0).sum()
     for name, a, w, e in zip(("dq", "dk", "dv"), got, want, tol):
         within(a, w, e, name)
     if s.bias is None:
         assert dbias is None
     else:
-        within(dbias, want_b[:, :buckets], tol_b[:, :buckets], "dbias")
+        within(dbias, want_b, tol_b, "dbias")
 
 
 @gpu
@@ -600,7 +602,7 @@ def test_gradients_of_a_broadcast_bias():
 
 
 # ---- buckets ---------------------------------------------------------------------------------------------------------
-@pytest.mark.parametrize("buckets,far,both", [(32, 128, True), (64, 512, True), (2, 1, True), (20, 100, True), (32, 128, False), (5, 17, False), (2, 3, False), (1024, 512, True), (8, 3, True)])
+@pytest.mark.parametrize("buckets,far,both", [(32, 128, True), (64, 448, True), (2, 1, True), (20, 100, True), (32, 128, False), (5, 17, False), (2, 3, False), (1024, 448, True), (8, 3, True)])
 def test_distance_buckets(buckets, far, both):
     """Against the definition in whole numbers: log(t / near) / log(far / near) * rest >= step where (t / near)^rest >= (far / near)^step."""
     side = buckets // 2 if both else buckets
@@ -623,7 +625,7 @@ def test_distance_buckets(buckets, far, both):
 
 
 def test_refusals_of_distance_buckets():
-    for args in ((1, 10), (3, 10, True), (32, 0), (32, 513), (1026, 300), (64, 10), (0, 5), (-2, 5)):
+    for args in ((1, 10), (3, 10, True), (32, 0), (32, 449), (1026, 300), (64, 10), (0, 5), (-2, 5)):
         with pytest.raises(pqt.PqtError) as e:
             pqt.pqt_distance_buckets(*args)
         assert e.value.code == pqt.PQT_EINVAL
@@ -785,7 +787,7 @@ def test_refusals_of_the_library(library_without_gpu):
     for bad in layout:
         refused(lib.pqt_attention, *call(**bad))
     wide = dict(qs=1000, ks=1000, vs=1000, os=1000)
-    beyond = (dict(d=129, **wide), dict(buckets=1025), dict(reach=513), dict(n=1 << 31), dict(texts=1 << 31), dict(n=1 << 30))
+    beyond = (dict(d=129, **wide), dict(buckets=1025), dict(reach=449), dict(n=1 << 31), dict(texts=1 << 31), dict(n=1 << 30))
     for bad in beyond:
         refused(lib.pqt_attention, *call(**bad), code=pqt.PQT_EUNSUPPORTED)
     assert lib.pqt_attention(*call(n=0, starts=None, q=None)) == pqt.PQT_OK
@@ -803,8 +805,9 @@ def test_refusals_of_the_library(library_without_gpu):
     assert lib.pqt_attention_gradient(*call(n=0, db=None)) == pqt.PQT_OK
     for fine in (dict(), dict(lengths=None, bias=None, buckets=0, dist=None, reach=0, db=None), dict(db=None)):
         refused(lib.pqt_attention_gradient, *call(**fine), code=pqt.PQT_EHIP)
-    assert pqt.pqt_attention_gradient_workspace(0, 1, 2, 3) == 0 and pqt.pqt_attention_gradient_workspace(100, 2, 4, 0) >= 1600
-    assert pqt.pqt_attention_gradient_workspace(100, 2, 4, 32) > pqt.pqt_attention_gradient_workspace(100, 2, 4, 0)
+    assert pqt.pqt_attention_gradient_workspace(0, 1, 2, 2, 64, 3) == 0 and pqt.pqt_attention_gradient_workspace(100, 2, 4, 3, 64, 0) == 0
+    assert pqt.pqt_attention_gradient_workspace(100, 2, 4, 4, 200, 0) == 0 and pqt.pqt_attention_gradient_workspace(100, 2, 4, 1, 64, 0) >= 1600
+    assert pqt.pqt_attention_gradient_workspace(100, 2, 4, 4, 64, 32) > pqt.pqt_attention_gradient_workspace(100, 2, 4, 4, 64, 0)
 
 
 def test_refusals_of_the_binding():
