@@ -12,7 +12,11 @@ SOURCES = ("pqt_api.hip", "pqt_host.cpp", "traverse.hip", "rank_bins.hip", "rera
            "rerank_pair_bytes.hip", "rerank_pair_long.hip", "rerank_pair2.hip", "rerank_pair4.hip", "rerank_pair6.hip",
            "rerank_pair8.hip", "rerank_pair16.hip",
            "exact_rerank.hip", "builder.hip", "place.hip", "train.hip", "brute_force.hip", "peaks.hip",
-           "attention_gradient.hip", "attention.hip", "rms_norm.hip", "layer_norm.hip", "embed.hip", "block_quantize.hip", "block_product.hip")
+           "attention.hip", "attention_gradient.hip",
+           # attention's kernels, one translation unit per type
+           "attention_bf16.hip", "attention_f16.hip", "attention_f32.hip", "attention_queries_bf16.hip", "attention_queries_f16.hip",
+           "attention_queries_f32.hip", "attention_keys_bf16.hip", "attention_keys_f16.hip", "attention_keys_f32.hip",
+           "rms_norm.hip", "layer_norm.hip", "embed.hip", "block_quantize.hip", "block_product.hip")
 OUTPUT = os.path.join(HERE, "libpqt.so")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # packed fp32 instructions are kept off for all device code

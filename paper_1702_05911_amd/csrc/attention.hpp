@@ -11,6 +11,40 @@
 #include "encoder.hpp"
 
 namespace pqt {
+
+struct AttentionArgs {
+    const void* q;
+    const void* k;
+    const void* v;
+    const void* grad;
+    const void* out_in;                    // gradient: what the forward pass wrote
+    const float* lse_in;
+    const void* starts;
+    const void* lengths;                   // or null: texts reach to the next one
+    const float* bias;                     // heads x buckets, or null
+    const int32_t* distances;              // buckets of -reach .. reach
+    void* out;
+    float* lse;
+    void* dq;
+    void* dk;
+    void* dv;
+    float* delta;                          // heads x n
+    float* parts;                          // workgroups x buckets
+    float* key_parts;                      // splits x heads of keys x n x (dk, dv), where the queries of a key are shared out
+    int64_t q_stride, k_stride, v_stride, grad_stride, out_stride, dq_stride, dk_stride, dv_stride;
+    int64_t n, texts;
+    int64_t tiles;                         // workgroups of a head
+    int wide;                              // starts and lengths are 64-bit numbers
+    int heads, group, d, buckets, reach, clear;
+    float scale;
+};
+
+// The kernels are compiled for one type in a translation unit of its own (attention_bf16.hip and so on): their launchers, by the rows of a workgroup
+// (16, 64 or 128), for rows that direct_rows() holds of or any.
+template <typename T> void launch_attention(const AttentionArgs& g, int rows, bool direct, hipStream_t st);
+template <typename T> void launch_attention_queries(const AttentionArgs& g, int rows, bool direct, hipStream_t st);
+template <typename T> void launch_attention_keys(const AttentionArgs& g, int rows, int splits, bool direct, hipStream_t st);
+
 namespace {
 
 constexpr int kMaxHeadD = 128;
@@ -190,32 +224,6 @@ __device__ __forceinline__ Fragment<T> rows_of_memory(const T* base, int64_t str
 }
 
 // ---- which rows ------------------------------------------------------------------------------------------------------
-struct AttentionArgs {
-    const void* q;
-    const void* k;
-    const void* v;
-    const void* grad;
-    const void* out_in;                    // gradient: what the forward pass wrote
-    const float* lse_in;
-    const void* starts;
-    const void* lengths;                   // or null: texts reach to the next one
-    const float* bias;                     // heads x buckets, or null
-    const int32_t* distances;              // buckets of -reach .. reach
-    void* out;
-    float* lse;
-    void* dq;
-    void* dk;
-    void* dv;
-    float* delta;                          // heads x n
-    float* parts;                          // workgroups x buckets
-    float* key_parts;                      // splits x heads of keys x n x (dk, dv), where the queries of a key are shared out
-    int64_t q_stride, k_stride, v_stride, grad_stride, out_stride, dq_stride, dk_stride, dv_stride;
-    int64_t n, texts;
-    int64_t tiles;                         // workgroups of a head
-    int wide;                              // starts and lengths are 64-bit numbers
-    int heads, group, d, buckets, reach, clear;
-    float scale;
-};
 
 __device__ __forceinline__ int64_t number(const void* p, int wide, int64_t i) {
     return wide ? static_cast<const int64_t*>(p)[i] : static_cast<const int32_t*>(p)[i];
@@ -279,6 +287,22 @@ __device__ __forceinline__ void place_of_workgroup(const AttentionArgs& g, int h
     t = at - (int64_t)head * g.tiles;
 }
 
+// The same where a row's heads are cut into `parts`, side by side.
+__device__ __forceinline__ void place_of_part(const AttentionArgs& g, int parts, int64_t& t, int& part) {
+    const int64_t total = g.tiles * parts, per = total >> 3;
+    const int x = blockIdx.x & 7, more = (int)(total & 7);
+    const int64_t at = x * per + min(x, more) + (blockIdx.x >> 3);
+    t = at / parts;
+    part = (int)(at - t * parts);
+}
+
+// Lanes of a wavefront meet: what one wrote to LDS another may read, in program order.
+__device__ __forceinline__ void wave_meets() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // zeros in rows from .. to of d columns
 template <typename T>
 __device__ __forceinline__ void clear_rows(T* p, int64_t stride, int64_t from, int64_t to, int d) {
@@ -290,11 +314,14 @@ __device__ __forceinline__ void clear_rows(T* p, int64_t stride, int64_t from, i
 // of two.  Finite entries are kept within 2^90, where that multiplication (scale up to 2^32) cannot overflow; -inf stays.
 constexpr float kBiasTop = 0x1p90f, kLowest = -0x1p92f;        // (kLowest: below every finite logit)
 
+__device__ __forceinline__ float scaled_bias(float entry, float scale) {
+    const float v = entry / scale;
+    return fabsf(entry) < __builtin_inff() ? fmaxf(-kBiasTop, fminf(v, kBiasTop)) : v;
+}
 __device__ __forceinline__ float bias_of(const AttentionArgs& g, int head, int distance) {
     const int b = g.distances[max(-g.reach, min(distance, g.reach)) + g.reach];
     if ((unsigned)b >= (unsigned)g.buckets) return 0.0f;       // a distance of no bucket has no bias
-    const float entry = g.bias[(int64_t)head * g.buckets + b], v = entry / g.scale;
-    return fabsf(entry) < __builtin_inff() ? fmaxf(-kBiasTop, fminf(v, kBiasTop)) : v;
+    return scaled_bias(g.bias[(int64_t)head * g.buckets + b], g.scale);
 }
 
 // The bias of the distances -W .. W (SIGN -1: W .. -W) in LDS, four times, copy c shifted by c places: the four consecutive ones that a lane needs for a
@@ -375,10 +402,16 @@ inline int attention_checks(const char* who, int type, int64_t n, int heads, int
     return PQT_OK;
 }
 
+inline bool short_texts(int64_t n, int64_t texts) { return texts > 0 && n / texts <= 32; }
+// Heads that a wavefront takes one after the other: 16,384 wavefronts are two rounds of what the card holds.
+inline int heads_of_a_wavefront(int64_t tiles, int heads, int waves) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>((heads + waves - 1) / waves, tiles * heads / 16384));
+}
+
 // Queries of a workgroup, by the texts' mean length and how many workgroups there are for 256 compute units.
 inline int rows_of_a_workgroup(int64_t n, int64_t texts, int heads) {
     const int64_t mean = texts ? n / texts : 0;
-    if (mean <= 32 || n / 64 * heads < 256) return 16;
+    if (short_texts(n, texts) || n / 64 * heads < 256) return 16;
     return mean <= 512 || n / 128 * heads < 512 ? 64 : 128;
 }
 

@@ -1,0 +1,253 @@
+// The kernel of attention's gradient that has queries: dq, delta and the parts of dbias (attention_gradient.hpp).
+#pragma once
+#include "attention_gradient.hpp"
+
+namespace pqt {
+namespace {
+
+template <typename T, int DP, int NW, int RT, int BN, bool DIRECT>
+__global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void attention_query_gradient_kernel(AttentionArgs g) {
+    constexpr int kThreads = NW * kWave, M = NW * RT * 16, KC = DP / 32, DT = DP / 16, kCopies = NW * 4;
+    typedef Tile<T, BN, DP> KeyTile;
+    __shared__ __align__(16) typename KeyTile::S k_0[KeyTile::kSize], k_1[KeyTile::kSize], v_0[KeyTile::kSize], v_1[KeyTile::kSize];
+    typedef typename KeyTile::Place Place;
+    const KeyTile k_even{(Place)k_0}, k_odd{(Place)k_1}, v_even{(Place)v_0}, v_odd{(Place)v_1};
+    __shared__ double far_sums[2][NW];
+    extern __shared__ __align__(16) float room[];              // the bias by distance, and kCopies x (2 W + 1) sums
+    const BiasTable table{room, BiasTable::pitch_of(most_places<RT, BN>(g.reach))};
+    float* const by_distance = room + 4 * table.pitch;
+    int64_t t;
+    int head;
+    place_of_workgroup(g, g.heads, t, head);
+    const Rows r = rows_of_workgroup<M>(g, t);
+    const int d = g.d, lane = threadIdx.x & (kWave - 1), col = lane & 15, quad = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    T* dq = static_cast<T*>(g.dq) + (int64_t)head * d;
+    float* parts = g.parts ? g.parts + (t * g.heads + head) * g.buckets : nullptr;
+    if (r.mine && (r.before || !r.text)) {                     // rows of no text
+        const int64_t from = r.before ? r.begin - r.before : r.begin + r.row0;
+        clear_rows(dq, g.dq_stride, from, r.before && r.text ? r.begin : min(r.begin + r.row0 + M, r.begin + r.span), d);
+    }
+    const int len = r.len, row0 = r.row0 + wave * RT * 16;
+    const bool work = r.mine && r.text && r.row0 < len;
+    if (!work && parts)
+        for (int b = threadIdx.x; b < g.buckets; b += kThreads) parts[b] = 0.0f;
+    if (!r.mine || !r.text) return;
+    f32x4 sums[RT][DT];
+    Lift<T> lift[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int b = 0; b < DT; ++b) sums[rt][b] = f32x4{};
+    if (work) {
+        const int kv = head / g.group;
+        const T* k = static_cast<const T*>(g.k) + r.begin * g.k_stride + (int64_t)kv * d;
+        const T* v = static_cast<const T*>(g.v) + r.begin * g.v_stride + (int64_t)kv * d;
+        const float cs = g.scale * kLog2e;
+        const int W = min(most_places<RT, BN>(g.reach), len + M + BN), width = 2 * W + 1;
+        Loader<T, BN, DP, kThreads, DIRECT> next_k(g.k_stride, d), next_v(g.v_stride, d);
+        next_k.begin(k_even, k, g.k_stride, 0, len, d);
+        next_v.begin(v_even, v, g.v_stride, 0, len, d);
+        if (g.bias) table.fill<1, kThreads>(g, head, W);
+        if (parts)
+            for (int i = threadIdx.x; i < kCopies * width; i += kThreads) by_distance[i] = 0.0f;
+        Fragment<T> q[RT][KC], grad[RT][KC];
+        float delta[RT], power[RT], factor[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int row = row0 + rt * 16 + col;
+            delta[rt] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                q[rt][c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, row0 + rt * 16, len, d, c);
+                grad[rt][c] = rows_of_memory(static_cast<const T*>(g.grad) + r.begin * g.grad_stride + (int64_t)head * d, g.grad_stride, row0 + rt * 16, len, d, c);
+                const f32x8 o = __builtin_convertvector(
+                    rows_of_memory(static_cast<const T*>(g.out_in) + r.begin * g.out_stride + (int64_t)head * d, g.out_stride, row0 + rt * 16, len, d, c), f32x8);
+                const f32x8 y = __builtin_convertvector(grad[rt][c], f32x8) * o;
+                delta[rt] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+            }
+            delta[rt] = sum_of_groups(delta[rt]);
+            const float lse = row < len ? g.lse_in[(int64_t)head * g.n + r.begin + row] : -__builtin_inff();
+            if (row < len && quad == 0) g.delta[(int64_t)head * g.n + r.begin + row] = delta[rt];
+            power[rt] = power_of(lse);
+            factor[rt] = rest_of_power(lse);
+            delta[rt] *= factor[rt];
+        }
+        double far_left = 0.0, far_right = 0.0;
+        next_k.finish(k_even);
+        next_v.finish(v_even);
+        __syncthreads();
+        const float before = g.bias ? table.v[0] : 0.0f, behind = g.bias ? table.v[2 * W] : 0.0f;
+        float* const mine = by_distance + (wave * 4 + quad) * width + W;
+        auto step = [&](int j0, KeyTile kt, KeyTile vt, KeyTile k_next, KeyTile v_next) __attribute__((always_inline)) {
+            const bool more = j0 + BN < len;
+            if (more) {
+                next_k.begin(k_next, k, g.k_stride, j0 + BN, len, d);
+                next_v.begin(v_next, v, g.v_stride, j0 + BN, len, d);
+            }
+            const int low = j0 - (row0 + RT * 16 - 1), high = j0 + BN - 1 - row0;
+            const bool near = g.bias && high > -g.reach && low < g.reach;
+            const float far = low >= g.reach ? behind : before;
+            const float* at = table.from(j0 + quad * 4 - row0 - col + W);
+            float carry[RT], far_sum = 0.0f;
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) carry[rt] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < BN / 32; ++c) {
+                f32x4 s[RT][2], dp[RT][2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        s[rt][h] = near ? four_of(at + c * 32 + h * 16 - rt * 16) : f32x4{far, far, far, far};
+                        dp[rt][h] = f32x4{};
+                    }
+#pragma unroll
+                    for (int x = 0; x < KC; ++x) {
+                        const Fragment<T> f = kt.rows(c * 32 + h * 16, x);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) s[rt][h] = multiply(f, q[rt][x], s[rt][h]);
+                    }
+#pragma unroll
+                    for (int x = 0; x < KC; ++x) {
+                        const Fragment<T> f = vt.rows(c * 32 + h * 16, x);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) dp[rt][h] = multiply(f, grad[rt][x], dp[rt][h]);
+                    }
+                }
+                Fragment<T> ds[RT];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            s[rt][h][e] = exp2_of(__builtin_fmaf(s[rt][h][e], cs, -power[rt])) * __builtin_fmaf(dp[rt][h][e], factor[rt], -delta[rt]);
+                        if (j0 + c * 32 + 32 > len) {          // places behind the text's last token
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (j0 + c * 32 + h * 16 + quad * 4 + e >= len) s[rt][h][e] = 0.0f;
+                        }
+                    }
+                    if (parts) {
+                        if (near) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                // lane `col` gets what lies at key 16 c + 4 quad - col from its query on; what moved past the sixteen lanes is the next sixteen keys'
+                                const f32x4 v = s[rt][h];
+                                const float sum = ((carry[rt] + v[0]) + from_right<1>(v[1])) + (from_right<2>(v[2]) + from_right<3>(v[3]));
+                                carry[rt] = from_left<15>(v[1]) + from_left<14>(v[2]) + from_left<13>(v[3]);
+                                mine[j0 + c * 32 + h * 16 + quad * 4 - (row0 + rt * 16) - col] += sum;
+                            }
+                        } else {
+                            const f32x4 both = s[rt][0] + s[rt][1];
+                            far_sum += (both[0] + both[1]) + (both[2] + both[3]);
+                        }
+                    }
+                    lift[rt].apply(s[rt][0], s[rt][1], sums[rt]);
+                    ds[rt] = fragment_of<T>(s[rt][0], s[rt][1]);
+                }
+#pragma unroll
+                for (int b = 0; b < DT; ++b) {
+                    const Fragment<T> f = kt.columns(c * 32, b);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) sums[rt][b] = multiply(f, ds[rt], sums[rt][b]);
+                }
+            }
+            if (parts) {
+                if (near) {
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) mine[j0 + BN + quad * 4 - (row0 + rt * 16) - col] += carry[rt];
+                } else if (low >= g.reach) far_right += far_sum;
+                else far_left += far_sum;
+            }
+            if constexpr (sizeof(T) == 2)
+                if (parts)
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        factor[rt] = -factor[rt];
+#pragma unroll
+                        for (int x = 0; x < KC; ++x) negate<T>(grad[rt][x]);
+                    }
+            if (more) {
+                next_k.finish(k_next);
+                next_v.finish(v_next);
+            }
+            __syncthreads();
+        };
+        for (int j0 = 0; j0 < len; j0 += 2 * BN) {
+            step(j0, k_even, v_even, k_odd, v_odd);
+            if (j0 + BN < len) step(j0 + BN, k_odd, v_odd, k_even, v_even);
+        }
+        if (parts) {
+#pragma unroll
+            for (int off = 1; off < kWave; off *= 2) {
+                far_left += __shfl_xor(far_left, off, kWave);
+                far_right += __shfl_xor(far_right, off, kWave);
+            }
+            if (lane == 0) {
+                far_sums[0][wave] = far_left;
+                far_sums[1][wave] = far_right;
+            }
+            for (int i = threadIdx.x; i < width; i += kThreads) {
+                float sum = by_distance[i];
+#pragma unroll
+                for (int x = 1; x < kCopies; ++x) sum += by_distance[x * width + i];
+                by_distance[i] = sum;
+                by_distance[width + i] = __int_as_float(g.distances[max(-g.reach, min(i - W, g.reach)) + g.reach]);
+            }
+            __syncthreads();
+            // eight lanes a bucket
+            const int first = g.distances[0], last = g.distances[2 * g.reach];
+            for (int e = threadIdx.x; e < g.buckets * 8; e += kThreads) {
+                const int b = e >> 3;
+                double sum = 0.0;
+                for (int i = e & 7; i < width; i += 8) sum += __float_as_int(by_distance[width + i]) == b ? by_distance[i] : 0.0f;
+#pragma unroll
+                for (int off = 1; off < 8; off *= 2) sum += __shfl_xor(sum, off, kWave);
+                if ((e & 7) == 0) {
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) sum += (first == b ? far_sums[0][w] : 0.0) + (last == b ? far_sums[1][w] : 0.0);
+                    parts[b] = (float)sum;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = row0 + rt * 16 + col;
+        if (row >= r.span) continue;
+        const float by = g.scale * lift[rt].inverse();
+        T* dst = dq + (r.begin + row) * g.dq_stride;
+#pragma unroll
+        for (int b = 0; b < DT; ++b) {
+            const int c = b * 16 + quad * 4;
+            store_piece<T, 4>(dst + c, row < len ? sums[rt][b] * by : f32x4{}, d - c);
+        }
+    }
+}
+
+}  // namespace
+
+template <typename T>
+void launch_attention_queries(const AttentionArgs& args, int rows, bool direct, hipStream_t st) {
+    AttentionArgs g = args;
+    g.tiles = g.n / rows + g.texts + 1;
+    const dim3 blocks((unsigned)(g.tiles * g.heads));
+    with_head(g.d, [&](auto dp) {
+        constexpr int DP = dp.value, kKeys = sizeof(T) == 4 && DP > 64 ? 32 : 64;
+        auto launch = [&](auto kernel, int waves, int most) {
+            const size_t table = g.bias ? BiasTable::bytes(most) : 0, sums = g.parts ? sizeof(float) * waves * 4 * (2 * most + 1) : 0;
+            hipLaunchKernelGGL(kernel, blocks, dim3(waves * kWave), table + sums, st, g);
+        };
+        auto of = [&](auto waves, auto rt, auto step) {
+            constexpr int NW = waves.value, RT = rt.value, BN = step.value;
+            if (direct) launch(attention_query_gradient_kernel<T, DP, NW, RT, BN, true>, NW, most_places<RT, BN>(g.reach));
+            else launch(attention_query_gradient_kernel<T, DP, NW, RT, BN, false>, NW, most_places<RT, BN>(g.reach));
+        };
+        if (rows == 16) of(Width<1>{}, Width<1>{}, Width<32>{});
+        else if (rows == 64) of(Width<4>{}, Width<1>{}, Width<kKeys>{});
+        else of(Width<4>{}, Width<2>{}, Width<kKeys>{});
+    });
+}
+
+}  // namespace pqt
