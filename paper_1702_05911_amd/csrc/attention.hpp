@@ -7,6 +7,7 @@
 // from one product into the next without leaving their lane, if the other operand's values are taken in that order.
 #pragma once
 #include <algorithm>
+#include <type_traits>
 
 #include "encoder.hpp"
 
@@ -155,13 +156,16 @@ struct Loader {
     static_assert(ROWS * kOfRow % THREADS == 0, "whole pieces for every thread");
     static constexpr uint32_t kNowhere = 0x80000000u;
     typedef typename FragmentOf<T>::piece Unaligned;
+    // where a thread's pieces lie equally far apart, the first one's place is kept, and the others' are counted from it
+    static constexpr int kRowsApart = THREADS / kOfRow;
+    static constexpr bool kEven = THREADS % kOfRow == 0 && kRowsApart % 16 == 0;
     u32x4 v[DIRECT ? 1 : kPieces];
-    uint32_t off[DIRECT ? kPieces : 1];
+    uint32_t off[DIRECT && !kEven ? kPieces : 1];
 
     __device__ __forceinline__ Loader(int64_t stride, int d) {
         if constexpr (DIRECT) {
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
+            for (int i = 0; i < (kEven ? 1 : kPieces); ++i) {
                 const int at = threadIdx.x % THREADS + i * THREADS, row = at / kOfRow, c = ((at % kOfRow) ^ Into::turn(row)) * E;
                 off[i] = c < d ? (uint32_t)((row * (int)stride + c) * (int)sizeof(T)) : kNowhere;
             }
@@ -176,12 +180,13 @@ struct Loader {
             const uint32_t bytes = __builtin_amdgcn_readfirstlane((uint32_t)(((rows - 1) * (int)stride + d) * (int)sizeof(T)));
             const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), (short)0, bytes, 0x00027000);
             const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x % THREADS) / kWave);
+            const uint32_t apart = kRowsApart * (uint32_t)stride * (uint32_t)sizeof(T);    // (kNowhere stays past every tile)
 #pragma unroll
             for (int i = 0; i < kPieces; ++i)
 #if defined(__HIP_DEVICE_COMPILE__)                            // (the host's pass over this file takes 16 bytes for an error, and leaves the kernels out)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_bytes*)(tile.v + (i * THREADS + wave * kWave) * E), 16, off[i], 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_bytes*)(tile.v + (i * THREADS + wave * kWave) * E), 16, kEven ? off[0] + i * apart : off[i], 0, 0, 0);
 #else
-                (void)from, (void)wave;
+                (void)from, (void)wave, (void)apart;
 #endif
         } else {
 #pragma unroll
@@ -358,6 +363,51 @@ __device__ __forceinline__ float sum_of_groups(float v) {
     return v + __shfl_xor(v, 32, kWave);
 }
 
+// Kinds of steps along a text, a body each: all places farther than `reach` on one side (or no bias), some nearer, either of them, and the last, whose rows behind
+// the text's end are left out.
+enum : int { kFar, kNear, kEither, kLast };
+template <int K> using Kind = std::integral_constant<int, K>;
+
+// Steps of BN rows along a text of `len`, by a wavefront with 16 RT rows from row0 on, in turn by one of two tiles: f(kind, odd, step).  Every wavefront of a
+// workgroup makes as many steps.  The last stands outside of the loop: what it alone needs takes no registers there.  RUNS: those far before the rows, those
+// nearer than `reach` and those far behind are runs of their own (a choice at every step would move the sums from registers to others where its ways
+// join, and what the products are added to as well); it takes code and registers that only long texts are worth.
+template <int RT, int BN, bool RUNS, typename F>
+__device__ __forceinline__ void walk(const AttentionArgs& g, int row0, int len, F&& f) {
+    typedef std::integral_constant<bool, false> Even;
+    typedef std::integral_constant<bool, true> Odd;
+    const int full = (len - 1) / BN;
+    int i = 0;
+    if constexpr (!RUNS) {
+        for (;; ++i) {
+            if (i == full) break;
+            f(Kind<kEither>{}, Even{}, i++);
+            if (i == full) break;
+            f(Kind<kEither>{}, Odd{}, i);
+        }
+    } else {
+        // near: from the first j0 > row0 - reach - BN + 1 to the last j0 < row0 + 16 RT - 1 + reach
+        const int near_from = g.bias ? min(full, (max(0, row0 - g.reach - BN + 2) + BN - 1) / BN) : full;
+        const int near_to = g.bias ? min(full, (row0 + RT * 16 - 1 + g.reach + BN - 1) / BN) : full;
+        auto run = [&](auto kind, int to) __attribute__((always_inline)) {
+            if (i < to && i % 2) f(kind, Odd{}, i++);
+#pragma nounroll
+            for (; i + 1 < to; i += 2) {
+                f(kind, Even{}, i);
+                f(kind, Odd{}, i + 1);
+            }
+            if (i < to) f(kind, Even{}, i++);
+        };
+#pragma nounroll
+        for (int side = 0; side < 2; ++side) {
+            run(Kind<kFar>{}, side ? full : near_from);
+            if (side == 0) run(Kind<kNear>{}, near_to);
+        }
+    }
+    if (full % 2) f(Kind<kLast>{}, Odd{}, full);
+    else f(Kind<kLast>{}, Even{}, full);
+}
+
 // calls f(Int<DP>) for heads of d values
 template <int V> struct Width { static constexpr int value = V; };
 template <typename F>
@@ -412,8 +462,9 @@ inline int heads_of_a_wavefront(int64_t tiles, int heads, int waves) {
 inline int rows_of_a_workgroup(int64_t n, int64_t texts, int heads) {
     const int64_t mean = texts ? n / texts : 0;
     if (short_texts(n, texts) || n / 64 * heads < 256) return 16;
-    return mean <= 512 || n / 128 * heads < 512 ? 64 : 128;
+    return mean <= 128 || n / 128 * heads < 512 ? 64 : 128;
 }
+inline bool long_texts(int64_t n, int64_t texts) { return texts > 0 && n / texts > 1024; }
 
 }  // namespace
 }  // namespace pqt

@@ -16,9 +16,10 @@ constexpr float kSlack = 8.0f;
 template <typename T> struct Shift { static constexpr float value = 0.0f; };
 template <> struct Shift<Half> { static constexpr float value = 6.0f; };
 
-template <typename T, int DP, int NW, int RT, int BN, bool DIRECT>
+template <typename T, int DP, int NW, int RT, int BN, bool DIRECT, bool RUNS>
 __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void attention_kernel(AttentionArgs g) {
     constexpr int kThreads = NW * kWave, M = NW * RT * 16, KC = DP / 32, DT = DP / 16;
+    constexpr int kPart = RUNS && sizeof(T) == 2 && DP <= 64 ? BN / 16 : 2;            // sixteens of keys whose weights are taken at once
     typedef Tile<T, BN, DP> KeyTile;
     // (variables of their own: reading one does not wait for loads to another)
     __shared__ __align__(16) typename KeyTile::S k_0[KeyTile::kSize], k_1[KeyTile::kSize], v_0[KeyTile::kSize], v_1[KeyTile::kSize];
@@ -72,47 +73,45 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
         next_v.finish(v_even);
         __syncthreads();
         const float before = g.bias ? table.v[0] : 0.0f, behind = g.bias ? table.v[2 * W] : 0.0f;
-        auto step = [&](int j0, KeyTile kt, KeyTile vt, KeyTile k_next, KeyTile v_next) __attribute__((always_inline)) {
-            const bool more = j0 + BN < len;
-            if (more) {
+        auto step = [&](auto kind, int j0, int low, bool near, KeyTile kt, KeyTile vt, KeyTile k_next, KeyTile v_next) __attribute__((always_inline)) {
+            constexpr int kKind = decltype(kind)::value;
+            if constexpr (kKind != kLast) {
                 next_k.begin(k_next, k, g.k_stride, j0 + BN, len, d);
                 next_v.begin(v_next, v, g.v_stride, j0 + BN, len, d);
             }
             // what the products are added to: the bias of every place, or of all of them where they are far away
-            const int low = j0 - (row0 + RT * 16 - 1), high = j0 + BN - 1 - row0;
-            const bool near = g.bias && high > -g.reach && low < g.reach;
             const float far = low >= g.reach ? behind : before;
+            const f32x4 all_far = f32x4{far, far, far, far};
             const float* at = table.from(j0 + quad * 4 - row0 - col + W);
 #pragma unroll
-            for (int c = 0; c < BN / 32; ++c) {
-                f32x4 s[RT][2];
+            for (int c = 0; c < BN / 16; c += kPart) {
+                f32x4 s[RT][kPart];
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
+                for (int h = 0; h < kPart; ++h) {
+                    if constexpr (kKind != kFar) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) s[rt][h] = near ? four_of(at + c * 32 + h * 16 - rt * 16) : f32x4{far, far, far, far};
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
+                        for (int rt = 0; rt < RT; ++rt) s[rt][h] = kKind == kNear || near ? four_of(at + (c + h - rt) * 16) : all_far;
+                    }
 #pragma unroll
                     for (int x = 0; x < KC; ++x) {
-                        const Fragment<T> f = kt.rows(c * 32 + h * 16, x);
+                        const Fragment<T> f = kt.rows((c + h) * 16, x);
 #pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) s[rt][h] = multiply(f, q[rt][x], s[rt][h]);
+                        for (int rt = 0; rt < RT; ++rt) s[rt][h] = multiply(f, q[rt][x], kKind == kFar && x == 0 ? all_far : s[rt][h]);
                     }
-                if (j0 + c * 32 + 32 > len) {                  // places behind the text's last token
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                    if constexpr (kKind == kLast) {            // places behind the text's last token
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (j0 + c * 32 + h * 16 + quad * 4 + e >= len) {
 #pragma unroll
-                                for (int rt = 0; rt < RT; ++rt) s[rt][h][e] = -__builtin_inff();
-                            }
+                            for (int rt = 0; rt < RT; ++rt) s[rt][h][e] = j0 + (c + h) * 16 + quad * 4 + e < len ? s[rt][h][e] : -__builtin_inff();
+                    }
                 }
                 float top[RT];
                 bool rises = false;
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
-                    top[rt] = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])), fmaxf(fmaxf(s[rt][1][0], s[rt][1][1]), fmaxf(s[rt][1][2], s[rt][1][3])));
+                    top[rt] = s[rt][0][0];
+#pragma unroll
+                    for (int h = 0; h < kPart; ++h) top[rt] = fmaxf(fmaxf(fmaxf(top[rt], s[rt][h][0]), fmaxf(s[rt][h][1], s[rt][h][2])), s[rt][h][3]);
                     rises |= (top[rt] - m[rt]) * cs > kSlack;
                 }
                 if (__any(rises)) {
@@ -125,36 +124,42 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
                         for (int b = 0; b < DT; ++b) o[rt][b] = o[rt][b] * keep;
                     }
                 }
-                Fragment<T> p[RT];
+                Fragment<T> p[RT][kPart / 2];
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     const float off = Shift<T>::value - m[rt] * cs;
+                    f32x4 sum = f32x4{};
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                    for (int h = 0; h < kPart; ++h) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            s[rt][h][e] = exp2_of(__builtin_fmaf(s[rt][h][e], cs, off));
-                            l[rt] += s[rt][h][e];
-                        }
-                    p[rt] = fragment_of<T>(s[rt][0], s[rt][1]);
+                        for (int e = 0; e < 4; ++e) s[rt][h][e] = exp2_of(__builtin_fmaf(s[rt][h][e], cs, off));
+                        sum = sum + s[rt][h];
+                    }
+                    l[rt] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+                    for (int h = 0; h < kPart / 2; ++h) p[rt][h] = fragment_of<T>(s[rt][2 * h], s[rt][2 * h + 1]);
                 }
 #pragma unroll
-                for (int b = 0; b < DT; ++b) {
-                    const Fragment<T> f = vt.columns(c * 32, b);
+                for (int h = 0; h < kPart / 2; ++h)
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) o[rt][b] = multiply(f, p[rt], o[rt][b]);
-                }
+                    for (int b = 0; b < DT; ++b) {
+                        const Fragment<T> f = vt.columns((c + 2 * h) * 16, b);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) o[rt][b] = multiply(f, p[rt][h], o[rt][b]);
+                    }
             }
-            if (more) {
+            if constexpr (kKind != kLast) {
                 next_k.finish(k_next);
                 next_v.finish(v_next);
+                __syncthreads();
             }
-            __syncthreads();
         };
-        for (int j0 = 0; j0 < len; j0 += 2 * BN) {
-            step(j0, k_even, v_even, k_odd, v_odd);
-            if (j0 + BN < len) step(j0 + BN, k_odd, v_odd, k_even, v_even);
-        }
+        walk<RT, BN, RUNS>(g, row0, len, [&](auto kind, auto odd, int i) __attribute__((always_inline)) {
+            const int j0 = i * BN, low = j0 - (row0 + RT * 16 - 1), high = j0 + BN - 1 - row0;
+            const bool near = g.bias && high > -g.reach && low < g.reach;
+            if constexpr (odd.value) step(kind, j0, low, near, k_odd, v_odd, k_even, v_even);
+            else step(kind, j0, low, near, k_even, v_even, k_odd, v_odd);
+        });
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -302,19 +307,22 @@ void launch_attention(const AttentionArgs& args, int rows, bool direct, hipStrea
     with_head(g.d, [&](auto dp) {
         constexpr int DP = dp.value, kKeys = sizeof(T) == 4 && DP > 64 ? 32 : 64;
         auto launch = [&](auto kernel, int waves, int most) { hipLaunchKernelGGL(kernel, blocks, dim3(waves * kWave), g.bias ? BiasTable::bytes(most) : 0, st, g); };
-        auto of = [&](auto waves, auto rt, auto step) {
+        auto of = [&](auto waves, auto rt, auto step, auto runs) {
             constexpr int NW = waves.value, RT = rt.value, BN = step.value;
-            if (direct) launch(attention_kernel<T, DP, NW, RT, BN, true>, NW, g.reach + RT * 16 + BN);
-            else launch(attention_kernel<T, DP, NW, RT, BN, false>, NW, g.reach + RT * 16 + BN);
+            if (direct) launch(attention_kernel<T, DP, NW, RT, BN, true, runs.value>, NW, g.reach + RT * 16 + BN);
+            else launch(attention_kernel<T, DP, NW, RT, BN, false, false>, NW, g.reach + RT * 16 + BN);
         };
+        typedef std::integral_constant<bool, false> No;
+        typedef std::integral_constant<bool, true> Yes;
         if (short_texts(g.n, g.texts)) {
             const int waves = std::min(4, g.heads), of_wave = heads_of_a_wavefront(g.tiles, g.heads, waves), parts = (g.heads + waves * of_wave - 1) / (waves * of_wave);
             const dim3 grid((unsigned)(g.tiles * parts)), threads(waves * kWave);
             if (direct) hipLaunchKernelGGL((attention_short_kernel<T, DP, true>), grid, threads, 0, st, g, of_wave);
             else hipLaunchKernelGGL((attention_short_kernel<T, DP, false>), grid, threads, 0, st, g, of_wave);
-        } else if (rows == 16) of(Width<1>{}, Width<1>{}, Width<32>{});
-        else if (rows == 64) of(Width<4>{}, Width<1>{}, Width<kKeys>{});
-        else of(Width<4>{}, Width<2>{}, Width<kKeys>{});
+        } else if (rows == 16) of(Width<1>{}, Width<1>{}, Width<32>{}, No{});
+        else if (rows == 64) of(Width<4>{}, Width<1>{}, Width<kKeys>{}, No{});
+        else if (!long_texts(g.n, g.texts)) of(Width<4>{}, Width<2>{}, Width<kKeys>{}, No{});
+        else of(Width<4>{}, Width<2>{}, Width<kKeys>{}, Yes{});
     });
 }
 
