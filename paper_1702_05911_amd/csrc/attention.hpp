@@ -106,11 +106,12 @@ struct Tile {
     typedef __attribute__((address_space(3))) S* Place;
     static constexpr int E = 16 / (int)sizeof(T), kOfRow = DP / E, kSize = ROWS * DP;
     Place v;                               // an LDS array of kSize values
+    int lane;                              // of the wavefront
 
     static __device__ __forceinline__ int turn(int row) { return kOfRow % 16 == 0 ? row & 15 : kOfRow % 8 == 0 ? row & 7 : row & 8 ? 3 : 0; }
     // values 32 chunk + 8 (lane >> 4) .. + 7 of row row0 + (lane & 15)
     __device__ __forceinline__ Fragment<T> rows(int row0, int chunk) const {
-        const int lane = threadIdx.x & (kWave - 1), row = lane & 15, q = lane >> 4;
+        const int row = lane & 15, q = lane >> 4;
         const Place p = v + (row0 + row) * DP;
         typedef __attribute__((address_space(3))) const u32x4 P;
         if constexpr (sizeof(T) == 2) {
@@ -122,7 +123,7 @@ struct Tile {
     }
     // the transpose's: of column 16 block + (lane & 15), the rows row0 + place(e)
     __device__ __forceinline__ Fragment<T> columns(int row0, int block) const {
-        const int lane = threadIdx.x & (kWave - 1), col = lane & 15, q = lane >> 4;
+        const int col = lane & 15, q = lane >> 4;
         if constexpr (sizeof(T) == 2) {
             // sixteen lanes read 4 x 16 values, 8 bytes each, and get a column's four
             typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -220,8 +221,8 @@ inline bool direct_rows(const void* p, int64_t stride, size_t element, int d) {
 
 // fragment `chunk` of a wavefront's own 16 rows row0 + (lane & 15), straight from memory
 template <typename T>
-__device__ __forceinline__ Fragment<T> rows_of_memory(const T* base, int64_t stride, int row0, int len, int d, int chunk) {
-    const int lane = threadIdx.x & (kWave - 1), row = row0 + (lane & 15), c = chunk * 32 + (lane >> 4) * 8;
+__device__ __forceinline__ Fragment<T> rows_of_memory(const T* base, int64_t stride, int row0, int len, int d, int chunk, int lane) {
+    const int row = row0 + (lane & 15), c = chunk * 32 + (lane >> 4) * 8;
     typedef typename Piece_<T, 8>::type V;
     V v = V{};
     if (row < len && c < d) v = load_raw<T, 8>(base + (int64_t)row * stride + c, d - c);
@@ -246,40 +247,41 @@ struct Rows {
 
 template <int M>
 __device__ __forceinline__ Rows rows_of_workgroup(const AttentionArgs& g, int64_t t) {
-    const int lane = threadIdx.x & (kWave - 1);
-    auto start = [&](int64_t s) __attribute__((always_inline)) { return min(max(number(g.starts, g.wide, s), (int64_t)0), g.n); };
-    // the last text with floor(start / M) + s <= t: 64 of them looked at at once.  (texts: the rows behind the last one.)
-    int64_t lo = 0, hi = g.texts + 1;
-    bool first = true;
+    const int lane = threadIdx.x & (kWave - 1), texts = (int)g.texts;
+    // the last text with floor(start / M) + s <= t: 64 of them looked at at once.  (s = texts: the rows behind the last one.)
+    int lo = 0, hi = texts + 1;
     Rows r{};
-    while (first || hi - lo > 1) {
-        const int64_t step = (hi - lo + kWave - 1) / kWave, probe = lo + lane * step;
-        const bool ok = probe < hi && start(probe) / M + probe <= t;
-        const int count = (int)__popcll(__ballot(ok));
-        if (count == 0) break;                                   // (of the first round only: later ones begin with one that is)
-        lo = lo + (int64_t)(count - 1) * step;
+    for (;;) {
+        const int step = (hi - lo + kWave - 1) / kWave, probe = lo + lane * step, s = min(probe, texts);
+        const int start = (int)min(max(number(g.starts, g.wide, s), (int64_t)0), g.n);
+        int64_t tokens = 0;                                    // (asked for beside the starts of the last look, not behind them)
+        if (step == 1 && g.lengths && texts) tokens = number(g.lengths, g.wide, min(s, texts - 1));
+        const int count = (int)__popcll(__ballot(probe < hi && start / M + probe <= t));
+        if (count == 0) {                                      // (at the first look only: later ones begin with a text that is) rows before the first text
+            r.begin = t * M;
+            r.span = M;
+            r.mine = g.clear != 0;
+            return r;
+        }
+        const int at = count - 1;
+        lo += at * step;
         hi = min(hi, lo + step);
-        first = false;
-    }
-    lo = __builtin_amdgcn_readfirstlane((int)lo);              // (rows and texts are fewer than 2^31)
-    if (first) {                                               // rows before the first text
-        r.begin = t * M;
-        r.span = M;
-        r.mine = g.clear != 0;
+        if (step > 1) continue;
+        const int begin = __builtin_amdgcn_readlane(start, at);
+        int end = (int)g.n;
+        r.text = lo < texts;
+        if (r.text) end = max(at + 1 < kWave ? __builtin_amdgcn_readlane(start, at + 1) : (int)min(max(number(g.starts, g.wide, lo + 1), (int64_t)0), g.n), begin);
+        end = __builtin_amdgcn_readfirstlane(end);
+        r.begin = begin;
+        r.span = end - begin;
+        r.len = r.text ? r.span : 0;
+        if (r.text && g.lengths) r.len = min(r.span, __builtin_amdgcn_readlane((int)min(max(tokens, (int64_t)0), (int64_t)0x7fffffff), at));
+        const int64_t row0 = (t - (begin / M + lo)) * M;
+        r.before = lo == 0 && row0 == 0 && g.clear ? begin % M : 0;
+        r.mine = r.before > 0 || (row0 < r.span && (r.text || g.clear));
+        r.row0 = (int)min(row0, (int64_t)r.span);
         return r;
     }
-    const int64_t begin = start(lo), end = lo < g.texts ? max(start(lo + 1), begin) : g.n;
-    r.text = lo < g.texts;
-    const int64_t have = r.text ? (g.lengths ? min(max(number(g.lengths, g.wide, lo), (int64_t)0), end - begin) : end - begin) : 0;
-    // (numbers of the workgroup, not of lanes)
-    r.begin = __builtin_amdgcn_readfirstlane((int)begin);
-    r.span = __builtin_amdgcn_readfirstlane((int)(end - begin));
-    r.len = __builtin_amdgcn_readfirstlane((int)have);
-    const int64_t row0 = (t - (r.begin / M + lo)) * M;
-    r.before = lo == 0 && row0 == 0 && g.clear ? r.begin % M : 0;
-    r.mine = r.before > 0 || (row0 < r.span && (r.text || g.clear));
-    r.row0 = (int)min(row0, (int64_t)r.span);
-    return r;
 }
 
 // Workgroup -> (rows, head).  Consecutive workgroups go to the eight XCDs in turn: each XCD gets a run of one head's rows after another, so that its L2
@@ -323,13 +325,7 @@ __device__ __forceinline__ float scaled_bias(float entry, float scale) {
     const float v = entry / scale;
     return fabsf(entry) < __builtin_inff() ? fmaxf(-kBiasTop, fminf(v, kBiasTop)) : v;
 }
-__device__ __forceinline__ float bias_of(const AttentionArgs& g, int head, int distance) {
-    const int b = g.distances[max(-g.reach, min(distance, g.reach)) + g.reach];
-    if ((unsigned)b >= (unsigned)g.buckets) return 0.0f;       // a distance of no bucket has no bias
-    return scaled_bias(g.bias[(int64_t)head * g.buckets + b], g.scale);
-}
-
-// The bias of the distances -W .. W (SIGN -1: W .. -W) in LDS, four times, copy c shifted by c places: the four consecutive ones that a lane needs for a
+// The bias of the distances on either side in LDS, four times, copy c shifted by c places: the four consecutive ones that a lane needs for a
 // result then begin at a multiple of 16 bytes in copy (first & 3), which is the same for all of a lane's.
 struct BiasTable {
     float* v;
@@ -337,10 +333,24 @@ struct BiasTable {
     static __host__ __device__ __forceinline__ int pitch_of(int most) { return (2 * most + 4 + 63) / 64 * 64 + 16; }      // for W up to `most`
     static size_t bytes(int most) { return 4 * sizeof(float) * pitch_of(most); }
 
-    template <int SIGN, int THREADS>
-    __device__ __forceinline__ void fill(const AttentionArgs& g, int head, int W) const {
-        for (int i = threadIdx.x % THREADS; i <= 2 * W; i += THREADS) {
-            const float b = bias_of(g, head, SIGN * (i - W));
+    // In two parts, so that a workgroup can ask for the buckets before it knows its rows: for the distances -W .. W (SIGN -1: W .. -W) ...
+    template <int SIGN, int THREADS, int N>
+    static __device__ __forceinline__ void look_up(const AttentionArgs& g, int W, int (&bucket)[N]) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int i = threadIdx.x % THREADS + n * THREADS;
+            bucket[n] = -1;
+            if (n * THREADS <= 2 * W && i <= 2 * W) bucket[n] = g.distances[max(-g.reach, min(SIGN * (i - W), g.reach)) + g.reach];
+        }
+    }
+    // ... and a head's bias of them
+    template <int THREADS, int N>
+    __device__ __forceinline__ void fill(const AttentionArgs& g, int head, int W, const int (&bucket)[N]) const {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int i = threadIdx.x % THREADS + n * THREADS;
+            if (n * THREADS > 2 * W || i > 2 * W) continue;
+            const float b = (unsigned)bucket[n] < (unsigned)g.buckets ? scaled_bias(g.bias[(int64_t)head * g.buckets + bucket[n]], g.scale) : 0.0f;     // (no bucket: no bias)
 #pragma unroll
             for (int c = 0; c < 4; ++c)
                 if (i >= c) v[c * pitch + i - c] = b;
@@ -452,7 +462,7 @@ inline int attention_checks(const char* who, int type, int64_t n, int heads, int
     return PQT_OK;
 }
 
-inline bool short_texts(int64_t n, int64_t texts) { return texts > 0 && n / texts <= 32; }
+inline bool short_texts(int64_t n, int64_t texts) { return texts > 0 && n / texts <= 64; }
 // Heads that a wavefront takes one after the other: 16,384 wavefronts are two rounds of what the card holds.
 inline int heads_of_a_wavefront(int64_t tiles, int heads, int waves) {
     return (int)std::max<int64_t>(1, std::min<int64_t>((heads + waves - 1) / waves, tiles * heads / 16384));

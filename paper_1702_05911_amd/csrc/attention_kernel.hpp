@@ -24,9 +24,12 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
     // (variables of their own: reading one does not wait for loads to another)
     __shared__ __align__(16) typename KeyTile::S k_0[KeyTile::kSize], k_1[KeyTile::kSize], v_0[KeyTile::kSize], v_1[KeyTile::kSize];
     typedef typename KeyTile::Place Place;
-    const KeyTile k_even{(Place)k_0}, k_odd{(Place)k_1}, v_even{(Place)v_0}, v_odd{(Place)v_1};
+    const KeyTile k_even{(Place)k_0, (int)threadIdx.x & (kWave - 1)}, k_odd{(Place)k_1, (int)threadIdx.x & (kWave - 1)}, v_even{(Place)v_0, (int)threadIdx.x & (kWave - 1)}, v_odd{(Place)v_1, (int)threadIdx.x & (kWave - 1)};
     extern __shared__ __align__(16) float bias_room[];
-    const BiasTable table{bias_room, BiasTable::pitch_of(g.reach + RT * 16 + BN)};
+    const int W = g.reach + RT * 16 + BN;                      // (a wavefront looks up no places but those of its own tiles)
+    const BiasTable table{bias_room, BiasTable::pitch_of(W)};
+    int bucket[(2 * (kMaxReach + RT * 16 + BN) + kThreads) / kThreads];
+    if (g.bias) BiasTable::look_up<1, kThreads>(g, W, bucket);
     int64_t t;
     int head;
     place_of_workgroup(g, g.heads, t, head);
@@ -58,17 +61,16 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
     const int steps = r.row0 < len ? (len + BN - 1) / BN : 0;      // (no queries: no keys)
     if (steps) {
         const float cs = g.scale * kLog2e;
-        const int W = min(g.reach + RT * 16, len + M) + BN;        // (a wavefront looks up no places but those of its own tiles)
         Loader<T, BN, DP, kThreads, DIRECT> next_k(g.k_stride, d), next_v(g.v_stride, d);
         next_k.begin(k_even, k, g.k_stride, 0, len, d);
         next_v.begin(v_even, v, g.v_stride, 0, len, d);
-        if (g.bias) table.fill<1, kThreads>(g, head, W);
         Fragment<T> q[RT][KC];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int c = 0; c < KC; ++c)
-                q[rt][c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, row0 + rt * 16, len, d, c);
+                q[rt][c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, row0 + rt * 16, len, d, c, lane);
+        if (g.bias) table.fill<kThreads>(g, head, W, bucket);
         next_k.finish(k_even);
         next_v.finish(v_even);
         __syncthreads();
@@ -190,7 +192,7 @@ __global__ __launch_bounds__(4 * kWave) void attention_short_kernel(AttentionArg
     typedef typename ValueTile::Place Place;
     const int d = g.d, lane = threadIdx.x & (kWave - 1), col = lane & 15, quad = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int waves = blockDim.x / kWave, of_workgroup = waves * heads_of_wave;
-    const ValueTile vt{(Place)room[wave]};
+    const ValueTile vt{(Place)room[wave], lane};
     int64_t t;
     int part;
     place_of_part(g, (g.heads + of_workgroup - 1) / of_workgroup, t, part);
@@ -231,7 +233,7 @@ __global__ __launch_bounds__(4 * kWave) void attention_short_kernel(AttentionArg
         Fragment<T> q[KC];
         if (steps) {
 #pragma unroll
-            for (int c = 0; c < KC; ++c) q[c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, r.row0, len, d, c);
+            for (int c = 0; c < KC; ++c) q[c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, r.row0, len, d, c, lane);
         }
         for (int j0 = 0; j0 < steps * BN; j0 += BN) {
             next_v.begin(vt, v, g.v_stride, j0, len, d);
@@ -239,7 +241,7 @@ __global__ __launch_bounds__(4 * kWave) void attention_short_kernel(AttentionArg
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int c = 0; c < KC; ++c) keys[h][c] = rows_of_memory(k, g.k_stride, j0 + h * 16, len, d, c);
+                for (int c = 0; c < KC; ++c) keys[h][c] = rows_of_memory(k, g.k_stride, j0 + h * 16, len, d, c, lane);
             f32x4 s[2] = {f32x4{}, f32x4{}};
             if (g.bias) {
                 if (steps > 1) look_up(j0);

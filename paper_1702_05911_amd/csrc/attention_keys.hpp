@@ -11,10 +11,13 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
     typedef Tile<T, BN, DP> QueryTile;
     __shared__ __align__(16) typename QueryTile::S q_0[QueryTile::kSize], q_1[QueryTile::kSize], g_0[QueryTile::kSize], g_1[QueryTile::kSize];
     typedef typename QueryTile::Place Place;
-    const QueryTile q_even{(Place)q_0}, q_odd{(Place)q_1}, g_even{(Place)g_0}, g_odd{(Place)g_1};
+    const QueryTile q_even{(Place)q_0, (int)threadIdx.x & (kWave - 1)}, q_odd{(Place)q_1, (int)threadIdx.x & (kWave - 1)}, g_even{(Place)g_0, (int)threadIdx.x & (kWave - 1)}, g_odd{(Place)g_1, (int)threadIdx.x & (kWave - 1)};
     __shared__ __align__(16) float powers[2][BN], deltas[2][BN];
     extern __shared__ __align__(16) float room[];
-    const BiasTable table{room, BiasTable::pitch_of(most_places<RT, BN>(g.reach))};
+    const int W = most_places<RT, BN>(g.reach);
+    const BiasTable table{room, BiasTable::pitch_of(W)};
+    int bucket[(2 * most_places<RT, BN>(kMaxReach) + kThreads) / kThreads];
+    if (g.bias) BiasTable::look_up<-1, kThreads>(g, W, bucket);
     int64_t t;
     int kv;
     place_of_workgroup(g, g.heads / g.group, t, kv);
@@ -47,14 +50,13 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
     const int from = (int)((int64_t)total * split / gridDim.y), to = (int)((int64_t)total * (split + 1) / gridDim.y);
     if (r.row0 < len && from < to) {
         const float cs = g.scale * kLog2e;
-        const int W = min(most_places<RT, BN>(g.reach), len + M + BN);
         Fragment<T> k[RT][KC], v[RT][KC];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
-                k[rt][c] = rows_of_memory(static_cast<const T*>(g.k) + r.begin * g.k_stride + (int64_t)kv * d, g.k_stride, row0 + rt * 16, len, d, c);
-                v[rt][c] = rows_of_memory(static_cast<const T*>(g.v) + r.begin * g.v_stride + (int64_t)kv * d, g.v_stride, row0 + rt * 16, len, d, c);
+                k[rt][c] = rows_of_memory(static_cast<const T*>(g.k) + r.begin * g.k_stride + (int64_t)kv * d, g.k_stride, row0 + rt * 16, len, d, c, lane);
+                v[rt][c] = rows_of_memory(static_cast<const T*>(g.v) + r.begin * g.v_stride + (int64_t)kv * d, g.v_stride, row0 + rt * 16, len, d, c, lane);
             }
         Loader<T, BN, DP, kThreads, DIRECT> next_q(g.q_stride, d), next_g(g.grad_stride, d);
         float next_power = 0.0f, next_delta = 0.0f;
@@ -80,7 +82,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
         auto step = [&](int at, int half, QueryTile qt, QueryTile gt, QueryTile q_next, QueryTile g_next) __attribute__((always_inline)) {
             const int i0 = at % steps * BN;
             if (g.bias && (i0 == 0 || at == from)) {           // another head's (the last barrier stands after the last reading of the one before)
-                table.fill<-1, kThreads>(g, kv * g.group + at / steps, W);
+                table.fill<kThreads>(g, kv * g.group + at / steps, W, bucket);
                 __syncthreads();
             }
             const bool more = at + 1 < to;

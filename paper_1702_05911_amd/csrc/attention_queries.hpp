@@ -11,10 +11,13 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
     typedef Tile<T, BN, DP> KeyTile;
     __shared__ __align__(16) typename KeyTile::S k_0[KeyTile::kSize], k_1[KeyTile::kSize], v_0[KeyTile::kSize], v_1[KeyTile::kSize];
     typedef typename KeyTile::Place Place;
-    const KeyTile k_even{(Place)k_0}, k_odd{(Place)k_1}, v_even{(Place)v_0}, v_odd{(Place)v_1};
+    const KeyTile k_even{(Place)k_0, (int)threadIdx.x & (kWave - 1)}, k_odd{(Place)k_1, (int)threadIdx.x & (kWave - 1)}, v_even{(Place)v_0, (int)threadIdx.x & (kWave - 1)}, v_odd{(Place)v_1, (int)threadIdx.x & (kWave - 1)};
     __shared__ double far_sums[2][NW];
     extern __shared__ __align__(16) float room[];              // the bias by distance, and kCopies x (2 W + 1) sums
-    const BiasTable table{room, BiasTable::pitch_of(most_places<RT, BN>(g.reach))};
+    const int W = most_places<RT, BN>(g.reach);
+    const BiasTable table{room, BiasTable::pitch_of(W)};
+    int bucket[(2 * most_places<RT, BN>(kMaxReach) + kThreads) / kThreads];
+    if (g.bias) BiasTable::look_up<1, kThreads>(g, W, bucket);
     float* const by_distance = room + 4 * table.pitch;
     int64_t t;
     int head;
@@ -43,11 +46,12 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
         const T* k = static_cast<const T*>(g.k) + r.begin * g.k_stride + (int64_t)kv * d;
         const T* v = static_cast<const T*>(g.v) + r.begin * g.v_stride + (int64_t)kv * d;
         const float cs = g.scale * kLog2e;
-        const int W = min(most_places<RT, BN>(g.reach), len + M + BN), width = 2 * W + 1;
         Loader<T, BN, DP, kThreads, DIRECT> next_k(g.k_stride, d), next_v(g.v_stride, d);
         next_k.begin(k_even, k, g.k_stride, 0, len, d);
         next_v.begin(v_even, v, g.v_stride, 0, len, d);
-        if (g.bias) table.fill<1, kThreads>(g, head, W);
+        if (g.bias) table.fill<kThreads>(g, head, W, bucket);
+        // (of the sums by distance, a short text has fewer)
+        const int S = min(W, len + M + BN), width = 2 * S + 1;
         if (parts)
             for (int i = threadIdx.x; i < kCopies * width; i += kThreads) by_distance[i] = 0.0f;
         Fragment<T> q[RT][KC], grad[RT][KC];
@@ -58,10 +62,10 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
             delta[rt] = 0.0f;
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
-                q[rt][c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, row0 + rt * 16, len, d, c);
-                grad[rt][c] = rows_of_memory(static_cast<const T*>(g.grad) + r.begin * g.grad_stride + (int64_t)head * d, g.grad_stride, row0 + rt * 16, len, d, c);
+                q[rt][c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, row0 + rt * 16, len, d, c, lane);
+                grad[rt][c] = rows_of_memory(static_cast<const T*>(g.grad) + r.begin * g.grad_stride + (int64_t)head * d, g.grad_stride, row0 + rt * 16, len, d, c, lane);
                 const f32x8 o = __builtin_convertvector(
-                    rows_of_memory(static_cast<const T*>(g.out_in) + r.begin * g.out_stride + (int64_t)head * d, g.out_stride, row0 + rt * 16, len, d, c), f32x8);
+                    rows_of_memory(static_cast<const T*>(g.out_in) + r.begin * g.out_stride + (int64_t)head * d, g.out_stride, row0 + rt * 16, len, d, c, lane), f32x8);
                 const f32x8 y = __builtin_convertvector(grad[rt][c], f32x8) * o;
                 delta[rt] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
             }
@@ -77,7 +81,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
         next_v.finish(v_even);
         __syncthreads();
         const float before = g.bias ? table.v[0] : 0.0f, behind = g.bias ? table.v[2 * W] : 0.0f;
-        float* const mine = by_distance + (wave * 4 + quad) * width + W;
+        float* const mine = by_distance + (wave * 4 + quad) * width + S;
         auto step = [&](int j0, KeyTile kt, KeyTile vt, KeyTile k_next, KeyTile v_next) __attribute__((always_inline)) {
             const bool more = j0 + BN < len;
             if (more) {
@@ -193,7 +197,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
 #pragma unroll
                 for (int x = 1; x < kCopies; ++x) sum += by_distance[x * width + i];
                 by_distance[i] = sum;
-                by_distance[width + i] = __int_as_float(g.distances[max(-g.reach, min(i - W, g.reach)) + g.reach]);
+                by_distance[width + i] = __int_as_float(g.distances[max(-g.reach, min(i - S, g.reach)) + g.reach]);
             }
             __syncthreads();
             // eight lanes a bucket
