@@ -305,6 +305,7 @@ __device__ __forceinline__ void place_of_part(const AttentionArgs& g, int parts,
 
 // Lanes of a wavefront meet: what one wrote to LDS another may read, in program order.
 __device__ __forceinline__ void wave_meets() {
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");       // (loads to LDS may overwrite what is read by then)
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");

@@ -12,7 +12,7 @@ namespace {
 
 // Weights are held as 2^(z - m + kShift), m the running maximum up to 2^kSlack: it follows the true one only when a logit passes it by that much, so that
 // most tiles rescale nothing.  f16 ones are lifted by 2^6: their least normal number is 2^-14, and small weights of long texts add up.
-constexpr float kSlack = 8.0f;
+constexpr float kSlack = 8.0f, kMostWeight = 0x1p14f;
 template <typename T> struct Shift { static constexpr float value = 0.0f; };
 template <> struct Shift<Half> { static constexpr float value = 6.0f; };
 
@@ -107,40 +107,46 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
                             for (int rt = 0; rt < RT; ++rt) s[rt][h][e] = j0 + (c + h) * 16 + quad * 4 + e < len ? s[rt][h][e] : -__builtin_inff();
                     }
                 }
-                float top[RT];
+                // The weights under the maximum as it is.  Their sum tells whether one of them passes it by far -- sixteen of them are compared at once, which
+                // needs no largest one -- and then, seldom, they are taken again.
+                Fragment<T> p[RT][kPart / 2];
+                float sum[RT];
+                auto weigh = [&]() __attribute__((always_inline)) {
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        const float off = Shift<T>::value - m[rt] * cs;
+                        f32x4 sums = f32x4{}, w[kPart];
+#pragma unroll
+                        for (int h = 0; h < kPart; ++h) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) w[h][e] = exp2_of(__builtin_fmaf(s[rt][h][e], cs, off));
+                            sums = sums + w[h];
+                        }
+                        sum[rt] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+#pragma unroll
+                        for (int h = 0; h < kPart / 2; ++h) p[rt][h] = fragment_of<T>(w[2 * h], w[2 * h + 1]);
+                    }
+                };
+                weigh();
                 bool rises = false;
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    top[rt] = s[rt][0][0];
-#pragma unroll
-                    for (int h = 0; h < kPart; ++h) top[rt] = fmaxf(fmaxf(fmaxf(top[rt], s[rt][h][0]), fmaxf(s[rt][h][1], s[rt][h][2])), s[rt][h][3]);
-                    rises |= (top[rt] - m[rt]) * cs > kSlack;
-                }
+                for (int rt = 0; rt < RT; ++rt) rises |= !(sum[rt] <= kMostWeight);
                 if (__any(rises)) {
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
-                        const float now = fmaxf(m[rt], max_of_groups(top[rt])), keep = exp2_of((m[rt] - now) * cs);
+                        float top = s[rt][0][0];
+#pragma unroll
+                        for (int h = 0; h < kPart; ++h) top = fmaxf(fmaxf(fmaxf(top, s[rt][h][0]), fmaxf(s[rt][h][1], s[rt][h][2])), s[rt][h][3]);
+                        const float now = fmaxf(m[rt], max_of_groups(top)), keep = exp2_of((m[rt] - now) * cs);
                         m[rt] = now;
                         l[rt] *= keep;
 #pragma unroll
                         for (int b = 0; b < DT; ++b) o[rt][b] = o[rt][b] * keep;
                     }
+                    weigh();
                 }
-                Fragment<T> p[RT][kPart / 2];
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const float off = Shift<T>::value - m[rt] * cs;
-                    f32x4 sum = f32x4{};
-#pragma unroll
-                    for (int h = 0; h < kPart; ++h) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[rt][h][e] = exp2_of(__builtin_fmaf(s[rt][h][e], cs, off));
-                        sum = sum + s[rt][h];
-                    }
-                    l[rt] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
-                    for (int h = 0; h < kPart / 2; ++h) p[rt][h] = fragment_of<T>(s[rt][2 * h], s[rt][2 * h + 1]);
-                }
+                for (int rt = 0; rt < RT; ++rt) l[rt] += sum[rt];
 #pragma unroll
                 for (int h = 0; h < kPart / 2; ++h)
 #pragma unroll

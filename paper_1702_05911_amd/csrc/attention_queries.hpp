@@ -5,7 +5,7 @@
 namespace pqt {
 namespace {
 
-template <typename T, int DP, int NW, int RT, int BN, bool DIRECT>
+template <typename T, int DP, int NW, int RT, int BN, bool DIRECT, bool RUNS>
 __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void attention_query_gradient_kernel(AttentionArgs g) {
     constexpr int kThreads = NW * kWave, M = NW * RT * 16, KC = DP / 32, DT = DP / 16, kCopies = NW * 4;
     typedef Tile<T, BN, DP> KeyTile;
@@ -82,15 +82,16 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
         __syncthreads();
         const float before = g.bias ? table.v[0] : 0.0f, behind = g.bias ? table.v[2 * W] : 0.0f;
         float* const mine = by_distance + (wave * 4 + quad) * width + S;
-        auto step = [&](int j0, KeyTile kt, KeyTile vt, KeyTile k_next, KeyTile v_next) __attribute__((always_inline)) {
-            const bool more = j0 + BN < len;
-            if (more) {
+        auto step = [&](auto kind, int j0, KeyTile kt, KeyTile vt, KeyTile k_next, KeyTile v_next) __attribute__((always_inline)) {
+            constexpr int kKind = decltype(kind)::value;
+            if constexpr (kKind != kLast) {
                 next_k.begin(k_next, k, g.k_stride, j0 + BN, len, d);
                 next_v.begin(v_next, v, g.v_stride, j0 + BN, len, d);
             }
             const int low = j0 - (row0 + RT * 16 - 1), high = j0 + BN - 1 - row0;
-            const bool near = g.bias && high > -g.reach && low < g.reach;
+            const bool near = kKind == kNear || (kKind != kFar && g.bias && high > -g.reach && low < g.reach);
             const float far = low >= g.reach ? behind : before;
+            const f32x4 all_far = f32x4{far, far, far, far};
             const float* at = table.from(j0 + quad * 4 - row0 - col + W);
             float carry[RT], far_sum = 0.0f;
 #pragma unroll
@@ -102,14 +103,14 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
                 for (int h = 0; h < 2; ++h) {
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
-                        s[rt][h] = near ? four_of(at + c * 32 + h * 16 - rt * 16) : f32x4{far, far, far, far};
+                        if constexpr (kKind != kFar) s[rt][h] = near ? four_of(at + c * 32 + h * 16 - rt * 16) : all_far;
                         dp[rt][h] = f32x4{};
                     }
 #pragma unroll
                     for (int x = 0; x < KC; ++x) {
                         const Fragment<T> f = kt.rows(c * 32 + h * 16, x);
 #pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) s[rt][h] = multiply(f, q[rt][x], s[rt][h]);
+                        for (int rt = 0; rt < RT; ++rt) s[rt][h] = multiply(f, q[rt][x], kKind == kFar && x == 0 ? all_far : s[rt][h]);
                     }
 #pragma unroll
                     for (int x = 0; x < KC; ++x) {
@@ -126,10 +127,9 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             s[rt][h][e] = exp2_of(__builtin_fmaf(s[rt][h][e], cs, -power[rt])) * __builtin_fmaf(dp[rt][h][e], factor[rt], -delta[rt]);
-                        if (j0 + c * 32 + 32 > len) {          // places behind the text's last token
+                        if constexpr (kKind == kLast) {        // places behind the text's last token
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (j0 + c * 32 + h * 16 + quad * 4 + e >= len) s[rt][h][e] = 0.0f;
+                            for (int e = 0; e < 4; ++e) s[rt][h][e] = j0 + c * 32 + h * 16 + quad * 4 + e < len ? s[rt][h][e] : 0.0f;
                         }
                     }
                     if (parts) {
@@ -164,24 +164,26 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
                 } else if (low >= g.reach) far_right += far_sum;
                 else far_left += far_sum;
             }
-            if constexpr (sizeof(T) == 2)
-                if (parts)
+            if constexpr (kKind != kLast) {
+                if constexpr (sizeof(T) == 2) {
+                    if (parts) {
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        factor[rt] = -factor[rt];
+                        for (int rt = 0; rt < RT; ++rt) {
+                            factor[rt] = -factor[rt];
 #pragma unroll
-                        for (int x = 0; x < KC; ++x) negate<T>(grad[rt][x]);
+                            for (int x = 0; x < KC; ++x) negate<T>(grad[rt][x]);
+                        }
                     }
-            if (more) {
+                }
                 next_k.finish(k_next);
                 next_v.finish(v_next);
             }
             __syncthreads();
         };
-        for (int j0 = 0; j0 < len; j0 += 2 * BN) {
-            step(j0, k_even, v_even, k_odd, v_odd);
-            if (j0 + BN < len) step(j0 + BN, k_odd, v_odd, k_even, v_even);
-        }
+        walk<RT, BN, RUNS>(g, row0, len, [&](auto kind, auto odd, int i) __attribute__((always_inline)) {
+            if constexpr (odd.value) step(kind, i * BN, k_odd, v_odd, k_even, v_even);
+            else step(kind, i * BN, k_even, v_even, k_odd, v_odd);
+        });
         if (parts) {
 #pragma unroll
             for (int off = 1; off < kWave; off *= 2) {
@@ -243,14 +245,17 @@ void launch_attention_queries(const AttentionArgs& args, int rows, bool direct, 
             const size_t table = g.bias ? BiasTable::bytes(most) : 0, sums = g.parts ? sizeof(float) * waves * 4 * (2 * most + 1) : 0;
             hipLaunchKernelGGL(kernel, blocks, dim3(waves * kWave), table + sums, st, g);
         };
-        auto of = [&](auto waves, auto rt, auto step) {
+        auto of = [&](auto waves, auto rt, auto step, auto runs) {
             constexpr int NW = waves.value, RT = rt.value, BN = step.value;
-            if (direct) launch(attention_query_gradient_kernel<T, DP, NW, RT, BN, true>, NW, most_places<RT, BN>(g.reach));
-            else launch(attention_query_gradient_kernel<T, DP, NW, RT, BN, false>, NW, most_places<RT, BN>(g.reach));
+            if (direct) launch(attention_query_gradient_kernel<T, DP, NW, RT, BN, true, runs.value>, NW, most_places<RT, BN>(g.reach));
+            else launch(attention_query_gradient_kernel<T, DP, NW, RT, BN, false, false>, NW, most_places<RT, BN>(g.reach));
         };
-        if (rows == 16) of(Width<1>{}, Width<1>{}, Width<32>{});
-        else if (rows == 64) of(Width<4>{}, Width<1>{}, Width<kKeys>{});
-        else of(Width<4>{}, Width<2>{}, Width<kKeys>{});
+        typedef std::integral_constant<bool, false> No;
+        typedef std::integral_constant<bool, true> Yes;
+        if (rows == 16) of(Width<1>{}, Width<1>{}, Width<32>{}, No{});
+        else if (rows == 64) of(Width<4>{}, Width<1>{}, Width<kKeys>{}, No{});
+        else if (!long_texts(g.n, g.texts)) of(Width<4>{}, Width<2>{}, Width<kKeys>{}, No{});
+        else of(Width<4>{}, Width<2>{}, Width<kKeys>{}, Yes{});
     });
 }
 
