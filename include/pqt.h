@@ -504,7 +504,7 @@ int pqt_rms_norm_gradient(const void* grad, int64_t grad_stride, const void* thr
  * lse as pqt_attention wrote them.  With p_ij = exp(z_ij - lse_i) and ds_ij = p_ij (grad_i . v_j - grad_i . out_i):
  *     dq_i = scale * sum of ds_ij k_j,  dk_j = scale * sum of ds_ij q_i,  dv_j = sum of p_ij grad_i,  dbias[head][b] = sum of ds_ij over b's distances;
  * dk and dv are sums over the heads that share them too.  Rows that pad a text get zeros, rows of no text are left or cleared as above.  The workspace is
- * asked for with buckets = 0 where there is no dbias.
+ * asked for with reach = -1 where there is no dbias.
  *
  * pqt_distance_buckets -- the usual buckets, on the host: distances (2 * far + 1 integers in host memory) for `buckets` of distances -far .. far.
  * both != 0: half of the buckets (an even number) for keys before the query and it itself, half for those behind it; else all for those before, with
@@ -515,7 +515,7 @@ int pqt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stri
                   int kv_heads, int d, const void* starts, const void* lengths, int place_bytes, int64_t texts, float scale, const float* bias,
                   int buckets, const int32_t* distances, int reach, int clear, void* out, int64_t out_stride, float* lse, int device,
                   void* hip_stream);
-size_t pqt_attention_gradient_workspace(int64_t n, int64_t texts, int heads, int kv_heads, int d, int buckets);
+size_t pqt_attention_gradient_workspace(int64_t n, int64_t texts, int heads, int kv_heads, int d, int reach);
 int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                            int64_t v_stride, const void* out, int64_t out_stride, const float* lse, int type, int64_t n, int heads, int kv_heads, int d,
                            const void* starts, const void* lengths, int place_bytes, int64_t texts, float scale, const float* bias, int buckets,

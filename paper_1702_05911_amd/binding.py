@@ -801,7 +801,7 @@ def pqt_attention_gradient(grad, q, k, v, out, lse, starts, heads, scale=None, b
     dk, dkptr, _, dkstep = _result(dk, (n, narrow), dtype, device)
     dv, dvptr, _, dvstep = _result(dv, (n, narrow), dtype, device)
     dbias = None if bias is None else torch.empty(heads, buckets, dtype=torch.float32, device=device)
-    nbytes = _lib.pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, buckets)
+    nbytes = _lib.pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, -1 if bias is None else reach)
     ws = _workspace(nbytes, device)
     _check(_lib.pqt_attention_gradient(gptr, gstep, *inputs, optr, ostep, lse.data_ptr(), kind, n, heads, kv_heads, d, sptr, lptr, size, texts,
                                        d ** -0.5 if scale is None else scale, bptr, buckets, dptr, reach, 0 if grads else 1, dqptr, dqstep, dkptr, dkstep,
@@ -827,8 +827,8 @@ def pqt_rms_norm_gradient_workspace(rows, D):
     return int(_lib.pqt_rms_norm_gradient_workspace(rows, D))
 
 
-def pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, buckets):
-    return int(_lib.pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, buckets))
+def pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, reach):
+    return int(_lib.pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, reach))
 
 
 def last_error():

@@ -30,7 +30,7 @@ struct AttentionArgs {
     void* dk;
     void* dv;
     float* delta;                          // heads x n
-    float* parts;                          // workgroups x buckets
+    float* parts;                          // workgroups x distances -reach .. reach
     float* key_parts;                      // splits x heads of keys x n x (dk, dv), where the queries of a key are shared out
     int64_t q_stride, k_stride, v_stride, grad_stride, out_stride, dq_stride, dk_stride, dv_stride;
     int64_t n, texts;
@@ -344,13 +344,13 @@ struct BiasTable {
             if (n * THREADS <= 2 * W && i <= 2 * W) bucket[n] = g.distances[max(-g.reach, min(SIGN * (i - W), g.reach)) + g.reach];
         }
     }
-    // ... and a head's bias of them
+    // ... and a head's bias of them, and of the two ends: of the distances up to S, which a short text does not pass
     template <int THREADS, int N>
-    __device__ __forceinline__ void fill(const AttentionArgs& g, int head, int W, const int (&bucket)[N]) const {
+    __device__ __forceinline__ void fill(const AttentionArgs& g, int head, int W, int S, const int (&bucket)[N]) const {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int i = threadIdx.x % THREADS + n * THREADS;
-            if (n * THREADS > 2 * W || i > 2 * W) continue;
+            if (n * THREADS > W + S || i < W - S || i > W + S) continue;
             const float b = (unsigned)bucket[n] < (unsigned)g.buckets ? scaled_bias(g.bias[(int64_t)head * g.buckets + bucket[n]], g.scale) : 0.0f;     // (no bucket: no bias)
 #pragma unroll
             for (int c = 0; c < 4; ++c)
@@ -473,7 +473,7 @@ inline int heads_of_a_wavefront(int64_t tiles, int heads, int waves) {
 inline int rows_of_a_workgroup(int64_t n, int64_t texts, int heads) {
     const int64_t mean = texts ? n / texts : 0;
     if (short_texts(n, texts) || n / 64 * heads < 256) return 16;
-    return mean <= 128 || n / 128 * heads < 512 ? 64 : 128;
+    return mean <= 128 || n / 128 * heads < 384 ? 64 : 128;
 }
 inline bool long_texts(int64_t n, int64_t texts) { return texts > 0 && n / texts > 1024; }
 

@@ -30,7 +30,27 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* parts, int64_t 
     out[blockIdx.y * columns + c] = (float)s;
 }
 
-// dk and dv from the parts of shared out queries: a wavefront a row, in the splits' order
+// dbias: a workgroup a head adds up `rows` parts (or joined parts) of every distance, and then the distances of every bucket, in 64 bits and a fixed order.
+__global__ __launch_bounds__(256) void bucket_kernel(const float* parts, int rows, AttentionArgs g, float* dbias) {
+    __shared__ double sums[2 * kMaxReach + 1];
+    __shared__ int bucket[2 * kMaxReach + 1];
+    const int distances = 2 * g.reach + 1;
+    for (int i = threadIdx.x; i < distances; i += 256) {
+        double s = 0.0;
+#pragma unroll 8
+        for (int r = 0; r < rows; ++r) s += parts[((int64_t)r * g.heads + blockIdx.x) * distances + i];
+        sums[i] = s;
+        bucket[i] = g.distances[i];
+    }
+    __syncthreads();
+    for (int b = threadIdx.x; b < g.buckets; b += 256) {
+        double s = 0.0;
+        for (int i = 0; i < distances; ++i) s += bucket[i] == b ? sums[i] : 0.0;
+        dbias[(int64_t)blockIdx.x * g.buckets + b] = (float)s;
+    }
+}
+
+// dk and dv from the parts of shared out queries, four values a thread at a time, in the splits' order
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void key_join_kernel(AttentionArgs g, int splits) {
     int64_t t;
@@ -39,17 +59,19 @@ __global__ __launch_bounds__(256) void key_join_kernel(AttentionArgs g, int spli
     place_of_workgroup(g, kv_heads, t, kv);
     const Rows r = rows_of_workgroup<64>(g, t);
     if (!r.mine || !r.text) return;
-    const int lane = threadIdx.x & (kWave - 1);
-    for (int row = r.row0 + threadIdx.x / kWave; row < min(r.row0 + 64, r.span); row += 256 / kWave) {
-        for (int c = lane * 4; c < 2 * DP; c += kWave * 4) {
-            f32x4 sum = f32x4{};
-            if (row < r.len)
-                for (int s = 0; s < splits; ++s)
-                    sum = sum + *reinterpret_cast<const f32x4*>(g.key_parts + (((int64_t)s * kv_heads + kv) * g.n + r.begin + row) * (2 * DP) + c);
-            const int x = c < DP ? c : c - DP;
-            T* to = c < DP ? static_cast<T*>(g.dk) + (r.begin + row) * g.dk_stride : static_cast<T*>(g.dv) + (r.begin + row) * g.dv_stride;
-            store_piece<T, 4>(to + (int64_t)kv * g.d + x, sum, g.d - x);
+    const int rows = min(64, r.span - r.row0);
+    const int64_t apart = (int64_t)kv_heads * g.n * (2 * DP);
+    for (int e = threadIdx.x; e < rows * (2 * DP / 4); e += 256) {
+        const int row = r.row0 + e / (2 * DP / 4), c = e % (2 * DP / 4) * 4, x = c < DP ? c : c - DP;
+        if (x >= g.d) continue;
+        f32x4 sum = f32x4{};
+        if (row < r.len) {
+            const float* part = g.key_parts + ((int64_t)kv * g.n + r.begin + row) * (2 * DP) + c;
+#pragma unroll 4
+            for (int s = 0; s < splits; ++s) sum = sum + *reinterpret_cast<const f32x4*>(part + s * apart);
         }
+        T* to = c < DP ? static_cast<T*>(g.dk) + (r.begin + row) * g.dk_stride : static_cast<T*>(g.dv) + (r.begin + row) * g.dv_stride;
+        store_piece<T, 4>(to + (int64_t)kv * g.d + x, sum, g.d - x);
     }
 }
 
@@ -57,24 +79,26 @@ __global__ __launch_bounds__(256) void key_join_kernel(AttentionArgs g, int spli
 struct GradientPlan {
     int rows;                              // of a workgroup
     int splits;                            // workgroups that share out a key's queries
-    int runs;                              // of the bias' parts that are joined side by side
+    int runs;                              // of the bias' parts that are joined side by side; 0: few parts, none are
     int64_t tiles, parts, key_parts, joined, all;
 };
-inline GradientPlan gradient_plan(int64_t n, int64_t texts, int heads, int kv_heads, int d, int buckets) {
+// (reach: -1 where there is no dbias)
+inline GradientPlan gradient_plan(int64_t n, int64_t texts, int heads, int kv_heads, int d, int reach) {
     GradientPlan p{};
     p.rows = rows_of_a_workgroup(n, texts, heads);
     p.tiles = n / p.rows + texts + 1;
-    // few workgroups have keys: up to eight share the queries, of which each has four tiles at least
+    // few workgroups have keys: up to four share the queries, of which each has four tiles at least
     const int64_t busy = std::max<int64_t>(1, n / p.rows) * kv_heads, of_a_key = (texts ? n / texts : 0) * (heads / kv_heads) / (4 * 64);
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, of_a_key), 768 / busy));
-    p.runs = (int)std::min<int64_t>(64, std::max<int64_t>(1, p.tiles / 256));
-    const int64_t columns = (int64_t)heads * buckets;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(4, of_a_key), 768 / busy));
+    p.runs = p.tiles > 64 ? (int)std::min<int64_t>(64, p.tiles / 32) : 0;
+    const int64_t columns = (int64_t)heads * (2 * reach + 1);
+    const bool sums = reach >= 0;
     int width = 0;
     with_head(d, [&](auto dp) { width = dp.value; });
     p.parts = (heads * n + 3) / 4 * 4;
-    p.key_parts = p.parts + (p.tiles * columns + 3) / 4 * 4;
+    p.key_parts = p.parts + (sums ? (p.tiles * columns + 3) / 4 * 4 : 0);
     p.joined = p.key_parts + (p.splits > 1 ? (int64_t)p.splits * kv_heads * n * 2 * width : 0);
-    p.all = p.joined + (p.runs > 1 ? p.runs * columns : 0);
+    p.all = p.joined + (sums ? p.runs * columns : 0);
     return p;
 }
 
@@ -83,10 +107,10 @@ inline GradientPlan gradient_plan(int64_t n, int64_t texts, int heads, int kv_he
 
 extern "C" {
 
-size_t pqt_attention_gradient_workspace(int64_t n, int64_t texts, int heads, int kv_heads, int d, int buckets) {
+size_t pqt_attention_gradient_workspace(int64_t n, int64_t texts, int heads, int kv_heads, int d, int reach) {
     using namespace pqt;
     if (n < 1 || texts < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || d < 1 || d > kMaxHeadD || n > kMaxRows || texts > kMaxRows || heads > 65535) return 0;
-    return (size_t)gradient_plan(n, texts, heads, kv_heads, d, std::max(0, std::min(buckets, kMaxBuckets))).all * sizeof(float);
+    return (size_t)gradient_plan(n, texts, heads, kv_heads, d, std::max(-1, std::min(reach, kMaxReach))).all * sizeof(float);
 }
 
 int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
@@ -106,7 +130,7 @@ int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q,
     if (!aligned_to(grad, eb) || !aligned_to(q, eb) || !aligned_to(k, eb) || !aligned_to(v, eb) || !aligned_to(out, eb) || !aligned_to(dq, eb) || !aligned_to(dk, eb) ||
         !aligned_to(dv, eb) || !aligned_to(lse, 4) || !aligned_to(dbias, 4))
         return fail(PQT_EINVAL, "pqt_attention_gradient: a pointer is not aligned to its element");
-    const size_t need = pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, dbias ? buckets : 0);
+    const size_t need = pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, dbias ? reach : -1);
     if (need && (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)))
         return fail(PQT_EINVAL, "pqt_attention_gradient: workspace of %zu bytes, aligned to 16, needed (%zu given)", need, workspace_bytes);
     if (n == 0 && !dbias) return PQT_OK;
@@ -114,9 +138,8 @@ int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q,
     DeviceGuard guard(device);
     if (!guard.ok) return fail(PQT_EHIP, "cannot select GPU %d", device);
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-    const int64_t columns = (int64_t)heads * buckets;
     if (n > 0) {
-        const GradientPlan plan = gradient_plan(n, texts, heads, kv_heads, d, dbias ? buckets : 0);
+        const GradientPlan plan = gradient_plan(n, texts, heads, kv_heads, d, dbias ? reach : -1);
         float* const at = static_cast<float*>(workspace);
         g.grad = grad;
         g.q = q;
@@ -153,13 +176,14 @@ int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q,
         });
         HIP_TRY(hipGetLastError());
         if (dbias) {
-            const unsigned across = (unsigned)((columns + kWave - 1) / kWave);
-            hipLaunchKernelGGL(join_kernel, dim3(across, (unsigned)plan.runs), dim3(1024), 0, st, g.parts, g.tiles, columns, plan.runs > 1 ? at + plan.joined : dbias);
-            if (plan.runs > 1) hipLaunchKernelGGL(join_kernel, dim3(across), dim3(1024), 0, st, at + plan.joined, (int64_t)plan.runs, columns, dbias);
+            const int64_t columns = (int64_t)heads * (2 * reach + 1);
+            if (plan.runs)
+                hipLaunchKernelGGL(join_kernel, dim3((unsigned)((columns + kWave - 1) / kWave), (unsigned)plan.runs), dim3(1024), 0, st, g.parts, g.tiles, columns, at + plan.joined);
+            hipLaunchKernelGGL(bucket_kernel, dim3((unsigned)heads), dim3(256), 0, st, plan.runs ? at + plan.joined : g.parts, plan.runs ? plan.runs : (int)g.tiles, g, dbias);
             HIP_TRY(hipGetLastError());
         }
     } else {
-        hipLaunchKernelGGL(join_kernel, dim3((unsigned)((columns + kWave - 1) / kWave)), dim3(1024), 0, st, static_cast<const float*>(nullptr), (int64_t)0, columns, dbias);
+        hipLaunchKernelGGL(bucket_kernel, dim3((unsigned)heads), dim3(256), 0, st, static_cast<const float*>(nullptr), 0, g, dbias);
         HIP_TRY(hipGetLastError());
     }
     return PQT_OK;

@@ -70,7 +70,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
 #pragma unroll
             for (int c = 0; c < KC; ++c)
                 q[rt][c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, row0 + rt * 16, len, d, c, lane);
-        if (g.bias) table.fill<kThreads>(g, head, W, bucket);
+        if (g.bias) table.fill<kThreads>(g, head, W, min(W, len + M + BN), bucket);
         next_k.finish(k_even);
         next_v.finish(v_even);
         __syncthreads();

@@ -6,7 +6,7 @@ namespace pqt {
 namespace {
 
 template <typename T, int DP, int NW, int RT, int BN, bool DIRECT, bool RUNS>
-__global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void attention_query_gradient_kernel(AttentionArgs g) {
+__global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 256 ? 2 : 1) void attention_query_gradient_kernel(AttentionArgs g) {
     constexpr int kThreads = NW * kWave, M = NW * RT * 16, KC = DP / 32, DT = DP / 16, kCopies = NW * 4;
     typedef Tile<T, BN, DP> KeyTile;
     __shared__ __align__(16) typename KeyTile::S k_0[KeyTile::kSize], k_1[KeyTile::kSize], v_0[KeyTile::kSize], v_1[KeyTile::kSize];
@@ -14,7 +14,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
     const KeyTile k_even{(Place)k_0, (int)threadIdx.x & (kWave - 1)}, k_odd{(Place)k_1, (int)threadIdx.x & (kWave - 1)}, v_even{(Place)v_0, (int)threadIdx.x & (kWave - 1)}, v_odd{(Place)v_1, (int)threadIdx.x & (kWave - 1)};
     __shared__ double far_sums[2][NW];
     extern __shared__ __align__(16) float room[];              // the bias by distance, and kCopies x (2 W + 1) sums
-    const int W = most_places<RT, BN>(g.reach);
+    const int W = most_places<RT, BN>(g.reach), width = 2 * W + 1;
     const BiasTable table{room, BiasTable::pitch_of(W)};
     int bucket[(2 * most_places<RT, BN>(kMaxReach) + kThreads) / kThreads];
     if (g.bias) BiasTable::look_up<1, kThreads>(g, W, bucket);
@@ -25,15 +25,16 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
     const Rows r = rows_of_workgroup<M>(g, t);
     const int d = g.d, lane = threadIdx.x & (kWave - 1), col = lane & 15, quad = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     T* dq = static_cast<T*>(g.dq) + (int64_t)head * d;
-    float* parts = g.parts ? g.parts + (t * g.heads + head) * g.buckets : nullptr;
+    const int distances = 2 * g.reach + 1;
+    float* parts = g.parts ? g.parts + (t * g.heads + head) * distances : nullptr;
     if (r.mine && (r.before || !r.text)) {                     // rows of no text
         const int64_t from = r.before ? r.begin - r.before : r.begin + r.row0;
         clear_rows(dq, g.dq_stride, from, r.before && r.text ? r.begin : min(r.begin + r.row0 + M, r.begin + r.span), d);
     }
-    const int len = r.len, row0 = r.row0 + wave * RT * 16;
+    const int len = r.len, row0 = r.row0 + wave * RT * 16, S = min(W, len + M + BN);
     const bool work = r.mine && r.text && r.row0 < len;
     if (!work && parts)
-        for (int b = threadIdx.x; b < g.buckets; b += kThreads) parts[b] = 0.0f;
+        for (int i = threadIdx.x; i < distances; i += kThreads) parts[i] = 0.0f;
     if (!r.mine || !r.text) return;
     f32x4 sums[RT][DT];
     Lift<T> lift[RT];
@@ -49,11 +50,11 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
         Loader<T, BN, DP, kThreads, DIRECT> next_k(g.k_stride, d), next_v(g.v_stride, d);
         next_k.begin(k_even, k, g.k_stride, 0, len, d);
         next_v.begin(v_even, v, g.v_stride, 0, len, d);
-        if (g.bias) table.fill<kThreads>(g, head, W, bucket);
-        // (of the sums by distance, a short text has fewer)
-        const int S = min(W, len + M + BN), width = 2 * S + 1;
+        if (g.bias) table.fill<kThreads>(g, head, W, S, bucket);
+        // (of the sums by distance, a short text needs fewer)
         if (parts)
-            for (int i = threadIdx.x; i < kCopies * width; i += kThreads) by_distance[i] = 0.0f;
+            for (int x = 0; x < kCopies; ++x)
+                for (int i = W - S + threadIdx.x; i <= W + S; i += kThreads) by_distance[x * width + i] = 0.0f;
         Fragment<T> q[RT][KC], grad[RT][KC];
         float delta[RT], power[RT], factor[RT];
 #pragma unroll
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
         next_v.finish(v_even);
         __syncthreads();
         const float before = g.bias ? table.v[0] : 0.0f, behind = g.bias ? table.v[2 * W] : 0.0f;
-        float* const mine = by_distance + (wave * 4 + quad) * width + S;
+        float* const mine = by_distance + (wave * 4 + quad) * width + W;
         auto step = [&](auto kind, int j0, KeyTile kt, KeyTile vt, KeyTile k_next, KeyTile v_next) __attribute__((always_inline)) {
             constexpr int kKind = decltype(kind)::value;
             if constexpr (kKind != kLast) {
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
                                 const f32x4 v = s[rt][h];
                                 const float sum = ((carry[rt] + v[0]) + from_right<1>(v[1])) + (from_right<2>(v[2]) + from_right<3>(v[3]));
                                 carry[rt] = from_left<15>(v[1]) + from_left<14>(v[2]) + from_left<13>(v[3]);
-                                mine[j0 + c * 32 + h * 16 + quad * 4 - (row0 + rt * 16) - col] += sum;
+                                add_to(mine + j0 + c * 32 + h * 16 + quad * 4 - (row0 + rt * 16) - col, sum);
                             }
                         } else {
                             const f32x4 both = s[rt][0] + s[rt][1];
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
             if (parts) {
                 if (near) {
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) mine[j0 + BN + quad * 4 - (row0 + rt * 16) - col] += carry[rt];
+                    for (int rt = 0; rt < RT; ++rt) add_to(mine + j0 + BN + quad * 4 - (row0 + rt * 16) - col, carry[rt]);
                 } else if (low >= g.reach) far_right += far_sum;
                 else far_left += far_sum;
             }
@@ -194,26 +195,36 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
                 far_sums[0][wave] = far_left;
                 far_sums[1][wave] = far_right;
             }
-            for (int i = threadIdx.x; i < width; i += kThreads) {
+            // the sums of the distances nearer than `reach`; what lies farther has its ends' buckets and is added up
+            auto sum_of = [&](int i) __attribute__((always_inline)) {
                 float sum = by_distance[i];
 #pragma unroll
                 for (int x = 1; x < kCopies; ++x) sum += by_distance[x * width + i];
-                by_distance[i] = sum;
-                by_distance[width + i] = __int_as_float(g.distances[max(-g.reach, min(i - S, g.reach)) + g.reach]);
+                return sum;
+            };
+            for (int i = threadIdx.x + 1; i < distances - 1; i += kThreads) {
+                const int at = i - g.reach;
+                parts[i] = at >= -S && at <= S ? sum_of(W + at) : 0.0f;
             }
             __syncthreads();
-            // eight lanes a bucket
-            const int first = g.distances[0], last = g.distances[2 * g.reach];
-            for (int e = threadIdx.x; e < g.buckets * 8; e += kThreads) {
-                const int b = e >> 3;
+            for (int side = wave; side < 2; side += NW) {
                 double sum = 0.0;
-                for (int i = e & 7; i < width; i += 8) sum += __float_as_int(by_distance[width + i]) == b ? by_distance[i] : 0.0f;
+                for (int at = g.reach + lane; at <= S; at += kWave) sum += sum_of(W + (side ? at : -at));
 #pragma unroll
-                for (int off = 1; off < 8; off *= 2) sum += __shfl_xor(sum, off, kWave);
-                if ((e & 7) == 0) {
+                for (int off = 1; off < kWave; off *= 2) sum += __shfl_xor(sum, off, kWave);
 #pragma unroll
-                    for (int w = 0; w < NW; ++w) sum += (first == b ? far_sums[0][w] : 0.0) + (last == b ? far_sums[1][w] : 0.0);
-                    parts[b] = (float)sum;
+                for (int w = 0; w < NW; ++w) sum += far_sums[side][w];
+                // (a reach of 0 has one bucket, both sides' and the middle's: the middle counts once)
+                if (g.reach > 0) {
+                    if (lane == 0) parts[side ? distances - 1 : 0] = (float)sum;
+                } else if (side == 0) {
+                    double right = 0.0;
+                    for (int at = 1 + lane; at <= S; at += kWave) right += sum_of(W + at);
+#pragma unroll
+                    for (int off = 1; off < kWave; off *= 2) right += __shfl_xor(right, off, kWave);
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) right += far_sums[1][w];
+                    if (lane == 0) parts[0] = (float)(sum + right);
                 }
             }
         }

@@ -805,9 +805,9 @@ def test_refusals_of_the_library(library_without_gpu):
     assert lib.pqt_attention_gradient(*call(n=0, db=None)) == pqt.PQT_OK
     for fine in (dict(), dict(lengths=None, bias=None, buckets=0, dist=None, reach=0, db=None), dict(db=None)):
         refused(lib.pqt_attention_gradient, *call(**fine), code=pqt.PQT_EHIP)
-    assert pqt.pqt_attention_gradient_workspace(0, 1, 2, 2, 64, 3) == 0 and pqt.pqt_attention_gradient_workspace(100, 2, 4, 3, 64, 0) == 0
-    assert pqt.pqt_attention_gradient_workspace(100, 2, 4, 4, 200, 0) == 0 and pqt.pqt_attention_gradient_workspace(100, 2, 4, 1, 64, 0) >= 1600
-    assert pqt.pqt_attention_gradient_workspace(100, 2, 4, 4, 64, 32) > pqt.pqt_attention_gradient_workspace(100, 2, 4, 4, 64, 0)
+    assert pqt.pqt_attention_gradient_workspace(0, 1, 2, 2, 64, 3) == 0 and pqt.pqt_attention_gradient_workspace(100, 2, 4, 3, 64, -1) == 0
+    assert pqt.pqt_attention_gradient_workspace(100, 2, 4, 4, 200, -1) == 0 and pqt.pqt_attention_gradient_workspace(100, 2, 4, 1, 64, -1) >= 1600
+    assert pqt.pqt_attention_gradient_workspace(100, 2, 4, 4, 64, 0) > pqt.pqt_attention_gradient_workspace(100, 2, 4, 4, 64, -1)
 
 
 def test_refusals_of_the_binding():
