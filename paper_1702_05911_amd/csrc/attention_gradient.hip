@@ -30,23 +30,34 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* parts, int64_t 
     out[blockIdx.y * columns + c] = (float)s;
 }
 
-// dbias: a workgroup a head adds up `rows` parts (or joined parts) of every distance, and then the distances of every bucket, in 64 bits and a fixed order.
-__global__ __launch_bounds__(256) void bucket_kernel(const float* parts, int rows, AttentionArgs g, float* dbias) {
-    __shared__ double sums[2 * kMaxReach + 1];
+// dbias: a workgroup a head adds up `rows` parts (or joined parts) of every distance, every fourth by a quarter of its threads, and then the distances of every
+// bucket, eight lanes each; in 64 bits and a fixed order.
+__global__ __launch_bounds__(1024) void bucket_kernel(const float* parts, int rows, AttentionArgs g, float* dbias) {
+    __shared__ double sums[4][2 * kMaxReach + 1];
     __shared__ int bucket[2 * kMaxReach + 1];
-    const int distances = 2 * g.reach + 1;
-    for (int i = threadIdx.x; i < distances; i += 256) {
+    const int distances = 2 * g.reach + 1, quarter = threadIdx.x >> 8;
+    for (int i = threadIdx.x & 255; i < distances; i += 256) {
+        if (quarter == 0) bucket[i] = g.distances[i];
         double s = 0.0;
-#pragma unroll 8
-        for (int r = 0; r < rows; ++r) s += parts[((int64_t)r * g.heads + blockIdx.x) * distances + i];
-        sums[i] = s;
-        bucket[i] = g.distances[i];
+        for (int r0 = quarter; r0 < rows; r0 += 4 * 16) {      // sixteen on their way
+            float v[16];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) v[u] = parts[((int64_t)min(r0 + 4 * u, rows - 1) * g.heads + blockIdx.x) * distances + i];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) s += r0 + 4 * u < rows ? v[u] : 0.0f;
+        }
+        sums[quarter][i] = s;
     }
     __syncthreads();
-    for (int b = threadIdx.x; b < g.buckets; b += 256) {
+    for (int i = threadIdx.x; i < distances; i += 1024) sums[0][i] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+    __syncthreads();
+    for (int e = threadIdx.x; e < g.buckets * 8; e += 1024) {
         double s = 0.0;
-        for (int i = 0; i < distances; ++i) s += bucket[i] == b ? sums[i] : 0.0;
-        dbias[(int64_t)blockIdx.x * g.buckets + b] = (float)s;
+#pragma unroll 8
+        for (int i = e & 7; i < distances; i += 8) s += bucket[i] == e >> 3 ? sums[0][i] : 0.0;
+#pragma unroll
+        for (int off = 1; off < 8; off *= 2) s += __shfl_xor(s, off, kWave);
+        if ((e & 7) == 0) dbias[(int64_t)blockIdx.x * g.buckets + (e >> 3)] = (float)s;
     }
 }
 
@@ -179,11 +190,11 @@ int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q,
             const int64_t columns = (int64_t)heads * (2 * reach + 1);
             if (plan.runs)
                 hipLaunchKernelGGL(join_kernel, dim3((unsigned)((columns + kWave - 1) / kWave), (unsigned)plan.runs), dim3(1024), 0, st, g.parts, g.tiles, columns, at + plan.joined);
-            hipLaunchKernelGGL(bucket_kernel, dim3((unsigned)heads), dim3(256), 0, st, plan.runs ? at + plan.joined : g.parts, plan.runs ? plan.runs : (int)g.tiles, g, dbias);
+            hipLaunchKernelGGL(bucket_kernel, dim3((unsigned)heads), dim3(1024), 0, st, plan.runs ? at + plan.joined : g.parts, plan.runs ? plan.runs : (int)g.tiles, g, dbias);
             HIP_TRY(hipGetLastError());
         }
     } else {
-        hipLaunchKernelGGL(bucket_kernel, dim3((unsigned)heads), dim3(256), 0, st, static_cast<const float*>(nullptr), 0, g, dbias);
+        hipLaunchKernelGGL(bucket_kernel, dim3((unsigned)heads), dim3(1024), 0, st, static_cast<const float*>(nullptr), 0, g, dbias);
         HIP_TRY(hipGetLastError());
     }
     return PQT_OK;

@@ -81,7 +81,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
         };
         auto step = [&](int at, int half, QueryTile qt, QueryTile gt, QueryTile q_next, QueryTile g_next) __attribute__((always_inline)) {
             const int i0 = at % steps * BN;
-            if (g.bias && (i0 == 0 || at == from)) {           // another head's (the last barrier stands after the last reading of the one before)
+            if (g.bias && i0 == 0 && at > from) {              // another head's (the last barrier stands after the last reading of the one before)
                 table.fill<kThreads>(g, kv * g.group + at / steps, W, min(W, len + M + BN), bucket);
                 __syncthreads();
             }
@@ -145,6 +145,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
             __syncthreads();
         };
         fetch(from, q_even, g_even);
+        if (g.bias) table.fill<kThreads>(g, kv * g.group + from / steps, W, min(W, len + M + BN), bucket);
         arrive(0, q_even, g_even);
         __syncthreads();
         for (int at = from; at < to; at += 2) {

@@ -50,33 +50,40 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
         Loader<T, BN, DP, kThreads, DIRECT> next_k(g.k_stride, d), next_v(g.v_stride, d);
         next_k.begin(k_even, k, g.k_stride, 0, len, d);
         next_v.begin(v_even, v, g.v_stride, 0, len, d);
-        if (g.bias) table.fill<kThreads>(g, head, W, S, bucket);
         // (of the sums by distance, a short text needs fewer)
         if (parts)
             for (int x = 0; x < kCopies; ++x)
                 for (int i = W - S + threadIdx.x; i <= W + S; i += kThreads) by_distance[x * width + i] = 0.0f;
         Fragment<T> q[RT][KC], grad[RT][KC];
-        float delta[RT], power[RT], factor[RT];
+        float delta[RT], power[RT], factor[RT], sum[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int row = row0 + rt * 16 + col;
+            sum[rt] = row < len ? g.lse_in[(int64_t)head * g.n + r.begin + row] : -__builtin_inff();
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                q[rt][c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, row0 + rt * 16, len, d, c, lane);
+                grad[rt][c] = rows_of_memory(static_cast<const T*>(g.grad) + r.begin * g.grad_stride + (int64_t)head * d, g.grad_stride, row0 + rt * 16, len, d, c, lane);
+            }
+        }
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             const int row = row0 + rt * 16 + col;
             delta[rt] = 0.0f;
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
-                q[rt][c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, row0 + rt * 16, len, d, c, lane);
-                grad[rt][c] = rows_of_memory(static_cast<const T*>(g.grad) + r.begin * g.grad_stride + (int64_t)head * d, g.grad_stride, row0 + rt * 16, len, d, c, lane);
                 const f32x8 o = __builtin_convertvector(
                     rows_of_memory(static_cast<const T*>(g.out_in) + r.begin * g.out_stride + (int64_t)head * d, g.out_stride, row0 + rt * 16, len, d, c, lane), f32x8);
                 const f32x8 y = __builtin_convertvector(grad[rt][c], f32x8) * o;
                 delta[rt] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
             }
             delta[rt] = sum_of_groups(delta[rt]);
-            const float lse = row < len ? g.lse_in[(int64_t)head * g.n + r.begin + row] : -__builtin_inff();
             if (row < len && quad == 0) g.delta[(int64_t)head * g.n + r.begin + row] = delta[rt];
-            power[rt] = power_of(lse);
-            factor[rt] = rest_of_power(lse);
+            power[rt] = power_of(sum[rt]);
+            factor[rt] = rest_of_power(sum[rt]);
             delta[rt] *= factor[rt];
         }
+        if (g.bias) table.fill<kThreads>(g, head, W, S, bucket);
         double far_left = 0.0, far_right = 0.0;
         next_k.finish(k_even);
         next_v.finish(v_even);
