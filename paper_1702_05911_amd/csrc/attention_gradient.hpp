@@ -61,6 +61,9 @@ __device__ __forceinline__ void negate(Fragment<T>& f) {
 template <int N> __device__ __forceinline__ float from_right(float v) { return dpp_move<0x100 + N>(v); }     // of the lane N further, zero past sixteen
 template <int N> __device__ __forceinline__ float from_left(float v) { return dpp_move<0x110 + N>(v); }
 
+// From one copy of the sums by distance, -W .. W, to the next: whole pieces of four.
+__host__ __device__ constexpr int sums_pitch(int W) { return (2 * W + 4) / 4 * 4; }
+
 // Adds to a number in LDS that nobody else adds to meanwhile.  (LDS' own addition of floats is slow: 64 texts of up to 512 tokens 311 us, 179 so.)
 __device__ __forceinline__ void add_to(float* p, float v) { *p += v; }
 

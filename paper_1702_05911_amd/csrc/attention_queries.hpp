@@ -14,7 +14,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
     const KeyTile k_even{(Place)k_0, (int)threadIdx.x & (kWave - 1)}, k_odd{(Place)k_1, (int)threadIdx.x & (kWave - 1)}, v_even{(Place)v_0, (int)threadIdx.x & (kWave - 1)}, v_odd{(Place)v_1, (int)threadIdx.x & (kWave - 1)};
     __shared__ double far_sums[2][NW];
     extern __shared__ __align__(16) float room[];              // the bias by distance, and kCopies x (2 W + 1) sums
-    const int W = most_places<RT, BN>(g.reach), width = 2 * W + 1;
+    const int W = most_places<RT, BN>(g.reach), width = sums_pitch(W);
     const BiasTable table{room, BiasTable::pitch_of(W)};
     int bucket[(2 * most_places<RT, BN>(kMaxReach) + kThreads) / kThreads];
     if (g.bias) BiasTable::look_up<1, kThreads>(g, W, bucket);
@@ -51,9 +51,10 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
         next_k.begin(k_even, k, g.k_stride, 0, len, d);
         next_v.begin(v_even, v, g.v_stride, 0, len, d);
         // (of the sums by distance, a short text needs fewer)
+        const int first = (W - S) & ~3, pieces = (W + S - first) / 4 + 1;      // of four distances each
         if (parts)
             for (int x = 0; x < kCopies; ++x)
-                for (int i = W - S + threadIdx.x; i <= W + S; i += kThreads) by_distance[x * width + i] = 0.0f;
+                for (int i = threadIdx.x; i < pieces; i += kThreads) *reinterpret_cast<f32x4*>(&by_distance[x * width + first + 4 * i]) = f32x4{};
         Fragment<T> q[RT][KC], grad[RT][KC];
         float delta[RT], power[RT], factor[RT], sum[RT];
 #pragma unroll
@@ -202,21 +203,22 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
                 far_sums[0][wave] = far_left;
                 far_sums[1][wave] = far_right;
             }
-            // the sums of the distances nearer than `reach`; what lies farther has its ends' buckets and is added up
-            auto sum_of = [&](int i) __attribute__((always_inline)) {
-                float sum = by_distance[i];
+            // The sums of the distances nearer than `reach`; what lies farther has its ends' buckets and is added up.
+            for (int i = threadIdx.x; i < pieces; i += kThreads) {
+                float* const to = by_distance + first + 4 * i;
+                f32x4 sum = four_of(to);
 #pragma unroll
-                for (int x = 1; x < kCopies; ++x) sum += by_distance[x * width + i];
-                return sum;
-            };
-            for (int i = threadIdx.x + 1; i < distances - 1; i += kThreads) {
-                const int at = i - g.reach;
-                parts[i] = at >= -S && at <= S ? sum_of(W + at) : 0.0f;
+                for (int x = 1; x < kCopies; ++x) sum = sum + four_of(to + x * width);
+                *reinterpret_cast<f32x4*>(to) = sum;
             }
             __syncthreads();
+            for (int i = threadIdx.x + 1; i < distances - 1; i += kThreads) {
+                const int at = i - g.reach;
+                parts[i] = at >= -S && at <= S ? by_distance[W + at] : 0.0f;
+            }
             for (int side = wave; side < 2; side += NW) {
                 double sum = 0.0;
-                for (int at = g.reach + lane; at <= S; at += kWave) sum += sum_of(W + (side ? at : -at));
+                for (int at = g.reach + lane; at <= S; at += kWave) sum += by_distance[W + (side ? at : -at)];
 #pragma unroll
                 for (int off = 1; off < kWave; off *= 2) sum += __shfl_xor(sum, off, kWave);
 #pragma unroll
@@ -226,7 +228,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
                     if (lane == 0) parts[side ? distances - 1 : 0] = (float)sum;
                 } else if (side == 0) {
                     double right = 0.0;
-                    for (int at = 1 + lane; at <= S; at += kWave) right += sum_of(W + at);
+                    for (int at = 1 + lane; at <= S; at += kWave) right += by_distance[W + at];
 #pragma unroll
                     for (int off = 1; off < kWave; off *= 2) right += __shfl_xor(right, off, kWave);
 #pragma unroll
@@ -260,7 +262,7 @@ void launch_attention_queries(const AttentionArgs& args, int rows, bool direct, 
     with_head(g.d, [&](auto dp) {
         constexpr int DP = dp.value, kKeys = sizeof(T) == 4 && DP > 64 ? 32 : 64;
         auto launch = [&](auto kernel, int waves, int most) {
-            const size_t table = g.bias ? BiasTable::bytes(most) : 0, sums = g.parts ? sizeof(float) * waves * 4 * (2 * most + 1) : 0;
+            const size_t table = g.bias ? BiasTable::bytes(most) : 0, sums = g.parts ? sizeof(float) * waves * 4 * sums_pitch(most) : 0;
             hipLaunchKernelGGL(kernel, blocks, dim3(waves * kWave), table + sums, st, g);
         };
         auto of = [&](auto waves, auto rt, auto step, auto runs) {
