@@ -37,7 +37,7 @@ struct AttentionArgs {
     int64_t tiles;                         // workgroups of a head
     int wide;                              // starts and lengths are 64-bit numbers
     int heads, group, d, buckets, reach, clear;
-    float scale;
+    float scale, inverse_scale;
 };
 
 // The kernels are compiled for one type in a translation unit of its own (attention_bf16.hip and so on): their launchers, by the rows of a workgroup
@@ -229,6 +229,24 @@ __device__ __forceinline__ Fragment<T> rows_of_memory(const T* base, int64_t str
     return __builtin_bit_cast(Fragment<T>, v);
 }
 
+// The same where rows are whole aligned pieces, of the rows at base from 0 to last, without a branch and with the lanes' places in 32 bits: a row past the
+// last is read as that, and it is the caller who leaves it out.
+template <typename T>
+__device__ __forceinline__ Fragment<T> whole_rows_of_memory(const T* base, uint32_t stride_bytes, int row0, int last, int d, int chunk, int lane) {
+    const int c = chunk * 32 + (lane >> 4) * 8;
+    const uint32_t row = (uint32_t)min(row0 + (lane & 15), last) * stride_bytes;
+    const char* p = reinterpret_cast<const char*>(base);
+    constexpr int E = 16 / (int)sizeof(T);
+    u32x4 v[8 / E];
+#pragma unroll
+    for (int i = 0; i < 8 / E; ++i) {
+        v[i] = *reinterpret_cast<const u32x4*>(p + (row + (uint32_t)min(c + i * E, d - E) * (uint32_t)sizeof(T)));
+        if (chunk * 32 + 32 > d && c + i * E >= d) v[i] = u32x4{};
+    }
+    if constexpr (sizeof(T) == 2) return __builtin_bit_cast(Fragment<T>, v[0]);
+    else return __builtin_shufflevector(__builtin_bit_cast(f32x4, v[0]), __builtin_bit_cast(f32x4, v[1]), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
 // ---- which rows ------------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ int64_t number(const void* p, int wide, int64_t i) {
@@ -322,8 +340,8 @@ __device__ __forceinline__ void clear_rows(T* p, int64_t stride, int64_t from, i
 // of two.  Finite entries are kept within 2^90, where that multiplication (scale up to 2^32) cannot overflow; -inf stays.
 constexpr float kBiasTop = 0x1p90f, kLowest = -0x1p92f;        // (kLowest: below every finite logit)
 
-__device__ __forceinline__ float scaled_bias(float entry, float scale) {
-    const float v = entry / scale;
+__device__ __forceinline__ float scaled_bias(float entry, float inverse_scale) {
+    const float v = entry * inverse_scale;
     return fabsf(entry) < __builtin_inff() ? fmaxf(-kBiasTop, fminf(v, kBiasTop)) : v;
 }
 // The bias of the distances on either side in LDS, four times, copy c shifted by c places: the four consecutive ones that a lane needs for a
@@ -351,7 +369,7 @@ struct BiasTable {
         for (int n = 0; n < N; ++n) {
             const int i = threadIdx.x % THREADS + n * THREADS;
             if (n * THREADS > W + S || i < W - S || i > W + S) continue;
-            const float b = (unsigned)bucket[n] < (unsigned)g.buckets ? scaled_bias(g.bias[(int64_t)head * g.buckets + bucket[n]], g.scale) : 0.0f;     // (no bucket: no bias)
+            const float b = (unsigned)bucket[n] < (unsigned)g.buckets ? scaled_bias(g.bias[(int64_t)head * g.buckets + bucket[n]], g.inverse_scale) : 0.0f;     // (no bucket: no bias)
 #pragma unroll
             for (int c = 0; c < 4; ++c)
                 if (i >= c) v[c * pitch + i - c] = b;
@@ -456,6 +474,7 @@ inline int attention_checks(const char* who, int type, int64_t n, int heads, int
     g.lengths = lengths;
     g.wide = place_bytes == 8;
     g.scale = scale;
+    g.inverse_scale = 1.0f / scale;
     g.bias = bias;
     g.buckets = buckets;
     g.distances = distances;

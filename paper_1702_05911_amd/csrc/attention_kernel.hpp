@@ -227,6 +227,7 @@ __global__ __launch_bounds__(4 * kWave) void attention_short_kernel(AttentionArg
             }
     };
     if (g.bias && steps == 1) look_up(0);
+    const uint32_t q_bytes = (uint32_t)g.q_stride * (uint32_t)sizeof(T), k_bytes = (uint32_t)g.k_stride * (uint32_t)sizeof(T);
     Loader<T, BN, DP, kWave, DIRECT> next_v(g.v_stride, d);
     for (int head = head0 + wave; head < head_end; head += waves) {
         const int kv = head / g.group;
@@ -239,7 +240,11 @@ __global__ __launch_bounds__(4 * kWave) void attention_short_kernel(AttentionArg
         Fragment<T> q[KC];
         if (steps) {
 #pragma unroll
-            for (int c = 0; c < KC; ++c) q[c] = rows_of_memory(static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, r.row0, len, d, c, lane);
+            for (int c = 0; c < KC; ++c) {
+                const T* base = static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d;
+                if constexpr (DIRECT) q[c] = whole_rows_of_memory(base + r.row0 * g.q_stride, q_bytes, 0, len - 1 - r.row0, d, c, lane);
+                else q[c] = rows_of_memory(base, g.q_stride, r.row0, len, d, c, lane);
+            }
         }
         for (int j0 = 0; j0 < steps * BN; j0 += BN) {
             next_v.begin(vt, v, g.v_stride, j0, len, d);
@@ -247,7 +252,10 @@ __global__ __launch_bounds__(4 * kWave) void attention_short_kernel(AttentionArg
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int c = 0; c < KC; ++c) keys[h][c] = rows_of_memory(k, g.k_stride, j0 + h * 16, len, d, c, lane);
+                for (int c = 0; c < KC; ++c) {
+                    if constexpr (DIRECT) keys[h][c] = whole_rows_of_memory(k + j0 * g.k_stride, k_bytes, h * 16, len - 1 - j0, d, c, lane);
+                    else keys[h][c] = rows_of_memory(k, g.k_stride, j0 + h * 16, len, d, c, lane);
+                }
             f32x4 s[2] = {f32x4{}, f32x4{}};
             if (g.bias) {
                 if (steps > 1) look_up(j0);
@@ -255,8 +263,8 @@ __global__ __launch_bounds__(4 * kWave) void attention_short_kernel(AttentionArg
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float entry = g.bias[(int64_t)head * g.buckets + max(bucket[h][e], 0)];
-                        s[h][e] = bucket[h][e] < 0 ? 0.0f : scaled_bias(entry, g.scale);
+                        const float entry = scaled_bias(g.bias[(int64_t)head * g.buckets + (uint32_t)max(bucket[h][e], 0)], g.inverse_scale);
+                        s[h][e] = bucket[h][e] < 0 ? 0.0f : entry;
                     }
             }
 #pragma unroll
@@ -325,7 +333,7 @@ void launch_attention(const AttentionArgs& args, int rows, bool direct, hipStrea
         if (short_texts(g.n, g.texts)) {
             const int waves = std::min(4, g.heads), of_wave = heads_of_a_wavefront(g.tiles, g.heads, waves), parts = (g.heads + waves * of_wave - 1) / (waves * of_wave);
             const dim3 grid((unsigned)(g.tiles * parts)), threads(waves * kWave);
-            if (direct) hipLaunchKernelGGL((attention_short_kernel<T, DP, true>), grid, threads, 0, st, g, of_wave);
+            if (direct && direct_rows(g.q, g.q_stride, sizeof(T), g.d)) hipLaunchKernelGGL((attention_short_kernel<T, DP, true>), grid, threads, 0, st, g, of_wave);
             else hipLaunchKernelGGL((attention_short_kernel<T, DP, false>), grid, threads, 0, st, g, of_wave);
         } else if (rows == 16) of(Width<1>{}, Width<1>{}, Width<32>{}, No{});
         else if (rows == 64) of(Width<4>{}, Width<1>{}, Width<kKeys>{}, No{});
