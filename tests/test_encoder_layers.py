@@ -285,11 +285,16 @@ ATTENTION = [  # lengths, heads, heads of keys, d, type, buckets, reach, padded 
     ([100, 90, 0, 200, 130, 1, 99, 70, 60, 55, 300], 16, 8, 64, "bf16", 32, 128, 0, 0, 64, 5), ([400, 500, 700], 12, 3, 32, "f16", 2, 448, 0, 8, 32, 0),
     ([333, 444, 260], 16, 16, 100, "bf16", 32, 32, 500, 0, 64, 0), ([1025, 40], 16, 4, 128, "f32", 32, 128, 0, 0, 64, 0), ([777, 800], 12, 1, 96, "f16", 0, 0, 0, 1, 64, 100),
     ([1300], 16, 2, 97, "bf16", 16, 7, 0, 0, 64, 0), ([900, 200], 16, 16, 31, "f32", 33, 100, 0, 0, 64, 0), ([5000], 16, 4, 64, "bf16", 32, 128, 0, 0, 64, 3),
-    ([2100, 2050], 16, 16, 128, "f16", 32, 128, 2200, 0, 64, 0), ([4500], 16, 1, 30, "f32", 32, 200, 0, 3, 32, 0), ([4300], 16, 8, 96, "bf16", 0, 0, 0, 0, 64, 0)]
+    ([2100, 2050], 16, 16, 128, "f16", 32, 128, 2200, 0, 64, 0), ([4500], 16, 1, 30, "f32", 32, 200, 0, 3, 32, 0), ([4300], 16, 8, 96, "bf16", 0, 0, 0, 0, 64, 0),
+    # many texts of some hundred tokens; the farthest reach beside the widest heads; short texts with a long one among them; a single token a text
+    ([600, 550, 620, 580, 640, 590, 610, 570], 16, 16, 128, "bf16", 64, 448, 0, 0, 64, 0), ([600, 550, 620, 580, 640, 590, 610, 570], 16, 4, 128, "f32", 32, 448, 0, 0, 32, 3),
+    ([600, 550, 620, 580, 640, 590, 610, 0], 16, 16, 64, "f16", 32, 128, 700, 3, 64, 0), ([600, 550, 620, 580, 640, 590, 610, 570], 16, 16, 64, "bf16", 6, 2, 0, 0, 64, 1),
+    ([700] + [5] * 40 + [0, 1], 3, 1, 80, "bf16", 32, 40, 0, 0, 64, 0), ([1] * 70, 5, 5, 64, "f16", 32, 16, 0, 0, 32, 2), ([60] * 20 + [33, 64, 63, 1000], 6, 2, 128, "f32", 32, 30, 0, 0, 64, 0),
+    ([3000], 2, 1, 64, "bf16", 32, 128, 0, 0, 64, 0), ([129] * 30, 16, 16, 128, "f16", 4, 448, 130, 8, 64, 0)]
 
 
 @gpu
-@pytest.mark.parametrize("case", ATTENTION, ids=lambda c: "-".join(map(str, c)).replace(" ", ""))
+@pytest.mark.parametrize("case", ATTENTION, ids=lambda c: f"{len(c[0])}x{max(c[0])}-" + "-".join(map(str, c[1:])))
 def test_attention(case):
     lengths, heads, kv, d, kind, buckets, reach, padded, pad, ids, behind = case
     s = attention_inputs(lengths, heads, kv, d, kind, buckets, reach, padded, pad, ids, behind)
@@ -356,7 +361,7 @@ def check_gradient(s, grad, out, lse, got):
 
 
 @gpu
-@pytest.mark.parametrize("case", ATTENTION, ids=lambda c: "-".join(map(str, c)).replace(" ", ""))
+@pytest.mark.parametrize("case", ATTENTION, ids=lambda c: f"{len(c[0])}x{max(c[0])}-" + "-".join(map(str, c[1:])))
 def test_attention_gradient(case):
     lengths, heads, kv, d, kind, buckets, reach, padded, pad, ids, behind = case
     s = attention_inputs(lengths, heads, kv, d, kind, buckets, reach, padded, pad, ids, behind)
@@ -451,6 +456,19 @@ def test_one_bias_for_all(value):
     else:
         within(out, plain.double(), 20 * abs(value) * 8 * U * torch.ones_like(plain).double(), "shifted")         # (2 x max |v| x what a logit is off by)
     assert bool(lse.isfinite().all())
+
+
+@gpu
+@pytest.mark.parametrize("lengths", [[5], [40, 3, 77], [700, 300], [300] * 16])
+@pytest.mark.parametrize("bucket", [0, 2, -1, 3])
+def test_reach_of_zero(lengths, bucket):
+    """One bucket, or none, for all distances: its gradient is the sum over all places."""
+    s = attention_inputs(lengths, 16, 16, 32, "bf16", 3, 0)
+    s.distances = torch.tensor([bucket], dtype=torch.int32, device=dev())
+    out, lse = pqt.pqt_attention(s.q, s.k, s.v, s.starts, **arguments(s))
+    check_attention(s, out, lse)
+    grad = normal((s.n, 512), torch.bfloat16, 5)
+    check_gradient(s, grad, out, lse, pqt.pqt_attention_gradient(grad, s.q, s.k, s.v, out, lse, s.starts, **arguments(s)))
 
 
 @gpu
