@@ -59,7 +59,8 @@ int pqt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stri
     g.v_stride = v_stride;
     g.out_stride = out_stride;
     g.clear = clear;
-    const int rows = rows_of_a_workgroup(n, texts, heads);     // (the launch's limits were checked for the smallest workgroups)
+    // (the launch's limits were checked for the smallest workgroups)
+    const int rows = short_texts(n, texts) ? 16 : type == PQT_F32 && few_rows_of_floats(n, texts, d) ? 64 : rows_of_a_workgroup(n, texts, heads);
     with_type(type, [&](auto t) {
         launch_attention<decltype(t)>(g, rows, direct_rows(k, k_stride, sizeof(t), d) && direct_rows(v, v_stride, sizeof(t), d), st);
     });

@@ -302,6 +302,11 @@ __device__ __forceinline__ Rows rows_of_workgroup(const AttentionArgs& g, int64_
     }
 }
 
+// Where every second workgroup has no rows -- texts of exactly M, or of half of M -- the busy ones would all go to the same half of an XCD's shader engines,
+// which get workgroups in turn: of every sixteen, the second four are swapped in pairs, the third in halves, the fourth turned round.  (512 texts of 128 tokens,
+// 16 heads, 128 rows a workgroup: 232 us, 153 so; the gradient 894, 565.)  Longer texts, of whose workgroups two of three have rows, stay in order: a text of 8,191, 515 us so and 506.
+__device__ __forceinline__ int64_t out_of_step(const AttentionArgs& g, int64_t t) { return g.tiles <= 3 * g.texts && (t | 3) < g.tiles ? t ^ (t >> 2 & 3) : t; }
+
 // Workgroup -> (rows, head).  Consecutive workgroups go to the eight XCDs in turn: each XCD gets a run of one head's rows after another, so that its L2
 // holds the keys and values that they share.
 __device__ __forceinline__ void place_of_workgroup(const AttentionArgs& g, int heads, int64_t& t, int& head) {
@@ -309,7 +314,7 @@ __device__ __forceinline__ void place_of_workgroup(const AttentionArgs& g, int h
     const int x = blockIdx.x & 7, more = (int)(total & 7);
     const int64_t at = x * per + min(x, more) + (blockIdx.x >> 3);
     head = (int)(at / g.tiles);
-    t = at - (int64_t)head * g.tiles;
+    t = out_of_step(g, at - (int64_t)head * g.tiles);
 }
 
 // The same where a row's heads are cut into `parts`, side by side.
@@ -319,6 +324,7 @@ __device__ __forceinline__ void place_of_part(const AttentionArgs& g, int parts,
     const int64_t at = x * per + min(x, more) + (blockIdx.x >> 3);
     t = at / parts;
     part = (int)(at - t * parts);
+    t = out_of_step(g, t);
 }
 
 // Lanes of a wavefront meet: what one wrote to LDS another may read, in program order.
@@ -482,19 +488,27 @@ inline int attention_checks(const char* who, int type, int64_t n, int heads, int
     return PQT_OK;
 }
 
-inline bool short_texts(int64_t n, int64_t texts) { return texts > 0 && n / texts <= 64; }
-// Heads that a wavefront takes one after the other: 16,384 wavefronts are two rounds of what the card holds.
+// Texts whose keys a wavefront takes without a workgroup's help.  (65,000 tokens or so, 16 heads of 64 bf16 values, this kernel and 64 rows a workgroup of the other: texts of
+// 20 tokens 142 and 304 us, 36 203 and 215, 48 182 and 191, 64 191 and 167.)
+inline bool short_texts(int64_t n, int64_t texts) { return texts > 0 && n / texts <= 48; }
+// Heads that a wavefront takes one after the other: 16,384 wavefronts are two rounds of what the card holds.  (4,096 texts of 20 tokens, 16 heads: one head a
+// wavefront 264 us, two 213, four 191.)  All wavefronts of a row get as many, or one fewer.
 inline int heads_of_a_wavefront(int64_t tiles, int heads, int waves) {
-    return (int)std::max<int64_t>(1, std::min<int64_t>((heads + waves - 1) / waves, tiles * heads / 16384));
+    const int most = (int)std::max<int64_t>(1, std::min<int64_t>((heads + waves - 1) / waves, tiles * heads / 16384));
+    const int parts = (heads + waves * most - 1) / (waves * most);
+    return (heads + waves * parts - 1) / (waves * parts);
 }
 
-// Queries of a workgroup, by the texts' mean length and how many workgroups there are for 256 compute units.
-inline int rows_of_a_workgroup(int64_t n, int64_t texts, int heads) {
-    const int64_t mean = texts ? n / texts : 0;
-    if (short_texts(n, texts) || n / 64 * heads < 256) return 16;
-    return mean <= 128 || n / 128 * heads < 384 ? 64 : 128;
-}
+// Rows of a workgroup where texts are no short ones: wavefronts of two times 16 read a tile half as often, and 128 rows of a text of 64 or less would leave half of the workgroup
+// without any.  (16 heads of 64 bf16 values, 64 and 128 rows, the gradient in brackets: 1,024 texts of 64 tokens 167 and 187 us (635, 749), 800 of 80 206 and 186
+// (857, 775), 512 of 128 168 and 153 (662, 565).  Few workgroups: one text of 2,000 33 and 44 (112, 140), 2,500 49 and 53 (177, 184), 4,000 97 and 82 (367, 273).)
+inline int rows_of_a_workgroup(int64_t n, int64_t texts, int heads) { return (texts ? n / texts : n) <= 64 || n / 128 * heads < 384 ? 64 : 128; }
+// Texts of which the tiles far from a row are most: see walk().  (65,000 to 16,000 tokens, 16 heads of 64 bf16 values, without and with runs: 16 texts of 1,024 93.0 and 93.2 us (gradient 340,
+// 320), 10 of 1,600 146 and 144 (531, 498), four of 4,096 319 and 304 (1,095, 1,041).)
 inline bool long_texts(int64_t n, int64_t texts) { return texts > 0 && n / texts > 1024; }
+// fp32 keeps to 64 rows but for long texts and the widest heads: a second workgroup a compute unit is worth more there than half of the reading.  (Forward, 8 heads, 64 and 128 rows: 200 texts
+// of 200 tokens, heads of 64 values 278 and 374 us, 96 348 and 472, 128 609 and 595; four texts of 2,000, heads of 64 291 and 287.)
+inline bool few_rows_of_floats(int64_t n, int64_t texts, int d) { return d <= 96 && !long_texts(n, texts); }
 
 }  // namespace
 }  // namespace pqt

@@ -96,16 +96,29 @@ struct GradientPlan {
 // (reach: -1 where there is no dbias)
 inline GradientPlan gradient_plan(int64_t n, int64_t texts, int heads, int kv_heads, int d, int reach) {
     GradientPlan p{};
-    p.rows = rows_of_a_workgroup(n, texts, heads);
+    // 16 where texts are short (16 heads of 64 bf16 values, 16 and 64 rows: 3,000 texts of 20 tokens 1,191 and 1,302 us, 2,048 of 32 934 and 978, 1,800 of 36 1,213 and 910)
+    p.rows = texts && n / texts <= 32 ? 16 : rows_of_a_workgroup(n, texts, heads);
     p.tiles = n / p.rows + texts + 1;
-    // few workgroups have keys: up to four share the queries, of which each has four tiles at least
-    const int64_t busy = std::max<int64_t>(1, n / p.rows) * kv_heads, of_a_key = (texts ? n / texts : 0) * (heads / kv_heads) / (4 * 64);
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(4, of_a_key), 768 / busy));
+    int width = 0;
+    with_head(d, [&](auto dp) { width = dp.value; });
+    // Few workgroups have keys: up to eight share the queries, of which each has four tiles at least.  As many as make the time least, counted in rounds of what the
+    // card holds at once, four fifths of it: a round that is all but full leaves a shader engine with a workgroup too many, for which it waits.  (Heads of 64 bf16
+    // values, 16 of them: one text of 4,000, two of keys, shared by one 1,086 us, 4 427, 6 336, 8 392; two such 1,187, 3 632, 4 743, 6 624; one of 1,000, four of keys, 64 rows 130, 4 76, 8 70.
+    // Two texts of 3,150, 8 heads of 80 f16 values, two of keys: 4 395, 6 436, 8 403.)
+    const int key_rows = width > 96 ? std::min(p.rows, 64) : p.rows, at_once = key_rows <= 64 && width <= 64 ? 800 : 400;
+    const int64_t busy = std::max<int64_t>(1, n / key_rows) * kv_heads, most = std::min<int64_t>(std::min<int64_t>(8, (texts ? n / texts : 0) * (heads / kv_heads) / (4 * 64)), 800 / busy);
+    p.splits = 1;
+    int64_t rounds = (busy + at_once - 1) / at_once;
+    for (int s = 2; s <= most; ++s) {
+        const int64_t r = (busy * s + at_once - 1) / at_once;
+        if (r * p.splits < rounds * s) {
+            p.splits = s;
+            rounds = r;
+        }
+    }
     p.runs = p.tiles > 64 ? (int)std::min<int64_t>(64, p.tiles / 32) : 0;
     const int64_t columns = (int64_t)heads * (2 * reach + 1);
     const bool sums = reach >= 0;
-    int width = 0;
-    with_head(d, [&](auto dp) { width = dp.value; });
     p.parts = (heads * n + 3) / 4 * 4;
     p.key_parts = p.parts + (sums ? (p.tiles * columns + 3) / 4 * 4 : 0);
     p.joined = p.key_parts + (p.splits > 1 ? (int64_t)p.splits * kv_heads * n * 2 * width : 0);

