@@ -8,6 +8,9 @@ namespace {
 template <typename T, int DP, int NW, int RT, int BN, bool DIRECT, bool RUNS>
 __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 256 ? 2 : 1) void attention_query_gradient_kernel(AttentionArgs g) {
     constexpr int kThreads = NW * kWave, M = NW * RT * 16, KC = DP / 32, DT = DP / 16, kCopies = NW * 4;
+    // f16: ds in two parts.  A row's ds cancel in their sum, so that their rounding shows in dq half as much again as dq's own (2,301 and 4,001 tokens, 80 values:
+    // 3.1e-4 of dq's size off, its own rounding 2.1e-4).
+    constexpr bool kRest = std::is_same<T, Half>::value;
     typedef Tile<T, BN, DP> KeyTile;
     __shared__ __align__(16) typename KeyTile::S k_0[KeyTile::kSize], k_1[KeyTile::kSize], v_0[KeyTile::kSize], v_1[KeyTile::kSize];
     typedef typename KeyTile::Place Place;
@@ -128,7 +131,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
                         for (int rt = 0; rt < RT; ++rt) dp[rt][h] = multiply(f, grad[rt][x], dp[rt][h]);
                     }
                 }
-                Fragment<T> ds[RT];
+                Fragment<T> ds[RT], rest[kRest ? RT : 1];
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
@@ -158,12 +161,19 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
                     }
                     lift[rt].apply(s[rt][0], s[rt][1], sums[rt]);
                     ds[rt] = fragment_of<T>(s[rt][0], s[rt][1]);
+                    if constexpr (kRest) {
+                        const f32x8 kept = __builtin_convertvector(ds[rt], f32x8);
+                        rest[rt] = fragment_of<T>(s[rt][0] - __builtin_shufflevector(kept, kept, 0, 1, 2, 3), s[rt][1] - __builtin_shufflevector(kept, kept, 4, 5, 6, 7));
+                    }
                 }
 #pragma unroll
                 for (int b = 0; b < DT; ++b) {
                     const Fragment<T> f = kt.columns(c * 32, b);
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) sums[rt][b] = multiply(f, ds[rt], sums[rt][b]);
+                    for (int rt = 0; rt < RT; ++rt) {
+                        sums[rt][b] = multiply(f, ds[rt], sums[rt][b]);
+                        if constexpr (kRest) sums[rt][b] = multiply(f, rest[rt], sums[rt][b]);
+                    }
                 }
             }
             if (parts) {
@@ -274,6 +284,8 @@ void launch_attention_queries(const AttentionArgs& args, int rows, bool direct, 
         typedef std::integral_constant<bool, true> Yes;
         if (rows == 16) of(Width<1>{}, Width<1>{}, Width<32>{}, No{});
         else if (rows == 64) of(Width<4>{}, Width<1>{}, Width<kKeys>{}, No{});
+        // (f16's two parts of ds and runs together leave heads of 96 no registers: 65 spilled)
+        else if constexpr (std::is_same<T, Half>::value && DP == 96) of(Width<4>{}, Width<2>{}, Width<kKeys>{}, No{});
         else if (!long_texts(g.n, g.texts)) of(Width<4>{}, Width<2>{}, Width<kKeys>{}, No{});
         else of(Width<4>{}, Width<2>{}, Width<kKeys>{}, Yes{});
     });
