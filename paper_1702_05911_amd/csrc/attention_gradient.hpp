@@ -6,7 +6,7 @@
 // Two kernels, so that no sum is anybody else's to add to: one has queries and walks the keys (dq, delta, dbias), one has keys and walks the queries of
 // all heads that share them (dk, dv).  Each takes the weights anew, seven products instead of five, and the same inputs give the same bytes.
 // Bound by the vector unit beside the matrix unit (ds is eight operations a pair, f16's lift three more) at two workgroups a compute unit: 64 texts of up to 512 tokens, 16
-// heads of 64 bf16 values, 277 us (146 and 143), 0.35 PFLOP/s of the seven products; two texts of 4,001 and 2,301, 8 heads of 80 f16 values, two of keys, 430 us (217 and 237).
+// heads of 64 bf16 values, 280 us (146 and 143), 0.34 PFLOP/s of the seven products; two texts of 4,001 and 2,301, 8 heads of 80 f16 values, two of keys, 468 us (258 and 234).
 // As in the forward pass the products are turned so that a lane has one own row, whose weights and ds are the next product's operand where they are.
 //
 // dbias: a wavefront's ds of 16 queries by 16 keys are added up along their diagonals by moving lanes, so that a lane has one distance, and go to a sum by
