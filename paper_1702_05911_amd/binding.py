@@ -711,8 +711,10 @@ def pqt_rms_norm_gradient(grad, h, weight, rstd, through=None, out=None, stream=
 
 def pqt_distance_buckets(buckets, far, both=True, device=None):
     """pqt_distance_buckets.  Returns (2 * far + 1,) int32 on `device` (the CPU): the usual buckets of the distances -far .. far."""
-    distances = torch.empty(2 * far + 1, dtype=torch.int32) if far > 0 else None
-    _check(_lib.pqt_distance_buckets(buckets, far, 1 if both else 0, distances.data_ptr() if far > 0 else None))
+    # (the library refuses far less than these; its numbers have 32 bits)
+    buckets, far = max(-1, min(buckets, 1 << 20)), max(-1, min(far, 1 << 20))
+    distances = torch.empty(2 * max(far, 0) + 1, dtype=torch.int32)
+    _check(_lib.pqt_distance_buckets(buckets, far, 1 if both else 0, distances.data_ptr()))
     return distances if device is None else distances.to(device)
 
 

@@ -648,6 +648,12 @@ def test_distance_buckets(buckets, far, both):
     assert int(got.min()) == 0 and int(got.max()) < buckets
 
 
+@pytest.mark.parametrize("buckets,far", [(32, 2 ** 32 + 128), (2 ** 32 + 32, 128), (32, -1), (-2 ** 32 + 32, 128), (32, 0)])
+def test_refusals_of_distance_buckets_beyond_32_bits(buckets, far):
+    with pytest.raises(pqt.PqtError):
+        pqt.pqt_distance_buckets(buckets, far)
+
+
 def test_refusals_of_distance_buckets():
     for args in ((1, 10), (3, 10, True), (32, 0), (32, 449), (1026, 300), (64, 10), (0, 5), (-2, 5)):
         with pytest.raises(pqt.PqtError) as e:
