@@ -489,8 +489,8 @@ int pqt_rms_norm_gradient(const void* grad, int64_t grad_stride, const void* thr
 /*
  * pqt_attention -- attention among the tokens of every text.  Rows starts[s] .. starts[s + 1] - 1 of the n rows belong to text s of `texts`; starts:
  * device array of texts + 1 integers of place_bytes = 4 or 8, ascending.  lengths: as many integers of that size for each text, or NULL: only
- * a text's first lengths[s] rows hold tokens, the others pad it.  (Numbers out of range are taken as the nearest that is in range; results of texts that
- * overlap are not defined.)  A row of q has `heads` times d values, one of k and v `kv_heads` times d, which divides heads: heads / kv_heads
+ * a text's first lengths[s] rows hold tokens, the others pad it.  (Numbers out of range are taken as the nearest that is in range; where places do
+ * not ascend, results are not defined, and nothing outside of them is written.)  A row of q has `heads` times d values, one of k and v `kv_heads` times d, which divides heads: heads / kv_heads
  * consecutive heads share keys and values.  For every head and every token i, over the tokens j of its text:
  *     z_ij = scale * q_i . k_j + bias[head][distances[j - i]],   lse_i = log(sum over j of exp(z_ij)),   out_i = sum over j of exp(z_ij - lse_i) v_j.
  * bias: heads x buckets fp32, or NULL; distances: device array of 2 * reach + 1 integers (int32), the buckets of the distances -reach .. reach; farther

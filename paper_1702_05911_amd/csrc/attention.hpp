@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "encoder.hpp"
+#include "text_rows.hpp"
 
 namespace pqt {
 
@@ -253,53 +254,31 @@ __device__ __forceinline__ int64_t number(const void* p, int wide, int64_t i) {
     return wide ? static_cast<const int64_t*>(p)[i] : static_cast<const int32_t*>(p)[i];
 }
 
-// Rows begin .. begin + span of a text (of which `len` have tokens), and the first of those that a workgroup has.  Workgroup t of a head, of M rows each: text s
-// has those from floor(start / M) + s on, which leaves every text one for each M rows it begins, without a table of them.
-struct Rows {
-    int64_t begin;
-    int span, len, row0;
-    bool mine;                             // false: nothing to do
-    bool text;                             // false: rows of no text
-    int64_t before;                        // rows before the first text that this workgroup clears, too
-};
+// The lanes of a wavefront, of which each sees a text's start.
+struct Looking {
+    const AttentionArgs& g;
+    int probe, seen;
+    int64_t held;
 
+    __device__ __forceinline__ int in_range(int64_t start) const { return (int)min(max(start, (int64_t)0), g.n); }
+    __device__ __forceinline__ void look(int lo, int step) {
+        const int texts = (int)g.texts;
+        probe = lo + (int)(threadIdx.x & (kWave - 1)) * step;
+        const int s = min(probe, texts);
+        seen = in_range(number(g.starts, g.wide, s));
+        held = 0;                                              // (asked for beside the starts of the last look, not behind them)
+        if (step == 1 && g.lengths && texts) held = number(g.lengths, g.wide, min(s, texts - 1));
+    }
+    template <int M>
+    __device__ __forceinline__ int count(int hi, int64_t t) const { return (int)__popcll(__ballot(probe < hi && seen / M + probe <= t)); }
+    __device__ __forceinline__ int start(int lane) const { return __builtin_amdgcn_readlane(seen, lane); }
+    __device__ __forceinline__ int start_of(int text) const { return __builtin_amdgcn_readfirstlane(in_range(number(g.starts, g.wide, text))); }
+    __device__ __forceinline__ int tokens(int lane) const { return __builtin_amdgcn_readlane((int)min(max(held, (int64_t)0), (int64_t)0x7fffffff), lane); }
+};
 template <int M>
 __device__ __forceinline__ Rows rows_of_workgroup(const AttentionArgs& g, int64_t t) {
-    const int lane = threadIdx.x & (kWave - 1), texts = (int)g.texts;
-    // the last text with floor(start / M) + s <= t: 64 of them looked at at once.  (s = texts: the rows behind the last one.)
-    int lo = 0, hi = texts + 1;
-    Rows r{};
-    for (;;) {
-        const int step = (hi - lo + kWave - 1) / kWave, probe = lo + lane * step, s = min(probe, texts);
-        const int start = (int)min(max(number(g.starts, g.wide, s), (int64_t)0), g.n);
-        int64_t tokens = 0;                                    // (asked for beside the starts of the last look, not behind them)
-        if (step == 1 && g.lengths && texts) tokens = number(g.lengths, g.wide, min(s, texts - 1));
-        const int count = (int)__popcll(__ballot(probe < hi && start / M + probe <= t));
-        if (count == 0) {                                      // (at the first look only: later ones begin with a text that is) rows before the first text
-            r.begin = t * M;
-            r.span = M;
-            r.mine = g.clear != 0;
-            return r;
-        }
-        const int at = count - 1;
-        lo += at * step;
-        hi = min(hi, lo + step);
-        if (step > 1) continue;
-        const int begin = __builtin_amdgcn_readlane(start, at);
-        int end = (int)g.n;
-        r.text = lo < texts;
-        if (r.text) end = max(at + 1 < kWave ? __builtin_amdgcn_readlane(start, at + 1) : (int)min(max(number(g.starts, g.wide, lo + 1), (int64_t)0), g.n), begin);
-        end = __builtin_amdgcn_readfirstlane(end);
-        r.begin = begin;
-        r.span = end - begin;
-        r.len = r.text ? r.span : 0;
-        if (r.text && g.lengths) r.len = min(r.span, __builtin_amdgcn_readlane((int)min(max(tokens, (int64_t)0), (int64_t)0x7fffffff), at));
-        const int64_t row0 = (t - (begin / M + lo)) * M;
-        r.before = lo == 0 && row0 == 0 && g.clear ? begin % M : 0;
-        r.mine = r.before > 0 || (row0 < r.span && (r.text || g.clear));
-        r.row0 = (int)min(row0, (int64_t)r.span);
-        return r;
-    }
+    Looking looking{g, 0, 0, 0};
+    return rows_of_looks<M>(looking, g.n, (int)g.texts, g.lengths != nullptr, g.clear != 0, t);
 }
 
 // Where every second workgroup has no rows -- texts of exactly M, or of half of M -- the busy ones would all go to the same half of an XCD's shader engines,
