@@ -323,7 +323,7 @@ __device__ __forceinline__ void clear_rows(T* p, int64_t stride, int64_t from, i
 // ---- the bias by distance --------------------------------------------------------------------------------------------
 // Products are taken unscaled, with bias / scale as what they are added to, so that a logit is one multiplication by scale * log2 e away from its power
 // of two.  Finite entries are kept within 2^90, where that multiplication (scale up to 2^32) cannot overflow; -inf stays.
-constexpr float kBiasTop = 0x1p90f, kLowest = -0x1p92f;        // (kLowest: below every finite logit)
+constexpr float kBiasTop = 0x1p90f, kLowest = -0x1.fffffep127f;        // (kLowest: no finite logit is below)
 
 __device__ __forceinline__ float scaled_bias(float entry, float inverse_scale) {
     const float v = entry * inverse_scale;

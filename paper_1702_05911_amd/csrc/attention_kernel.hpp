@@ -14,9 +14,12 @@
 namespace pqt {
 namespace {
 
-// Weights are held as 2^(z - m + kShift), m the running maximum up to 2^kSlack: it follows the true one only when a logit passes it by that much, so that
-// most tiles rescale nothing.  f16 ones are lifted by 2^6: their least normal number is 2^-14, and small weights of long texts add up.
-constexpr float kSlack = 8.0f, kMostWeight = 0x1p14f;
+// Weights are held as 2^(z - m + Shift), m the running maximum.  It follows the true one only when logits pass it by far -- a lane's weights of a step add up to more than
+// kMostWeight, or a short text's logit passes it by kSlack --, so that most tiles rescale nothing.  f16 ones are lifted by 2^6: their least normal number is
+// 2^-14, and small weights of long texts add up.
+// z - m is one multiplication and addition where m is small.  From kLargePower on the rounding of m's own power of two shows (a bias of -1e9 is 64 away from the next
+// number), and the maximum is taken away before the multiplication.
+constexpr float kSlack = 8.0f, kMostWeight = 0x1p14f, kLargePower = 0x1p12f, kMostPower = 0x1.fffffep127f;
 template <typename T> struct Shift { static constexpr float value = 0.0f; };
 template <> struct Shift<Half> { static constexpr float value = 6.0f; };
 
@@ -115,15 +118,17 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
                 // needs no largest one -- and then, seldom, they are taken again.
                 Fragment<T> p[RT][kPart / 2];
                 float sum[RT];
-                auto weigh = [&]() __attribute__((always_inline)) {
+                auto weigh = [&](auto again) __attribute__((always_inline)) {
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
-                        const float off = Shift<T>::value - m[rt] * cs;
+                        // a maximum whose power is large: at first all but -inf weigh infinitely much, and so are taken again
+                        const bool large = !(fabsf(m[rt] * cs) < kLargePower);
+                        const float off = large ? again.value ? Shift<T>::value : kMostPower : Shift<T>::value - m[rt] * cs, from = again.value && large ? m[rt] : 0.0f;
                         f32x4 sums = f32x4{}, w[kPart];
 #pragma unroll
                         for (int h = 0; h < kPart; ++h) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) w[h][e] = exp2_of(__builtin_fmaf(s[rt][h][e], cs, off));
+                            for (int e = 0; e < 4; ++e) w[h][e] = exp2_of(__builtin_fmaf(again.value ? s[rt][h][e] - from : s[rt][h][e], cs, off));
                             sums = sums + w[h];
                         }
                         sum[rt] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
@@ -131,7 +136,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
                         for (int h = 0; h < kPart / 2; ++h) p[rt][h] = fragment_of<T>(w[2 * h], w[2 * h + 1]);
                     }
                 };
-                weigh();
+                weigh(std::false_type{});
                 bool rises = false;
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) rises |= !(sum[rt] <= kMostWeight);
@@ -147,7 +152,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
 #pragma unroll
                         for (int b = 0; b < DT; ++b) o[rt][b] = o[rt][b] * keep;
                     }
-                    weigh();
+                    weigh(std::true_type{});
                 }
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) l[rt] += sum[rt];
@@ -288,12 +293,11 @@ __global__ __launch_bounds__(4 * kWave) void attention_short_kernel(AttentionArg
 #pragma unroll
                 for (int b = 0; b < DT; ++b) o[b] = o[b] * keep;
             }
-            const float off = Shift<T>::value - m * cs;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[h][e] = exp2_of(__builtin_fmaf(s[h][e], cs, off));
+                    s[h][e] = exp2_of(__builtin_fmaf(s[h][e] - m, cs, Shift<T>::value));
                     l += s[h][e];
                 }
             const Fragment<T> p = fragment_of<T>(s[0], s[1]);

@@ -1,11 +1,13 @@
 """The query encoder's layers where calls are unusual: places that do not ascend, and what the tests beside these leave out.
 
 References and tolerances are those of test_query_encoder_layers.py."""
+import math
+
 import pytest
 import torch
 
 import test_query_encoder_layers as base
-from test_query_encoder_layers import INF, TYPES, dev, gpu, guarded, normal, pqt
+from test_query_encoder_layers import INF, LEAST, TYPES, U, UNIT, arguments, attention_inputs, dev, gpu, guarded, normal, pqt, within
 
 
 def ptr(t):
@@ -53,3 +55,84 @@ def test_places_in_any_order_stay_inside(kind, texts, n):
                                                *layout, ptr(parts[0]), step, ptr(parts[1]), step, ptr(parts[2]), step, ptr(dbias), ws.data_ptr() + 256, need, 0, stream))
     check()
     assert bool((ws[:256] == 7).all()) and bool((ws[256 + need:] == 7).all())
+
+
+# ---- large finite biases ---------------------------------------------------------------------------------------------
+FAR = [-1e6, -1e8, -1e9, -1e10, -1e12, 1e12, 1e30, torch.finfo(torch.float32).min]
+TEXTS = [[20, 1, 0, 33], [70, 3, 1, 60], [300] * 16, [2100, 2050]]     # short texts, workgroups of 64 and of 128 rows, far steps in runs
+
+
+def counted(s, value):
+    """What a bias counts as: finite bias / scale within 2^90."""
+    return max(-2.0 ** 90, min(value / s.scale, 2.0 ** 90)) * s.scale
+
+
+def between(s, out, lse, value, uniform):
+    """Whatever the rounding of logits beside such a bias leaves of their differences, results are means of v: weights that are not negative and add up to one."""
+    unit = base.weight_unit(s.q.dtype) * 1.01
+    for at, m in zip(s.at, s.of):
+        if not m:
+            continue
+        v = s.v[at:at + m].double()
+        off = (m + 16) * U * v.abs().amax(0) + unit * v.abs().amax(0)
+        off = off + v.abs().amax(0) * UNIT[s.q.dtype] * 1.01 + LEAST[s.q.dtype]
+        got = out[at:at + m].double()
+        assert bool((got <= v.amax(0) + off).all() and (got >= v.amin(0) - off).all())
+        if uniform:
+            want = v.mean(0, keepdim=True).expand(m, -1)
+            within(out[at:at + m], want, ((m + 16) * U + unit) * v.abs().mean(0, keepdim=True).expand(m, -1), "mean")
+        z = torch.stack([s.q[at:at + m, h * s.d:(h + 1) * s.d].double() @ s.k[at:at + m, h * s.d:(h + 1) * s.d].double().t() for h in range(s.heads)]).abs().amax() * s.scale
+        want = counted(s, value)
+        assert bool(((lse[:, at:at + m].double() - want).abs() <= float(z) + math.log(m) + abs(want) * 16 * U).all())
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("d", [32, 64, 80])
+@pytest.mark.parametrize("lengths", TEXTS, ids=lambda t: f"{len(t)}x{max(t)}")
+def test_one_far_bias_for_all(kind, d, lengths):
+    """A bias beside which logits are rounded, the same for all places.  From 1e9 on (bias / scale above 2^32, whose numbers are 512 apart) products below 2^8 vanish: equal weights."""
+    s = attention_inputs(lengths, 8, 8, d, kind, 0, 0)
+    s.bias, s.distances, s.reach = torch.zeros((8, 1), device=dev()), torch.zeros(1, dtype=torch.int32, device=dev()), 0
+    size = lambda t: float(t.double().unflatten(1, (8, d)).square().sum(2).amax().sqrt())               # noqa: E731
+    assert size(s.q) * size(s.k) < 2 ** 8
+    for value in FAR:
+        s.bias.fill_(value)
+        out, lse = pqt.pqt_attention(s.q, s.k, s.v, s.starts, **arguments(s))
+        between(s, out, lse, value, abs(value) >= 1e9)
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("d", [32, 64, 80])
+@pytest.mark.parametrize("lengths", TEXTS, ids=lambda t: f"{len(t)}x{max(t)}")
+def test_one_key_left_with_a_far_bias(kind, d, lengths):
+    """All places masked but the query's own, whose bias is far: its value is the result.  And all but those behind: the last token has none, the one before it the last."""
+    s = attention_inputs(lengths, 8, 8, d, kind, 2, 1)
+    for value in FAR + [-1e4, 5.0]:
+        s.bias = torch.tensor([[value, -INF]] * 8, device=dev())
+        s.distances = torch.tensor([1, 0, 1], dtype=torch.int32, device=dev())
+        out, lse = pqt.pqt_attention(s.q, s.k, s.v, s.starts, **arguments(s))
+        want = s.v.double()
+        within(out, want, want.abs() * 8 * U, "own value")
+        assert bool(lse.isfinite().all())
+        s.distances = torch.tensor([1, 1, 0], dtype=torch.int32, device=dev())
+        out, lse = pqt.pqt_attention(s.q, s.k, s.v, s.starts, **arguments(s))
+        for at, m in zip(s.at, s.of):
+            if m:
+                assert bool((lse[:, at + m - 1] == -INF).all()) and not bool(out[at + m - 1].any())
+            if m > 1:
+                last = s.v[at + m - 1:at + m].double()
+                within(out[at + m - 2:at + m - 1], last, last.abs() * 8 * U, "last value")
+                assert bool(out[at:at + m].isfinite().all()) and bool(lse[:, at:at + m - 1].isfinite().all())
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_products_far_below_zero(kind):
+    """A single token whose logit is -1e30 or so has all of the weight, as one of any size has."""
+    x = torch.full((3, 64), 1e14, dtype=TYPES[kind], device=dev())
+    v = normal((3, 64), TYPES[kind], 1)
+    starts = torch.arange(4, device=dev())
+    out, lse = pqt.pqt_attention(x, -x, v, starts, 1)
+    assert torch.equal(out, v) and bool((lse < -1e28).all())
