@@ -503,6 +503,7 @@ int pqt_rms_norm_gradient(const void* grad, int64_t grad_stride, const void* thr
  * pqt_attention_gradient -- the gradients of q, k, v (n rows each, as those) and of bias (heads x buckets fp32, may be NULL) from that of out; out and
  * lse as pqt_attention wrote them.  With p_ij = exp(z_ij - lse_i) and ds_ij = p_ij (grad_i . v_j - grad_i . out_i):
  *     dq_i = scale * sum of ds_ij k_j,  dk_j = scale * sum of ds_ij q_i,  dv_j = sum of p_ij grad_i,  dbias[head][b] = sum of ds_ij over b's distances;
+ * (rows whose |lse| passes 2839, where fp32 no longer tells p, get it from q, k and bias once more);
  * dk and dv are sums over the heads that share them too.  Rows that pad a text get zeros, rows of no text are left or cleared as above.  The workspace is
  * asked for with reach = -1 where there is no dbias.
  *

@@ -31,6 +31,7 @@ struct AttentionArgs {
     void* dk;
     void* dv;
     float* delta;                          // heads x n
+    float2* large_sums;                    // heads x n: of rows with a large sum (large_sum()), maximum and logarithm of the sum beside it
     float* parts;                          // workgroups x distances -reach .. reach
     float* key_parts;                      // splits x heads of keys x n x (dk, dv), where the queries of a key are shared out
     int64_t q_stride, k_stride, v_stride, grad_stride, out_stride, dq_stride, dk_stride, dv_stride;
@@ -365,6 +366,10 @@ struct BiasTable {
 };
 __device__ __forceinline__ f32x4 four_of(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 
+// From this power of two on -- of a row's maximum, or of the sum that lse is the logarithm of -- a multiplication's rounding shows in the weights taken from it: 2^12 is
+// up to 2^-12 off, a part in 6,000 of a weight, and a bias of -1e9 is 64 away from the next number.  Weights are taken from differences there.
+constexpr float kLargePower = 0x1p12f;
+
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
 
 // the largest, and the sum, over the four groups of sixteen lanes
@@ -378,8 +383,8 @@ __device__ __forceinline__ float sum_of_groups(float v) {
 }
 
 // Kinds of steps along a text, a body each: all places farther than `reach` on one side (or no bias), some nearer, either of them, and the last, whose rows behind
-// the text's end are left out.
-enum : int { kFar, kNear, kEither, kLast };
+// the text's end are left out.  (The gradient's second walk, for rows with a large sum, has one body for all.)
+enum : int { kFar, kNear, kEither, kLast, kLarge };
 template <int K> using Kind = std::integral_constant<int, K>;
 
 // Steps of BN rows along a text of `len`, by a wavefront with 16 RT rows from row0 on, in turn by one of two tiles: f(kind, odd, step).  Every wavefront of a

@@ -91,7 +91,7 @@ struct GradientPlan {
     int rows;                              // of a workgroup
     int splits;                            // workgroups that share out a key's queries
     int runs;                              // of the bias' parts that are joined side by side; 0: few parts, none are
-    int64_t tiles, parts, key_parts, joined, all;
+    int64_t tiles, large_sums, parts, key_parts, joined, all;
 };
 // (reach: -1 where there is no dbias)
 inline GradientPlan gradient_plan(int64_t n, int64_t texts, int heads, int kv_heads, int d, int reach) {
@@ -119,7 +119,8 @@ inline GradientPlan gradient_plan(int64_t n, int64_t texts, int heads, int kv_he
     p.runs = p.tiles > 64 ? (int)std::min<int64_t>(64, p.tiles / 32) : 0;
     const int64_t columns = (int64_t)heads * (2 * reach + 1);
     const bool sums = reach >= 0;
-    p.parts = (heads * n + 3) / 4 * 4;
+    p.large_sums = (heads * n + 3) / 4 * 4;
+    p.parts = p.large_sums + (2 * heads * n + 3) / 4 * 4;
     p.key_parts = p.parts + (sums ? (p.tiles * columns + 3) / 4 * 4 : 0);
     p.joined = p.key_parts + (p.splits > 1 ? (int64_t)p.splits * kv_heads * n * 2 * width : 0);
     p.all = p.joined + (sums ? p.runs * columns : 0);
@@ -175,6 +176,7 @@ int pqt_attention_gradient(const void* grad, int64_t grad_stride, const void* q,
         g.dk = dk;
         g.dv = dv;
         g.delta = at;
+        g.large_sums = reinterpret_cast<float2*>(at + plan.large_sums);
         g.parts = dbias ? at + plan.parts : nullptr;
         g.key_parts = at + plan.key_parts;
         g.grad_stride = grad_stride;

@@ -69,12 +69,31 @@ __host__ __device__ constexpr int sums_pitch(int W) { return (2 * W + 4) / 4 * 4
 // Adds to a number in LDS that nobody else adds to meanwhile.  (LDS' own addition of floats is slow: 64 texts of up to 512 tokens 311 us, 179 so.)
 __device__ __forceinline__ void add_to(float* p, float v) { *p += v; }
 
-// the logarithm of the sum as a power of two's; rows without weights have none
-__device__ __forceinline__ float power_of(float lse) { return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e; }
-// what weights are to be multiplied by for that power's rounding, the same for all of a row: 1 - rest * ln 2 (the rest is below 2^-13 even of sums of e^1000)
+// A row whose lse is so large that weights cannot be taken from it: with a bias of -1e9 on all that the row has left, the next lse is 64 away.  Such rows have no weights in
+// the steps that all rows take.  Where a workgroup meets one, seldom, it walks its text a second time: the queries' kernel takes the row's maximum and sum anew, and both
+// take the weights from these.  (This costs others nothing that shows; a question at each of the usual steps instead 2 % on average, up to 10; steps of either kind by
+// workgroup 3 %, up to 17, for registers.)
+__device__ __forceinline__ bool large_sum(float lse) { return fabsf(lse * kLog2e) >= kLargePower && fabsf(lse) < __builtin_inff(); }
+// (Its lanes' places are counted anew, behind a number that the compiler does not see through: shared with the first walk's they would be held in registers all the while.)
+struct LaneOf {
+    int lane, col, quad;
+    __device__ __forceinline__ explicit LaneOf(int l) : lane(l), col(l & 15), quad(l >> 4) {}
+    static __device__ __forceinline__ LaneOf anew() {
+        int l = threadIdx.x & (kWave - 1);
+        asm volatile("" : "+v"(l));
+        return LaneOf(l);
+    }
+};
+// (such rows' maxima lie in the room of the second tile then, which that walk has no use for)
+typedef float TileFloat __attribute__((may_alias));
+typedef f32x4 TileFloats __attribute__((may_alias));
+
+// the logarithm of the sum as a power of two's; rows without weights, and those with a large sum, have none
+__device__ __forceinline__ float power_of(float lse) { return fabsf(lse * kLog2e) >= kLargePower ? __builtin_inff() : lse * kLog2e; }
+// what weights are to be multiplied by for that power's rounding, the same for all of a row: 1 - rest * ln 2 (the rest is below 2^-12)
 __device__ __forceinline__ float rest_of_power(float lse) {
     const float rest = __builtin_fmaf(lse, kLog2e, -(lse * kLog2e)) + lse * kLog2eRest;
-    return fabsf(lse) < __builtin_inff() ? __builtin_fmaf(rest, -kLn2, 1.0f) : 1.0f;
+    return fabsf(lse * kLog2e) < kLargePower ? __builtin_fmaf(rest, -kLn2, 1.0f) : 1.0f;
 }
 
 // Places of the bias table, and of the sums by distance, on either side: those of the tiles that are near, and sixteen for what is carried past one.

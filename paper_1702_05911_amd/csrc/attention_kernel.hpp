@@ -17,9 +17,8 @@ namespace {
 // Weights are held as 2^(z - m + Shift), m the running maximum.  It follows the true one only when logits pass it by far -- a lane's weights of a step add up to more than
 // kMostWeight, or a short text's logit passes it by kSlack --, so that most tiles rescale nothing.  f16 ones are lifted by 2^6: their least normal number is
 // 2^-14, and small weights of long texts add up.
-// z - m is one multiplication and addition where m is small.  From kLargePower on the rounding of m's own power of two shows (a bias of -1e9 is 64 away from the next
-// number), and the maximum is taken away before the multiplication.
-constexpr float kSlack = 8.0f, kMostWeight = 0x1p14f, kLargePower = 0x1p12f, kMostPower = 0x1.fffffep127f;
+// z - m is one multiplication and addition where m is small; from kLargePower on the maximum is taken away before the multiplication.
+constexpr float kSlack = 8.0f, kMostWeight = 0x1p14f, kMostPower = 0x1.fffffep127f;
 template <typename T> struct Shift { static constexpr float value = 0.0f; };
 template <> struct Shift<Half> { static constexpr float value = 6.0f; };
 

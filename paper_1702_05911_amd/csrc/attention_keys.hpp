@@ -5,14 +5,16 @@
 namespace pqt {
 namespace {
 
+// (four wavefronts a SIMD where 128 registers are enough, three where 168 are)
 template <typename T, int DP, int NW, int RT, int BN, bool DIRECT>
-__global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void attention_key_gradient_kernel(AttentionArgs g) {
+__global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? (RT * DP > 64 || (RT == 2 && !DIRECT) ? 2 : RT * DP == 32 ? 4 : 3) : 1) void attention_key_gradient_kernel(AttentionArgs g) {
     constexpr int kThreads = NW * kWave, M = NW * RT * 16, KC = DP / 32, DT = DP / 16;
     typedef Tile<T, BN, DP> QueryTile;
     __shared__ __align__(16) typename QueryTile::S q_0[QueryTile::kSize], q_1[QueryTile::kSize], g_0[QueryTile::kSize], g_1[QueryTile::kSize];
     typedef typename QueryTile::Place Place;
     const QueryTile q_even{(Place)q_0, (int)threadIdx.x & (kWave - 1)}, q_odd{(Place)q_1, (int)threadIdx.x & (kWave - 1)}, g_even{(Place)g_0, (int)threadIdx.x & (kWave - 1)}, g_odd{(Place)g_1, (int)threadIdx.x & (kWave - 1)};
     __shared__ __align__(16) float powers[2][BN], deltas[2][BN];
+    __shared__ int large_rows;
     extern __shared__ __align__(16) float room[];
     const int W = most_places<RT, BN>(g.reach);
     const BiasTable table{room, BiasTable::pitch_of(W)};
@@ -59,7 +61,8 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
                 v[rt][c] = rows_of_memory(static_cast<const T*>(g.v) + r.begin * g.v_stride + (int64_t)kv * d, g.v_stride, row0 + rt * 16, len, d, c, lane);
             }
         Loader<T, BN, DP, kThreads, DIRECT> next_q(g.q_stride, d), next_g(g.grad_stride, d);
-        float next_power = 0.0f, next_delta = 0.0f;
+        if (threadIdx.x == 0) large_rows = 0;                  // (set by lanes of the same wavefront)
+        float next_sum = 0.0f, next_delta = 0.0f;
         auto fetch = [&](int at, QueryTile qt, QueryTile gt) __attribute__((always_inline)) {
             const int head = kv * g.group + at / steps, i0 = at % steps * BN;
             next_q.begin(qt, static_cast<const T*>(g.q) + r.begin * g.q_stride + (int64_t)head * d, g.q_stride, i0, len, d);
@@ -67,7 +70,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
             if (threadIdx.x < BN) {
                 const int i = i0 + (int)threadIdx.x;
                 const int64_t place = (int64_t)head * g.n + r.begin + min(i, len - 1);
-                next_power = i < len ? power_of(g.lse_in[place]) : __builtin_inff();
+                next_sum = i < len ? g.lse_in[place] : -__builtin_inff();
                 next_delta = i < len ? g.delta[place] : 0.0f;
             }
         };
@@ -75,22 +78,23 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
             next_q.finish(qt);
             next_g.finish(gt);
             if (threadIdx.x < BN) {
-                powers[half][threadIdx.x] = next_power;
+                powers[half][threadIdx.x] = power_of(next_sum);
                 deltas[half][threadIdx.x] = next_delta;
+                if (large_sum(next_sum)) large_rows = 1;
             }
         };
-        auto step = [&](int at, int half, QueryTile qt, QueryTile gt, QueryTile q_next, QueryTile g_next) __attribute__((always_inline)) {
+        auto step = [&](auto large, LaneOf of, int at, int half, QueryTile qt, QueryTile gt, QueryTile q_next, QueryTile g_next) __attribute__((always_inline)) {
             const int i0 = at % steps * BN;
             if (g.bias && i0 == 0 && at > from) {              // another head's (the last barrier stands after the last reading of the one before)
                 table.fill<kThreads>(g, kv * g.group + at / steps, W, min(W, len + M + BN), bucket);
                 __syncthreads();
             }
-            const bool more = at + 1 < to;
+            const bool more = !large.value && at + 1 < to;
             if (more) fetch(at + 1, q_next, g_next);
             const int low = row0 - (i0 + BN - 1), high = row0 + RT * 16 - 1 - i0;      // distances key - query
             const bool near = g.bias && high > -g.reach && low < g.reach;
             const float far = g.bias ? table.v[low >= g.reach ? 0 : 2 * W] : 0.0f;
-            const float* bias_at = table.from(i0 + quad * 4 - row0 - col + W);
+            const float* bias_at = table.from(i0 + of.quad * 4 - row0 - of.col + W);
 #pragma unroll
             for (int c = 0; c < BN / 32; ++c) {
                 f32x4 s[RT][2], dp[RT][2];
@@ -114,8 +118,13 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
 #pragma unroll
                         for (int rt = 0; rt < RT; ++rt) dp[rt][x] = multiply(f, v[rt][y], dp[rt][x]);
                     }
-                    const f32x4 power = *reinterpret_cast<const f32x4*>(&powers[half][i + quad * 4]);
-                    const f32x4 delta = *reinterpret_cast<const f32x4*>(&deltas[half][i + quad * 4]);
+                    if constexpr (large.value) {
+                        const f32x4 top = *reinterpret_cast<const TileFloats*>(reinterpret_cast<TileFloat*>(q_1) + i + of.quad * 4);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) s[rt][x] = s[rt][x] - top;
+                    }
+                    const f32x4 power = *reinterpret_cast<const f32x4*>(&powers[half][i + of.quad * 4]);
+                    const f32x4 delta = *reinterpret_cast<const f32x4*>(&deltas[half][i + of.quad * 4]);
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -149,8 +158,27 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 ? 2 : 1) void 
         arrive(0, q_even, g_even);
         __syncthreads();
         for (int at = from; at < to; at += 2) {
-            step(at, 0, q_even, g_even, q_odd, g_odd);
-            if (at + 1 < to) step(at + 1, 1, q_odd, g_odd, q_even, g_even);
+            step(std::false_type{}, LaneOf(lane), at, 0, q_even, g_even, q_odd, g_odd);
+            if (at + 1 < to) step(std::false_type{}, LaneOf(lane), at + 1, 1, q_odd, g_odd, q_even, g_even);
+        }
+        if (__builtin_amdgcn_readfirstlane(large_rows)) {      // the second walk: see large_sum()
+            const LaneOf of = LaneOf::anew();
+            const QueryTile qt{(Place)q_0, of.lane}, gt{(Place)g_0, of.lane};
+            if (g.bias) table.fill<kThreads>(g, kv * g.group + from / steps, W, min(W, len + M + BN), bucket);
+#pragma nounroll
+            for (int at = from; at < to; ++at) {
+                fetch(at, qt, gt);
+                arrive(0, qt, gt);
+                if (threadIdx.x < BN) {
+                    const bool has = large_sum(next_sum);      // (of a row that there is)
+                    float2 sum = float2{0.0f, __builtin_inff()};
+                    if (has) sum = g.large_sums[(int64_t)(kv * g.group + at / steps) * g.n + r.begin + at % steps * BN + (int)threadIdx.x];
+                    reinterpret_cast<TileFloat*>(q_1)[threadIdx.x] = sum.x;
+                    powers[0][threadIdx.x] = sum.y;
+                }
+                __syncthreads();
+                step(std::true_type{}, of, at, 0, qt, gt, qt, gt);
+            }
         }
     }
 #pragma unroll

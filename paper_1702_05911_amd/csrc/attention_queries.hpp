@@ -5,8 +5,9 @@
 namespace pqt {
 namespace {
 
+// (three wavefronts a SIMD where 168 registers are enough)
 template <typename T, int DP, int NW, int RT, int BN, bool DIRECT, bool RUNS>
-__global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 256 ? 2 : 1) void attention_query_gradient_kernel(AttentionArgs g) {
+__global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 256 ? (RT == 1 && DP <= (DIRECT ? 96 : 64) ? 3 : 2) : 1) void attention_query_gradient_kernel(AttentionArgs g) {
     constexpr int kThreads = NW * kWave, M = NW * RT * 16, KC = DP / 32, DT = DP / 16, kCopies = NW * 4;
     // f16: ds in two parts.  A row's ds cancel in their sum, so that their rounding shows in dq half as much again as dq's own (2,301 and 4,001 tokens, 80 values:
     // 3.1e-4 of dq's size off, its own rounding 2.1e-4; the kernel 217 us, so 258).  For bf16, and in dk, it shows less: 1.4 times.
@@ -16,6 +17,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
     typedef typename KeyTile::Place Place;
     const KeyTile k_even{(Place)k_0, (int)threadIdx.x & (kWave - 1)}, k_odd{(Place)k_1, (int)threadIdx.x & (kWave - 1)}, v_even{(Place)v_0, (int)threadIdx.x & (kWave - 1)}, v_odd{(Place)v_1, (int)threadIdx.x & (kWave - 1)};
     __shared__ double far_sums[2][NW];
+    __shared__ int large_rows[NW];
     extern __shared__ __align__(16) float room[];              // the bias by distance, and kCopies x (2 W + 1) sums
     const int W = most_places<RT, BN>(g.reach), width = sums_pitch(W);
     const BiasTable table{room, BiasTable::pitch_of(W)};
@@ -60,6 +62,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
                 for (int i = threadIdx.x; i < pieces; i += kThreads) *reinterpret_cast<f32x4*>(&by_distance[x * width + first + 4 * i]) = f32x4{};
         Fragment<T> q[RT][KC], grad[RT][KC];
         float delta[RT], power[RT], factor[RT], sum[RT];
+        bool large = false;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             const int row = row0 + rt * 16 + col;
@@ -86,17 +89,21 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
             power[rt] = power_of(sum[rt]);
             factor[rt] = rest_of_power(sum[rt]);
             delta[rt] *= factor[rt];
+            large |= large_sum(sum[rt]);
         }
+        large = __any(large);
+        if (lane == 0) large_rows[wave] = large;
         if (g.bias) table.fill<kThreads>(g, head, W, S, bucket);
         double far_left = 0.0, far_right = 0.0;
         next_k.finish(k_even);
         next_v.finish(v_even);
         __syncthreads();
         const float before = g.bias ? table.v[0] : 0.0f, behind = g.bias ? table.v[2 * W] : 0.0f;
-        float* const mine = by_distance + (wave * 4 + quad) * width + W;
-        auto step = [&](auto kind, int j0, KeyTile kt, KeyTile vt, KeyTile k_next, KeyTile v_next) __attribute__((always_inline)) {
+        auto step = [&](auto kind, LaneOf of, int j0, KeyTile kt, KeyTile vt, KeyTile k_next, KeyTile v_next) __attribute__((always_inline)) {
             constexpr int kKind = decltype(kind)::value;
-            if constexpr (kKind != kLast) {
+            const int lane = of.lane, col = of.col, quad = of.quad;
+            float* const mine = by_distance + (wave * 4 + quad) * width + W;
+            if constexpr (kKind < kLast) {
                 next_k.begin(k_next, k, g.k_stride, j0 + BN, len, d);
                 next_v.begin(v_next, v, g.v_stride, j0 + BN, len, d);
             }
@@ -136,10 +143,11 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
                 for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
+                        if constexpr (kKind == kLarge) s[rt][h] = s[rt][h] - reinterpret_cast<TileFloat*>(k_1)[(wave * RT + rt) * 16 + col];
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             s[rt][h][e] = exp2_of(__builtin_fmaf(s[rt][h][e], cs, -power[rt])) * __builtin_fmaf(dp[rt][h][e], factor[rt], -delta[rt]);
-                        if constexpr (kKind == kLast) {        // places behind the text's last token
+                        if constexpr (kKind >= kLast) {        // places behind the text's last token
 #pragma unroll
                             for (int e = 0; e < 4; ++e) s[rt][h][e] = j0 + c * 32 + h * 16 + quad * 4 + e < len ? s[rt][h][e] : 0.0f;
                         }
@@ -183,7 +191,7 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
                 } else if (low >= g.reach) far_right += far_sum;
                 else far_left += far_sum;
             }
-            if constexpr (kKind != kLast) {
+            if constexpr (kKind < kLast) {
                 if constexpr (sizeof(T) == 2) {
                     if (parts) {
 #pragma unroll
@@ -200,9 +208,69 @@ __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 2
             __syncthreads();
         };
         walk<RT, BN, RUNS>(g, row0, len, [&](auto kind, auto odd, int i) __attribute__((always_inline)) {
-            if constexpr (odd.value) step(kind, i * BN, k_odd, v_odd, k_even, v_even);
-            else step(kind, i * BN, k_even, v_even, k_odd, v_odd);
+            if constexpr (odd.value) step(kind, LaneOf(lane), i * BN, k_odd, v_odd, k_even, v_even);
+            else step(kind, LaneOf(lane), i * BN, k_even, v_even, k_odd, v_odd);
         });
+        large = false;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) large |= large_rows[w] != 0;
+        if (__builtin_amdgcn_readfirstlane(large)) {           // the second walk: see large_sum()
+            const LaneOf of = LaneOf::anew();
+            const int lane = of.lane, col = of.col, quad = of.quad;
+            const KeyTile kt{(Place)k_0, lane}, vt{(Place)v_0, lane};
+            // maxima and sums, by products that start as the steps' do
+            float most[RT], total[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                most[rt] = kLowest;
+                total[rt] = 0.0f;
+            }
+#pragma nounroll
+            for (int j0 = 0; j0 < len; j0 += 16) {
+                const int tile = j0 - j0 % BN, low = tile - (row0 + RT * 16 - 1), high = tile + BN - 1 - row0;
+                const bool near = g.bias && high > -g.reach && low < g.reach;
+                const float far = low >= g.reach ? behind : before;
+                const float* at = table.from(j0 + quad * 4 - row0 - col + W);
+                f32x4 s[RT];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) s[rt] = near ? four_of(at - rt * 16) : f32x4{far, far, far, far};
+#pragma unroll
+                for (int x = 0; x < KC; ++x) {
+                    const Fragment<T> f = rows_of_memory(k, g.k_stride, j0, len, d, x, lane);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) s[rt] = multiply(f, q[rt][x], s[rt]);
+                }
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[rt][e] = j0 + quad * 4 + e < len ? s[rt][e] : -__builtin_inff();
+                    const float now = fmaxf(fmaxf(fmaxf(most[rt], s[rt][0]), fmaxf(s[rt][1], s[rt][2])), s[rt][3]);
+                    total[rt] *= exp2_of((most[rt] - now) * cs);
+                    most[rt] = now;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) total[rt] += exp2_of((s[rt][e] - now) * cs);
+                }
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const int row = row0 + rt * 16 + col;
+                const int64_t place = (int64_t)head * g.n + r.begin + row;
+                const bool has = row < len && large_sum(g.lse_in[place]);
+                const float top = max_of_groups(most[rt]);
+                power[rt] = has ? __builtin_amdgcn_logf(sum_of_groups(total[rt] * exp2_of((most[rt] - top) * cs))) : __builtin_inff();
+                reinterpret_cast<TileFloat*>(k_1)[(wave * RT + rt) * 16 + col] = has ? top : 0.0f;
+                if (has && quad == 0) g.large_sums[place] = float2{top, power[rt]};
+            }
+#pragma nounroll
+            for (int j0 = 0; j0 < len; j0 += BN) {
+                next_k.begin(kt, k, g.k_stride, j0, len, d);
+                next_v.begin(vt, v, g.v_stride, j0, len, d);
+                next_k.finish(kt);
+                next_v.finish(vt);
+                __syncthreads();
+                step(Kind<kLarge>{}, of, j0, kt, vt, kt, vt);
+            }
+        }
         if (parts) {
 #pragma unroll
             for (int off = 1; off < kWave; off *= 2) {

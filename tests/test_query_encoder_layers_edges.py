@@ -136,3 +136,104 @@ def test_products_far_below_zero(kind):
     starts = torch.arange(4, device=dev())
     out, lse = pqt.pqt_attention(x, -x, v, starts, 1)
     assert torch.equal(out, v) and bool((lse < -1e28).all())
+
+
+def mean_gradient(s, grad, out, got, share):
+    """Against the formula with the weights share(text's tokens) given, as large biases leave them: one weight of its row's is exact to 8 U."""
+    dq, dk, dv, dbias = got
+    unit, small = base.weight_unit(s.q.dtype) * 1.01, 2.0 ** -32 if s.q.dtype == torch.float16 else 0.0
+    scale = torch.tensor(s.scale, dtype=torch.float32).double().item()
+    names = ("dq", "dk", "dv")
+    want, tol = [[torch.zeros(s.n, s.heads * s.d, dtype=torch.float64, device=dev()) for _ in names] for _ in range(2)]
+    want_b, tol_b = [torch.zeros(s.heads, s.bias.shape[1], dtype=torch.float64, device=dev()) for _ in range(2)]
+    for at, m in zip(s.at, s.of):
+        if not m:
+            continue
+        p, bucket = share(m)
+        for h in range(s.heads):
+            rows, columns = slice(at, at + m), slice(h * s.d, (h + 1) * s.d)
+            q, k, v, g, o = (t[rows, columns].double() for t in (s.q, s.k, s.v, grad, out))
+            ds = p * (g @ v.t() - (g * o).sum(1, keepdim=True))
+            off = ds.abs() * (m + 12) * U + p * 1.01 * (s.d + 6) * U * (g.abs() @ v.abs().t() + (g.abs() * o.abs()).sum(1, keepdim=True)) + 2.0 ** -120
+            row = off + ds.abs() * unit + small * ds.abs().amax(1, keepdim=True)
+            key = off + ds.abs() * unit + small * ds.abs().amax(0, keepdim=True)
+            add = (m + 8) * U
+            for i, (w, e) in enumerate(((scale * ds @ k, scale * (row + ds.abs() * add) @ k.abs()), (scale * ds.t() @ q, scale * (key + ds.abs() * add).t() @ q.abs()),
+                                        (p.t() @ g, (p * ((m + 12) * U + unit + add) + small + 2.0 ** -120).t() @ g.abs()))):
+                want[i][rows, columns], tol[i][rows, columns] = w, e
+            for b in range(s.bias.shape[1]):
+                want_b[h, b] += ds[bucket == b].sum()
+                tol_b[h, b] += (off + ds.abs() * (m + 2 * s.reach + 64 + len(s.of)) * U)[bucket == b].sum()
+    for name, a, w, e in zip(names, got, want, tol):
+        within(a, w, e, name)
+    within(dbias, want_b, tol_b, "dbias")
+
+
+def rows_add_up(s, grad, got):
+    """Every row's weights add up to one, whatever they are: dv's sum over the keys is grad's over the queries, and dbias' over all buckets nothing."""
+    unit = base.weight_unit(s.q.dtype) * 1.01
+    for at, m in zip(s.at, s.of):
+        if not m:
+            continue
+        g, dv = grad[at:at + m].double(), got[2][at:at + m].double()
+        off = g.abs().sum(0) * ((2 * m + 24) * U + unit) + dv.abs().sum(0) * UNIT[s.q.dtype] * 1.01 + m * (LEAST[s.q.dtype] + 2.0 ** -24 * g.abs().amax(0))
+        assert bool(((dv.sum(0) - g.sum(0)).abs() <= off).all()), float(((dv.sum(0) - g.sum(0)).abs() - off).amax())
+    assert all(bool(t.isfinite().all()) for t in got)
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("d", [32, 64, 80, 128])
+@pytest.mark.parametrize("lengths", TEXTS, ids=lambda t: f"{len(t)}x{max(t)}")
+def test_gradient_of_one_far_bias_for_all(kind, d, lengths):
+    """A bias beside which logits are rounded, the same for all places: their weights add up to one, and are equal from 1e9 on."""
+    s = attention_inputs(lengths, 8, 8, d, kind, 0, 0)
+    s.bias, s.distances, s.reach = torch.zeros((8, 1), device=dev()), torch.zeros(1, dtype=torch.int32, device=dev()), 0
+    grad = normal((s.n, 8 * d), TYPES[kind], 5)
+    for value in [-4e3, -1e4, -1e5] + FAR:                         # (lse is so large that both kernels take rows' sums anew)
+        s.bias.fill_(value)
+        out, lse = pqt.pqt_attention(s.q, s.k, s.v, s.starts, **arguments(s))
+        got = pqt.pqt_attention_gradient(grad, s.q, s.k, s.v, out, lse, s.starts, **arguments(s))
+        rows_add_up(s, grad, got)
+        if abs(value) >= 1e9:
+            mean_gradient(s, grad, out, got, lambda m: (torch.full((m, m), 1.0 / m, dtype=torch.float64, device=dev()), torch.zeros((m, m), device=dev())))
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("d", [32, 64, 80, 128])
+@pytest.mark.parametrize("lengths", TEXTS, ids=lambda t: f"{len(t)}x{max(t)}")
+def test_gradient_of_one_key_left_with_a_far_bias(kind, d, lengths):
+    """All places masked but the query's own, whose bias is far: dv is grad, and nothing else has a gradient."""
+    s = attention_inputs(lengths, 8, 8, d, kind, 2, 1)
+    s.distances = torch.tensor([1, 0, 1], dtype=torch.int32, device=dev())
+    grad = normal((s.n, 8 * d), TYPES[kind], 5)
+    for value in FAR + [-1e4]:
+        s.bias = torch.tensor([[value, -INF]] * 8, device=dev())
+        out, lse = pqt.pqt_attention(s.q, s.k, s.v, s.starts, **arguments(s))
+        got = pqt.pqt_attention_gradient(grad, s.q, s.k, s.v, out, lse, s.starts, **arguments(s))
+        mean_gradient(s, grad, out, got, lambda m: (torch.eye(m, dtype=torch.float64, device=dev()), 1 - torch.eye(m, device=dev())))
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+def test_gradient_of_far_rows_beside_others(kind):
+    """Heads whose biases are all 1e5 lower beside ordinary ones, shared key heads, a padded batch, workgroups that share a key's queries: the ordinary heads' gradients are the
+    same bytes as without them, and the lower ones' weights add up to one a row."""
+    s = attention_inputs([900, 1, 0, 40], 8, 2, 64, kind, 32, 40, 901)
+    grad = torch.nan_to_num(normal((s.n, 512), TYPES[kind], 5))
+    out, lse = pqt.pqt_attention(s.q, s.k, s.v, s.starts, **arguments(s))
+    plain = pqt.pqt_attention_gradient(grad, s.q, s.k, s.v, out, lse, s.starts, **arguments(s))
+    s.bias[:4] -= 1e5                                              # the heads of the first keys' head
+    far, far_lse = pqt.pqt_attention(s.q, s.k, s.v, s.starts, **arguments(s))
+    got = pqt.pqt_attention_gradient(grad, s.q, s.k, s.v, far, far_lse, s.starts, **arguments(s))
+    base.check_attention(s, far, far_lse)
+    for a, b, w in zip(got, plain, (256, 64, 64)):
+        assert torch.equal(a[:, w:], b[:, w:])
+    assert torch.equal(got[3][4:], plain[3][4:])
+    assert bool((far_lse[:4][lse[:4].isfinite()] < -9e4).all())
+    for at, m in zip(s.at, s.of):                                  # four heads' weights add up to four
+        if m:
+            g, dv = grad[at:at + m, :256].double().unflatten(1, (4, 64)), got[2][at:at + m, :64].double()
+            off = g.abs().sum((0, 1)) * ((2 * m + 40) * U + base.weight_unit(s.q.dtype) * 1.01) + dv.abs().sum(0) * UNIT[s.q.dtype] * 1.01 + m * 2.0 ** -20
+            assert bool(((dv.sum(0) - g.sum((0, 1))).abs() <= off).all())
