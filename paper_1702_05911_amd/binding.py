@@ -783,8 +783,8 @@ def pqt_attention(q, k, v, starts, heads, scale=None, bias=None, distances=None,
 
 def pqt_attention_gradient(grad, q, k, v, out, lse, starts, heads, scale=None, bias=None, distances=None, lengths=None, grads=None, stream=None):
     """pqt_attention_gradient.  grad: (n, heads * d), the gradient of `out`; out, lse: what pqt_attention returned, the others what it was given.
-    grads: three matrices for the results, of q's, k's and v's sizes (slices of one, where these are), or None.  Returns (dq, dk, dv, dbias), dbias (heads,
-    buckets) float32, or None where there is no bias."""
+    grads: three matrices for the results, of q's, k's and v's sizes (slices of one, where these are), any of them None, or None.  Returns (dq, dk, dv, dbias), dbias
+    (heads, buckets) float32, or None where there is no bias.  Rows of no text are zeros in results that the call makes, and left as they were in the caller's."""
     if stream is not None:
         with _running_on(stream, grad, q, k, v, out, lse, starts, bias, distances, lengths, *(grads or ())):
             return pqt_attention_gradient(grad, q, k, v, out, lse, starts, heads, scale, bias, distances, lengths, grads)
@@ -798,15 +798,20 @@ def pqt_attention_gradient(grad, q, k, v, out, lse, starts, heads, scale=None, b
         raise ValueError(f"lse must be a contiguous float32 tensor {(heads, n)} on {device}")
     sptr, lptr, size, texts = _texts(starts, lengths, device)
     bptr, buckets, dptr, reach = _bias(bias, distances, heads, device)
-    dq, dk, dv = grads or (None, None, None)
-    dq, dqptr, _, dqstep = _result(dq, (n, wide), dtype, device)
-    dk, dkptr, _, dkstep = _result(dk, (n, narrow), dtype, device)
-    dv, dvptr, _, dvstep = _result(dv, (n, narrow), dtype, device)
+    to_q, to_k, to_v = grads or (None, None, None)
+    dq, dqptr, _, dqstep = _result(to_q, (n, wide), dtype, device)
+    dk, dkptr, _, dkstep = _result(to_k, (n, narrow), dtype, device)
+    dv, dvptr, _, dvstep = _result(to_v, (n, narrow), dtype, device)
+    clear = to_q is None and to_k is None and to_v is None
+    if not clear:                                                  # the library clears rows of no text in all three or in none
+        for made, to in ((dq, to_q), (dk, to_k), (dv, to_v)):
+            if to is None:
+                made.zero_()
     dbias = None if bias is None else torch.empty(heads, buckets, dtype=torch.float32, device=device)
     nbytes = _lib.pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, -1 if bias is None else reach)
     ws = _workspace(nbytes, device)
     _check(_lib.pqt_attention_gradient(gptr, gstep, *inputs, optr, ostep, lse.data_ptr(), kind, n, heads, kv_heads, d, sptr, lptr, size, texts,
-                                       d ** -0.5 if scale is None else scale, bptr, buckets, dptr, reach, 0 if grads else 1, dqptr, dqstep, dkptr, dkstep,
+                                       d ** -0.5 if scale is None else scale, bptr, buckets, dptr, reach, 1 if clear else 0, dqptr, dqstep, dkptr, dkstep,
                                        dvptr, dvstep, None if dbias is None else dbias.data_ptr(), ws.data_ptr() if nbytes else None, nbytes, device.index,
                                        _current(device.index)))
     return dq, dk, dv, dbias

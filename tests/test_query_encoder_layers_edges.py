@@ -237,3 +237,33 @@ def test_gradient_of_far_rows_beside_others(kind):
             g, dv = grad[at:at + m, :256].double().unflatten(1, (4, 64)), got[2][at:at + m, :64].double()
             off = g.abs().sum((0, 1)) * ((2 * m + 40) * U + base.weight_unit(s.q.dtype) * 1.01) + dv.abs().sum(0) * UNIT[s.q.dtype] * 1.01 + m * 2.0 ** -20
             assert bool(((dv.sum(0) - g.sum((0, 1))).abs() <= off).all())
+
+
+# ---- results that the call makes beside the caller's -----------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("given", [(0,), (1,), (2,), (0, 2), (1, 2), (), (0, 1, 2)])
+def test_gradients_some_of_which_the_call_makes(given):
+    """Of three results some are the caller's, whose rows of no text stay as they were, the others the call's own, whose are zeros."""
+    s = attention_inputs([20, 0, 90], 4, 2, 48, "bf16", 32, 20, 0, 0, 64, 70, 1, 30)
+    grad = torch.nan_to_num(normal((s.n, 192), torch.bfloat16, 5))
+    out, lse = pqt.pqt_attention(s.q, s.k, s.v, s.starts, **arguments(s))
+    want = pqt.pqt_attention_gradient(grad, s.q, s.k, s.v, out, lse, s.starts, **arguments(s))
+    held = [torch.full((s.n, w), 7.0, dtype=torch.bfloat16, device=dev()) if i in given else None for i, w in enumerate((192, 96, 96))]
+    left = [torch.full((s.n, w), float("nan"), dtype=torch.bfloat16, device=dev()) for w in (192, 96, 96) for _ in range(8)]
+    del left                                                       # what the allocator hands out next
+    got = pqt.pqt_attention_gradient(grad, s.q, s.k, s.v, out, lse, s.starts, grads=held, **arguments(s))
+    a, b = s.at[0], s.at[-1]
+    for i in range(3):
+        assert torch.equal(got[i][a:b], want[i][a:b])
+        rest = torch.cat([got[i][:a], got[i][b:]])
+        assert bool((rest == (7.0 if i in given else 0.0)).all()) and (held[i] is None or got[i] is held[i])
+    assert torch.equal(got[3], want[3])
+
+
+@gpu
+def test_gradients_are_three_or_none():
+    x = torch.zeros((4, 8), device=dev())
+    at, lse = torch.tensor([0, 4], device=dev()), torch.zeros((2, 4), device=dev())
+    for grads in ((x,), (x, x), (x, x, x, x)):
+        with pytest.raises(ValueError):
+            pqt.pqt_attention_gradient(x, x, x, x, x, lse, at, 2, grads=grads)
