@@ -718,12 +718,17 @@ def pqt_distance_buckets(buckets, far, both=True, device=None):
     return distances if device is None else distances.to(device)
 
 
+_MOST = 2 ** 31 - 1                # attention's heads, values, buckets and distances are 32-bit numbers of the library, which refuses far smaller ones
+
+
 def _heads(q, k, v, heads):
     """Sizes of attention's inputs: rows, values of a head, heads of keys, and the three with their strides and common type."""
     qptr, kind, qstep = _matrix("q", q)
     n, wide = q.shape
     if heads < 1 or wide % heads:
         raise ValueError(f"q has {wide} values in a row, which are not those of {heads} heads")
+    if wide > _MOST:
+        raise PqtError(PQT_EUNSUPPORTED, f"q has {wide} values in a row, at most {_MOST}")
     d = wide // heads
     narrow = k.shape[1] if k.dim() == 2 else 0
     if d < 1 or narrow < d or narrow % d or heads % (narrow // d):
@@ -756,6 +761,8 @@ def _bias(bias, distances, heads, device):
         raise ValueError(f"bias must be a contiguous float32 tensor (heads, buckets) on {device}, with {heads} heads")
     if distances is None or distances.dim() != 1 or distances.shape[0] % 2 == 0:
         raise ValueError("distances must be a 1-D tensor of the buckets of the distances -reach .. reach")
+    if bias.shape[1] > _MOST or distances.shape[0] > _MOST:
+        raise PqtError(PQT_EUNSUPPORTED, f"{bias.shape[1]} buckets of {distances.shape[0]} distances, at most {_MOST}")
     return bias.data_ptr(), bias.shape[1], _vector("distances", distances, distances.shape[0], _PLACES, device), distances.shape[0] // 2
 
 
@@ -835,6 +842,8 @@ def pqt_rms_norm_gradient_workspace(rows, D):
 
 
 def pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, reach):
+    if max(heads, kv_heads, d, reach) > _MOST or min(heads, kv_heads, d, reach) < -_MOST:
+        return 0                                                   # (32-bit numbers of the library)
     return int(_lib.pqt_attention_gradient_workspace(n, texts, heads, kv_heads, d, reach))
 
 

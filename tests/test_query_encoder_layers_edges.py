@@ -267,3 +267,31 @@ def test_gradients_are_three_or_none():
     for grads in ((x,), (x, x), (x, x, x, x)):
         with pytest.raises(ValueError):
             pqt.pqt_attention_gradient(x, x, x, x, x, lse, at, 2, grads=grads)
+
+
+# ---- sizes past 32 bits ----------------------------------------------------------------------------------------------
+def test_bias_of_more_buckets_or_distances_than_32_bits():
+    """2^32 + 4 buckets are not four, nor as many distances five."""
+    meta = torch.device("meta")
+    of = lambda buckets, distances: (torch.empty((2, buckets), device=meta), torch.empty(distances, dtype=torch.int32, device=meta))       # noqa: E731
+    for bias, distances in (of(2 ** 32 + 4, 5), of(4, 2 ** 32 + 5)):
+        with pytest.raises(pqt.PqtError) as e:
+            pqt._bias(bias, distances, 2, meta)
+        assert e.value.code == pqt.PQT_EUNSUPPORTED
+    assert pqt._bias(*of(4, 5), 2, meta)[1::2] == (4, 2)
+
+
+def test_workspace_of_more_heads_than_32_bits():
+    for args in ((100, 2, 2 ** 32 + 4, 4, 64, -1), (100, 2, 4, 2 ** 32 + 4, 64, -1), (100, 2, 4, 4, 2 ** 32 + 64, -1), (100, 2, 4, 4, 64, 2 ** 32), (100, 2, 4 - 2 ** 32, 4, 64, 0)):
+        assert pqt.pqt_attention_gradient_workspace(*args) == 0
+    assert pqt.pqt_attention_gradient_workspace(100, 2, 4, 4, 64, -1) > 0
+
+
+@gpu
+def test_rows_of_more_values_than_32_bits():
+    """A row of 2^32 + 64 values is one head of too many, not of 64."""
+    x, at = torch.empty((1, 2 ** 32 + 64), dtype=torch.bfloat16, device=dev()), torch.tensor([0, 1], device=dev())
+    for heads in (1, 2 ** 31 + 32):
+        with pytest.raises(pqt.PqtError) as e:
+            pqt.pqt_attention(x, x, x, at, heads)
+        assert e.value.code == pqt.PQT_EUNSUPPORTED
