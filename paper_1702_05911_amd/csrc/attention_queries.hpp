@@ -352,9 +352,9 @@ void launch_attention_queries(const AttentionArgs& args, int rows, bool direct, 
         typedef std::integral_constant<bool, true> Yes;
         if (rows == 16) of(Width<1>{}, Width<1>{}, Width<32>{}, No{});
         else if (rows == 64) of(Width<4>{}, Width<1>{}, Width<kKeys>{}, No{});
-        // (f16's two parts of ds and runs together leave heads of 96 no registers: 65 spilled)
-        else if constexpr (std::is_same<T, Half>::value && DP == 96) of(Width<4>{}, Width<2>{}, Width<kKeys>{}, No{});
         else if (!long_texts(g.n, g.texts)) of(Width<4>{}, Width<2>{}, Width<kKeys>{}, No{});
+        // (at heads of 96 runs spill 62 registers, f16's two parts of ds 75, and pay all the same: four texts of 4,096 tokens, 16 heads, without and with runs bf16 1,720 and 1,641 us, f16 2,120 and 2,041;
+        // two of 3,150, 8 heads of 80, 359 and 345, 438 and 425; 16 of 1,100, 12 heads of 96, 567 and 585, 691 and 712)
         else of(Width<4>{}, Width<2>{}, Width<kKeys>{}, Yes{});
     });
 }
