@@ -498,6 +498,8 @@ int pqt_rms_norm_gradient(const void* grad, int64_t grad_stride, const void* thr
  * gets zeros and an lse of -inf, as the rows that pad a text do.  Finite bias / scale counts within 2^90.  Rows of no text are left as they were, or,
  * with clear != 0, get the same.  out: n x heads * d of `type`, the type of q, k and v; lse: heads x n fp32, or NULL.
  * For bf16 and f16 the weights exp(z_ij - lse_i) are rounded to that type where they are multiplied; sums are fp32.
+ * Which kernel runs is chosen by n, texts and the heads, as lengths are not known on the host: a long text among many short ones takes longer than by itself (one of
+ * 2,500 tokens and 300 of 10, 16 heads of 64 bf16 values: 627 us in one call, 52 and 15 in two).
  * 1 <= d <= 128, reach <= 448, buckets <= 1024, 2^-32 <= scale <= 2^32; (n / 16 + texts + 1) * heads below 2^24 (beyond: PQT_EUNSUPPORTED).
  *
  * pqt_attention_gradient -- the gradients of q, k, v (n rows each, as those) and of bias (heads x buckets fp32, may be NULL) from that of out; out and

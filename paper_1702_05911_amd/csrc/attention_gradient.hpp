@@ -5,9 +5,13 @@
 //
 // Two kernels, so that no sum is anybody else's to add to: one has queries and walks the keys (dq, delta, dbias), one has keys and walks the queries of
 // all heads that share them (dk, dv).  Each takes the weights anew, seven products instead of five, and the same inputs give the same bytes.
-// Bound by the vector unit beside the matrix unit (ds is eight operations a pair, f16's lift three more) at two workgroups a compute unit: 64 texts of up to 512 tokens, 16
-// heads of 64 bf16 values, 280 us (146 and 143), 0.34 PFLOP/s of the seven products; two texts of 4,001 and 2,301, 8 heads of 80 f16 values, two of keys, 468 us (258 and 234).
+// Bound by neither unit's rate but by what a step waits for, at two workgroups a compute unit or fewer: 64 texts of up to 512 tokens, 16 heads of 64 bf16 values, 274 us (148 and 138),
+// 0.35 PFLOP/s of the seven products; the queries' kernel has the vector unit busy for 44 % of the time and the matrix unit for 16, the keys' for 39 and 23, and their wavefronts wait for 42
+// and 37 % of theirs (loads, LDS, barriers).  Two texts of 4,001 and 2,301, 8 heads of 80 f16 values, two of keys, 462 us (244 and 241): 34 and 24 %, 33 and 28, with 0.8 and 1.4
+// wavefronts a SIMD of the two that fit, as workgroups do not come out even.
 // As in the forward pass the products are turned so that a lane has one own row, whose weights and ds are the next product's operand where they are.
+//
+// fp32: the keys' kernel takes its weights from lse's rounded power of two, the queries' corrects for it (rest_of_power): 8 texts of up to 48 tokens are 7.2e-7 off, the plain form in 32 bits 5.1e-7.
 //
 // dbias: a wavefront's ds of 16 queries by 16 keys are added up along their diagonals by moving lanes, so that a lane has one distance, and go to a sum by
 // distance in LDS which only this lane's group of sixteen adds to; distances to buckets at the workgroup's end.  Tiles farther away than `reach`

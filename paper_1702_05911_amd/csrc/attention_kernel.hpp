@@ -5,9 +5,10 @@
 // taken transposed -- keys by queries, then values' columns by queries -- so that a lane has one query's logits, and the weights become the second
 // product's operand where they are.
 //
-// Bound by the vector unit beside the matrix unit: a weight is a multiplication and addition, a power of two, a sum and a conversion, for 4 d operations of
-// products (one text of 8,191 tokens, 16 heads of 128 bf16 values, four of keys: 506 us, 1.09 PFLOP/s where a large library product makes 1.6; 512 texts of up to
-// 256, 12 heads of 64: 198 us, 555 MB at 2.8 TB/s).
+// Long texts are bound by the vector and the matrix unit in turn: a weight is a multiplication and addition, a power of two, a sum and a conversion, for 4 d operations of
+// products, and each unit is busy for half of the time (one text of 8,191 tokens, 16 heads of 128 bf16 values, four of keys: 508 us, 1.08 PFLOP/s where a large library
+// product makes 1.6; its kernel spills 46 registers, none of them within a run of steps).  Shorter ones wait for their first loads and last stores: 512 texts of up to 256, 12 heads of 64, 201 us,
+// 555 MB at 2.8 TB/s, vector unit 57 % of the time, matrix unit 13 %, 41 % of the wavefronts' time waiting.
 #pragma once
 #include "attention.hpp"
 

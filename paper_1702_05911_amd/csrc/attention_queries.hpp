@@ -10,7 +10,7 @@ template <typename T, int DP, int NW, int RT, int BN, bool DIRECT, bool RUNS>
 __global__ __launch_bounds__(NW* kWave, NW == 4 && sizeof(T) == 2 && RT * DP < 256 ? (RT == 1 && DP <= (DIRECT ? 96 : 64) ? 3 : 2) : 1) void attention_query_gradient_kernel(AttentionArgs g) {
     constexpr int kThreads = NW * kWave, M = NW * RT * 16, KC = DP / 32, DT = DP / 16, kCopies = NW * 4;
     // f16: ds in two parts.  A row's ds cancel in their sum, so that their rounding shows in dq half as much again as dq's own (2,301 and 4,001 tokens, 80 values:
-    // 3.1e-4 of dq's size off, its own rounding 2.1e-4; the kernel 217 us, so 258).  For bf16, and in dk, it shows less: 1.4 times.
+    // 3.1e-4 of dq's size off, its own rounding 2.1e-4; the kernel 217 us, so 258, and by runs of steps 244).  For bf16, and in dk, it shows less: 1.4 times.
     constexpr bool kRest = std::is_same<T, Half>::value;
     typedef Tile<T, BN, DP> KeyTile;
     __shared__ __align__(16) typename KeyTile::S k_0[KeyTile::kSize], k_1[KeyTile::kSize], v_0[KeyTile::kSize], v_1[KeyTile::kSize];
