@@ -295,3 +295,53 @@ def test_rows_of_more_values_than_32_bits():
         with pytest.raises(pqt.PqtError) as e:
             pqt.pqt_attention(x, x, x, at, heads)
         assert e.value.code == pqt.PQT_EUNSUPPORTED
+
+
+MIXED = [c for c in base.ATTENTION if c[5] and 1 < sum(c[0]) <= 5000]
+
+
+@gpu
+@pytest.mark.parametrize("case", MIXED, ids=lambda c: f"{len(c[0])}x{max(c[0])}-" + "-".join(map(str, c[1:])))
+def test_rows_that_a_far_bias_leaves_among_others(case):
+    """A mask of -2e4 on the query itself and all behind it, as training code has it in place of -inf: a text's first token has nothing else, the others do.  Logits there are off by up to
+    2e4 * 8 U, a weight by a hundredth: the formula tells what is right."""
+    lengths, heads, kv, d, kind, buckets, reach, padded, pad, ids, behind = case
+    s = attention_inputs(lengths, heads, kv, d, kind, buckets, reach, padded, pad, ids, behind)
+    s.bias[:, s.distances[s.distances.shape[0] // 2:].unique().long()] -= 2e4
+    out, lse = pqt.pqt_attention(s.q, s.k, s.v, s.starts, **arguments(s))
+    base.check_attention(s, out, lse)
+    grad = torch.full((s.n, heads * d + pad), float("nan"), dtype=TYPES[kind], device=dev())[:, :heads * d]
+    for at, m in zip(s.at, s.of):
+        grad[at:at + m] = normal((m, heads * d), TYPES[kind], 77 + m, 0, 0.01)
+        assert m == 0 or bool((lse[:, at] < -1.9e4).all())
+    got = pqt.pqt_attention_gradient(grad, s.q, s.k, s.v, out, lse, s.starts, **arguments(s))
+    base.check_gradient(s, grad, out, lse, got)
+    again = pqt.pqt_attention_gradient(grad, s.q, s.k, s.v, out, lse, s.starts, **arguments(s))
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+@gpu
+def test_far_rows_in_a_graph():
+    """A captured gradient of such rows, replayed with other inputs and with none of them."""
+    s = attention_inputs([300, 1, 0, 77], 4, 2, 64, "bf16", 32, 40)
+    grad = torch.nan_to_num(normal((s.n, 256), torch.bfloat16, 5))
+    biases = [s.bias.clone(), s.bias - 1e9, s.bias.clone()]
+    biases[2][:, :16] = torch.finfo(torch.float32).min
+
+    def both():
+        out, lse = pqt.pqt_attention(s.q, s.k, s.v, s.starts, **arguments(s))
+        return (out, lse) + pqt.pqt_attention_gradient(grad, s.q, s.k, s.v, out, lse, s.starts, **arguments(s))
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = both()
+    for bias in biases + biases[::-1]:
+        s.bias.copy_(bias)
+        want = [t.clone() for t in both()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want)) and all(bool(t.isfinite().all()) for t in want)
