@@ -4,7 +4,8 @@
 // stays in registers, held by a group of lanes as in layer_norm.hip, the next row's values on their way while it is worked on.  Where
 // y goes into blocks, sixteen lanes hold a block's 128 values: its largest is found among them and the codes leave as 8 bytes a lane, so that y
 // itself, in 32 bits, never reaches memory.  Bound by memory: 100,003 rows of 960 bf16 values with the residual 147 us, 5.2 TB/s (a large copy 5.1); 16,385 rows of 2,000 into
-// blocks 46 us, 5.0 TB/s of the 230 MB it moves.
+// blocks 46 us, 5.0 TB/s of the 230 MB it moves.  fp32 rows of more than 16,384 values spill 146 to 219 registers, two rows of four pieces a lane: 4,000 of 16,384 with the
+// residual 228 us, 4.6 TB/s, of 20,000 489, 2.6 TB/s.
 //
 // Backward, with z = h * rstd and g = grad * weight: dx = through + rstd * (g - z * mean(g * z)), dweight = sum over rows of grad * z.  grad, h and what
 // arrives along the residual's way are read once; the columns' sums stay in registers while a group walks its rows, and are joined by
