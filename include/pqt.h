@@ -495,7 +495,8 @@ int pqt_rms_norm_gradient(const void* grad, int64_t grad_stride, const void* thr
  *     z_ij = scale * q_i . k_j + bias[head][distances[j - i]],   lse_i = log(sum over j of exp(z_ij)),   out_i = sum over j of exp(z_ij - lse_i) v_j.
  * bias: heads x buckets fp32, or NULL; distances: device array of 2 * reach + 1 integers (int32), the buckets of the distances -reach .. reach; farther
  * ones have their ends', and a bucket outside 0 .. buckets - 1 has no bias.  A bias of -inf masks its distances; a token to which it leaves nothing
- * gets zeros and an lse of -inf, as the rows that pad a text do.  Finite bias / scale counts within 2^90.  Rows of no text are left as they were, or,
+ * gets zeros and an lse of -inf, as the rows that pad a text do.  Finite bias / scale counts within 2^90; products are added to it
+ * in fp32, so that beside a bias of size B a logit may be off by d * 2^-24 * B.  Rows of no text are left as they were, or,
  * with clear != 0, get the same.  out: n x heads * d of `type`, the type of q, k and v; lse: heads x n fp32, or NULL.
  * For bf16 and f16 the weights exp(z_ij - lse_i) are rounded to that type where they are multiplied; sums are fp32.
  * Which kernel runs is chosen by n, texts and the heads, as lengths are not known on the host: a long text among many short ones takes longer than by itself (one of

@@ -303,8 +303,8 @@ MIXED = [c for c in base.ATTENTION if c[5] and 1 < sum(c[0]) <= 5000]
 @gpu
 @pytest.mark.parametrize("case", MIXED, ids=lambda c: f"{len(c[0])}x{max(c[0])}-" + "-".join(map(str, c[1:])))
 def test_rows_that_a_far_bias_leaves_among_others(case):
-    """A mask of -2e4 on the query itself and all behind it, as training code has it in place of -inf: a text's first token has nothing else, the others do.  Logits there are off by up to
-    2e4 * 8 U, a weight by a hundredth: the formula tells what is right."""
+    """A mask of -2e4 on the query itself and all behind it, as training code has it in place of -inf: a text's first token has nothing else, the others do.  Logits there are off by
+    some 2e4 * 8 U, a weight by a hundredth: the formula tells what is right."""
     lengths, heads, kv, d, kind, buckets, reach, padded, pad, ids, behind = case
     s = attention_inputs(lengths, heads, kv, d, kind, buckets, reach, padded, pad, ids, behind)
     s.bias[:, s.distances[s.distances.shape[0] // 2:].unique().long()] -= 2e4
